@@ -277,6 +277,41 @@ int moe_trans(moe_handle_t h, const int32_t* expert_dest, const int32_t* pool_ve
 int moe_agg(moe_handle_t h, const int32_t* expert_dest, int n_tensors, const float* const* group_grads,
             float* const* pool_grads, const size_t* floats_per_expert, void* stream);
 
+/* ---- around the layer in a training step ------------------------------------------------------------
+ *
+ * The layer is one half of a pre-norm block: what its gate reads is the layer norm of the residual stream, and the
+ * stream goes on past it.  These two calls need no handle: a model's norms are as many as its widths.
+ *
+ * moe_norm_t: rows >= 0 (none: the forward call does nothing, the backward call writes zero parameter gradients), 1 <= d <= 16384, any d
+ * (rows lie d elements apart and need no alignment beyond an element's), eps > 0 and finite. */
+typedef struct {
+    int rows, d;
+    moe_dtype_t dtype;          /* of the activations; parameters, statistics and parameter gradients are float */
+    float eps;
+} moe_norm_t;
+
+/* S = X + R, rounded once to the element type; mean = sum_c S / d, rstd = 1 / sqrt(sum_c (S - mean)^2 / d + eps) per row in fp32;
+ * Y = (S - mean) rstd gamma + beta, rounded once.
+ *   in : X[rows,d] elt, R[rows,d] elt (the residual stream; NULL: S is X itself), gamma[d], beta[d] (NULL: none) float
+ *   out: S[rows,d] elt (given with R, NULL without), Y[rows,d] elt, mean[rows], rstd[rows] float (both or neither: a backward call
+ *        needs them, a forward-only pass does not)
+ * S may be X or R, and without R Y may be X; other overlaps are not allowed. */
+int moe_norm_fwd(const moe_norm_t* cfg, const void* X, const void* R, const float* gamma, const float* beta,
+                 void* S, void* Y, float* mean, float* rstd, void* stream);
+
+/* Bytes of workspace (256-byte aligned device memory) moe_norm_bwd may use for any number of rows of this width and type. */
+int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes);
+
+/* Gradient of moe_norm_fwd.  With xh = (S - mean) rstd and g = dY gamma:
+ *   dX = dS + rstd (g - sum_c g / d - xh sum_c (g xh) / d), rounded once;  dgamma = sum_rows dY xh,  dbeta = sum_rows dY
+ * fp32 sums in a fixed order (same bits every run on a GPU of as many compute units).
+ *   in : dY[rows,d] elt, S[rows,d] elt (X where there was no R), gamma[d], mean[rows], rstd[rows] as moe_norm_fwd left them;
+ *        dS[rows,d] elt (the residual stream's own gradient; NULL: none)
+ *   out: dX[rows,d] elt (the gradient of X and of R alike), dgamma[d] float, dbeta[d] float (NULL: not wanted)
+ * dX may be dY or dS.  Uses the workspace. */
+int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd,
+                 const void* dS, void* dX, float* dgamma, float* dbeta, void* ws, void* stream);
+
 /* ---- planner (Sections 4.2-4.3 and 5.3 of the paper) ------------------------------------------
  *
  * moe_plan runs the paper's greedy search for a lightweight expert placement (Algorithm 1) on the

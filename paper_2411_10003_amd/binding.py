@@ -29,7 +29,7 @@ EXPORTS = [
     "moe_combine", "moe_combine_bwd", "moe_expert_ffn_bwd", "moe_dispatch_bwd", "moe_gate_bwd",
     "moe_plan", "moe_gate_bwd_params", "moe_input_grad", "moe_expert_ffn_bwd_acc", "moe_trans", "moe_recv_layout",
     "moe_dispatch_after_counts", "moe_set_act_saved", "moe_expert_counts_static", "moe_agg", "moe_calib_copy", "moe_calib_mfma",
-    "moe_calib_round_bf16",
+    "moe_calib_round_bf16", "moe_norm_fwd", "moe_norm_workspace_bytes", "moe_norm_bwd",
 ]
 
 
@@ -51,6 +51,10 @@ class _Layout(ctypes.Structure):
 class _Planner(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("D", "E", "n", "overlap")] + \
                [(n, ctypes.c_double) for n in ("alpha", "size_input", "size_params", "size_grads", "B", "t", "T_FNEC", "T_BNEC")]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 class _PlanOut(ctypes.Structure):
@@ -96,6 +100,9 @@ def load() -> ctypes.CDLL:
         lib.moe_calib_mfma.argtypes = [vp, ctypes.c_size_t, ip, ctypes.POINTER(ip), ctypes.POINTER(ip), vp]
         lib.moe_calib_round_bf16.argtypes = [vp, vp, ctypes.c_size_t, vp]
         lib.moe_recv_layout.argtypes = [vp, ctypes.POINTER(_Layout), vp, ctypes.POINTER(_Layout), vp]
+        lib.moe_norm_fwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 9
+        lib.moe_norm_workspace_bytes.argtypes = [ctypes.POINTER(_Norm), ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_norm_bwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 11
         lib.moe_plan.argtypes = [ctypes.POINTER(_Planner), vp, ctypes.POINTER(_PlanOut), vp]
         _lib = lib
     return _lib
@@ -264,6 +271,61 @@ def _entry(name: str) -> int:
     if name not in _entries:
         _entries[name] = ctypes.cast(getattr(load(), name), ctypes.c_void_p).value
     return _entries[name]
+
+
+def _checked(rc: int, where: str) -> None:
+    if rc != 0:
+        lib = load()
+        detail = lib.moe_status_string(rc).decode()
+        if rc == -7:
+            detail += f", hipError {lib.moe_last_hip_error()}"
+        raise MoeError(rc, where, detail)
+
+
+class Norm:
+    """The layer norm of one width and type, with the workspace of its backward pass.  The rows of a call are those of its first tensor."""
+
+    MAX_CALLS = 64                                         # row counts whose call objects are kept
+
+    def __init__(self, *, d: int, dtype: str, eps: float = 1e-5, device="cuda:0", alloc_workspace: bool = True):
+        self.lib = load()
+        self.d, self.eps = d, eps
+        self.elt = TORCH_DTYPE[DTYPES[dtype]]
+        self._dtype = DTYPES[dtype]
+        n = ctypes.c_size_t()
+        _checked(self.lib.moe_norm_workspace_bytes(ctypes.byref(_Norm(0, d, self._dtype, eps)), ctypes.byref(n)), "moe_norm_workspace_bytes")
+        self.workspace_bytes = n.value
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+        self._calls: Dict[int, tuple] = {}
+
+    def _for_rows(self, first: torch.Tensor):
+        rows, rest = divmod(first.numel(), self.d)
+        calls = self._calls.get(rows)
+        if rest:
+            raise ValueError(f"{first.numel()} elements are no rows of {self.d}")
+        if calls is None:
+            if len(self._calls) >= self.MAX_CALLS:
+                self._calls.clear()
+            c = _Norm(rows, self.d, self._dtype, self.eps)
+            e, f, all_, cfg = self.elt, torch.float32, rows * self.d, ctypes.addressof(c)
+            fwd = (cfg, (e, all_, "X"), (e, all_, "residual"), (f, self.d, "gamma"), (f, self.d, "beta"), (e, all_, "total"), (e, all_, "Y"),
+                   (f, rows, "mean"), (f, rows, "rstd"), "int")
+            bwd = (cfg, (e, all_, "dY"), (e, all_, "S"), (f, self.d, "gamma"), (f, rows, "mean"), (f, rows, "rstd"), (e, all_, "residual_grad"),
+                   (e, all_, "dX"), (f, self.d, "dgamma"), (f, self.d, "dbeta"), "int", "int")
+            calls = self._calls[rows] = (_call_type()(_entry("moe_norm_fwd"), fwd, _ptr), _call_type()(_entry("moe_norm_bwd"), bwd, _ptr), c)
+        return calls
+
+    def fwd(self, X, gamma, beta, Y, *, residual=None, total=None, mean=None, rstd=None):
+        rc = self._for_rows(X)[0](X, residual, gamma, beta, total, Y, mean, rstd, _stream())
+        if rc != 0:
+            _checked(rc, "moe_norm_fwd")
+
+    def bwd(self, dY, S, gamma, mean, rstd, dX, dgamma, dbeta=None, *, residual_grad=None):
+        if self.ws is None:
+            raise ValueError("no workspace attached")
+        rc = self._for_rows(dY)[1](dY, S, gamma, mean, rstd, residual_grad, dX, dgamma, dbeta, self.ws.data_ptr(), _stream())
+        if rc != 0:
+            _checked(rc, "moe_norm_bwd")
 
 
 class Handle:

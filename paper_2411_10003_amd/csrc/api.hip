@@ -354,6 +354,44 @@ int moe_recv_layout(moe_handle_t h, const moe_layout_t* local, const int32_t* re
     return hip_status(launch_recv_layout(h->s, local->dest_slots, recv_offsets, out->slot_offsets, out->dest_slots, (hipStream_t)stream));
 }
 
+static int check_norm(const moe_norm_t* c)
+{
+    if (!c) return MOE_ERR_NULL;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    if (c->rows < 0 || c->rows >= (1 << 30) || c->d < 1 || c->d > NORM_MAX_D) return MOE_ERR_SHAPE;
+    if (!(c->eps > 0.0f) || !std::isfinite(c->eps)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+int moe_norm_fwd(const moe_norm_t* cfg, const void* X, const void* R, const float* gamma, const float* beta,
+                 void* S, void* Y, float* mean, float* rstd, void* stream)
+{
+    const int rc = check_norm(cfg);
+    if (rc != MOE_OK) return rc;
+    if (cfg->rows == 0) return MOE_OK;
+    if (!X || !gamma || !Y || (R == nullptr) != (S == nullptr) || (mean == nullptr) != (rstd == nullptr)) return MOE_ERR_NULL;
+    return hip_status(launch_norm_fwd(*cfg, X, R, gamma, beta, S, Y, mean, rstd, (hipStream_t)stream));
+}
+
+int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes)
+{
+    const int rc = check_norm(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!bytes) return MOE_ERR_NULL;
+    *bytes = align256((size_t)NORM_PARTIALS * 2 * cfg->d * sizeof(float));
+    return MOE_OK;
+}
+
+int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd,
+                 const void* dS, void* dX, float* dgamma, float* dbeta, void* ws, void* stream)
+{
+    const int rc = check_norm(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!dgamma || (cfg->rows > 0 && (!dY || !S || !gamma || !mean || !rstd || !dX))) return MOE_ERR_NULL;
+    if (!ws || misaligned(ws)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_norm_bwd(*cfg, dY, S, gamma, mean, rstd, dS, dX, dgamma, dbeta, (float*)ws, (hipStream_t)stream));
+}
+
 int moe_plan(const moe_planner_t* cfg, const int32_t* gating, const moe_plan_out_t* out, void* stream)
 {
     if (!cfg || !gating || !out) return MOE_ERR_NULL;

@@ -118,6 +118,13 @@ hipError_t launch_recv_layout(const moe_shape_t& s, const int32_t* local_dest_sl
 hipError_t launch_plan(const moe_planner_t& cfg, const int32_t* gating, const moe_plan_out_t& out, hipStream_t st);
 hipError_t launch_dispatch_bwd(const moe_shape_t& s, const void* dXp, const int32_t* pos, void* dX, hipStream_t st);
 
+constexpr int NORM_MAX_D = 16384;
+constexpr int NORM_PARTIALS = 512;     // blocks of the norm's gradient, each with one partial sum of the parameters' gradients
+hipError_t launch_norm_fwd(const moe_norm_t& c, const void* X, const void* R, const float* gamma, const float* beta, void* S, void* Y,
+                           float* mean, float* rstd, hipStream_t st);
+hipError_t launch_norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd, const void* dS,
+                           void* dX, float* dgamma, float* dbeta, float* partial, hipStream_t st);
+
 constexpr int SPLIT_UNITS = 320;       // partial tiles the K-split of a last round may need: at most one per block
 constexpr int UNEVEN_UNITS = 512;      // and an uneven cut: two for each of fewer tiles than there are blocks
 constexpr int SPLIT_COUNTERS = 1024;   // a counter for each of them, in the smaller tiles

@@ -1,0 +1,404 @@
+// The layer norm of a pre-norm block with the sum of the residual stream, and its gradient.
+//
+// forward, per row of d elements:  s = x + r (rounded once to the element type),  mean = sum s / d,
+//   rstd = 1 / sqrt(sum (s - mean)^2 / d + eps),  y = (s - mean) rstd gamma + beta
+// backward, with xh = (s - mean) rstd, g = dy gamma, c1 = sum g / d, c2 = sum g xh / d:
+//   dx = ds + rstd (g - c1 - xh c2);  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
+//
+// Bound by HBM: two to four elements move per element of the rows and a dozen vector instructions go with them.  A row
+// is read once: it stays in the registers of the TPR threads that share it, U pieces of 16 bytes each, through both of the forward sums
+// (the variance is that of the centred row, not a difference of squares).  Sums are fp32 and in a fixed order.
+#include "internal.h"
+
+#include <type_traits>
+
+namespace {
+
+// 16 bytes of a row.  Rows of odd widths begin at any multiple of an element; the memory path takes such requests whole.
+template <typename ET> struct Piece;
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    typedef unsigned mem_t __attribute__((ext_vector_type(4), aligned(4)));
+    typedef float one_t;
+    static __device__ __forceinline__ void unpack(const moe_piece_t& v, float* f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+    }
+    static __device__ __forceinline__ moe_piece_t pack(const float* f) {
+        return moe_piece_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+};
+template <> struct Piece<bf16_t> {
+    static constexpr int N = 8;
+    typedef unsigned mem_t __attribute__((ext_vector_type(4), aligned(2)));
+    typedef bf16_t one_t;
+    static __device__ __forceinline__ void unpack(const moe_piece_t& v, float* f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ moe_piece_t pack(const float* f) {
+        return moe_piece_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+    }
+};
+
+// `n`: elements of this piece inside the row; only with TAIL is it ever less than a whole piece.
+template <typename ET, bool TAIL> __device__ __forceinline__ moe_piece_t load_row_piece(const ET* p, int n)
+{
+    typedef typename Piece<ET>::mem_t mem_t;
+    if (!TAIL || n == Piece<ET>::N) return *reinterpret_cast<const mem_t*>(p);
+    float f[Piece<ET>::N];
+#pragma unroll
+    for (int i = 0; i < Piece<ET>::N; ++i) {
+        if constexpr (std::is_same<ET, float>::value) f[i] = i < n ? p[i] : 0.0f;
+        else f[i] = i < n ? bf16_to_f32(p[i]) : 0.0f;
+    }
+    return Piece<ET>::pack(f);
+}
+template <typename ET, bool TAIL> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
+{
+    typedef typename Piece<ET>::mem_t mem_t;
+    if (!TAIL || n == Piece<ET>::N) { *reinterpret_cast<mem_t*>(p) = v; return; }
+    float f[Piece<ET>::N];
+    Piece<ET>::unpack(v, f);
+#pragma unroll
+    for (int i = 0; i < Piece<ET>::N; ++i)
+        if (i < n) {
+            if constexpr (std::is_same<ET, float>::value) p[i] = f[i];
+            else p[i] = (bf16_t)(__float_as_uint(f[i]) >> 16);             // it is one already
+        }
+}
+// The parameters of a piece's columns.
+template <int N, bool TAIL> __device__ __forceinline__ void load_columns(const float* p, int n, float* f)
+{
+    typedef float quad_t __attribute__((ext_vector_type(4), aligned(4)));
+    if (!TAIL || n == N) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const quad_t q = *reinterpret_cast<const quad_t*>(p + 4 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[4 * i + k] = q[k];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = i < n ? p[i] : 0.0f;
+}
+
+constexpr int threads_of(int tpr) { return tpr > 256 ? tpr : 256; }
+
+// Sums of M values over the TPR threads of a row, the same bits in each of them.  Rows of more than a wave go through `words`
+// (LDS, M x waves floats); two sets of them in turn, so that one barrier a sum is enough.
+template <int TPR, int M> __device__ __forceinline__ void row_sums(float (&v)[M], float* words, int& turn)
+{
+#pragma unroll
+    for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] += __shfl_xor(v[i], off, 64);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        float* w = words + turn * (2 * W);
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < M; ++i) w[i * W + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            float s = 0.0f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) s += w[i * W + k];
+            v[i] = s;
+        }
+    }
+}
+
+template <typename ET, int TPR, int U, bool TAIL>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
+    const ET* X, const ET* R, const float* __restrict__ gamma, const float* __restrict__ beta, ET* S, ET* Y,
+    float* __restrict__ mean_out, float* __restrict__ rstd_out, int rows, int d, float eps)
+{
+    constexpr int N = Piece<ET>::N, RPB = threads_of(TPR) / TPR;
+    __shared__ float words[TPR > 64 ? 4 * (TPR / 64) : 1];
+    int turn = 0;
+    const int c = threadIdx.x % TPR;
+    const float inv_d = 1.0f / (float)d;
+    // rows of a block are a block apart from the next block's; the threads of a row leave the loop together
+    for (long row = (long)blockIdx.x * RPB + threadIdx.x / TPR; row < rows; row += (long)gridDim.x * RPB) {
+        const size_t base = (size_t)row * d;
+        moe_piece_t x[U], r[U];
+        int n[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            n[u] = min(N, max(0, d - (c + u * TPR) * N));
+            x[u] = moe_piece_t{0, 0, 0, 0};
+            if (n[u] > 0) x[u] = load_row_piece<ET, TAIL>(X + base + (c + u * TPR) * N, n[u]);
+        }
+        if (R) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                r[u] = moe_piece_t{0, 0, 0, 0};
+                if (n[u] > 0) r[u] = load_row_piece<ET, TAIL>(R + base + (c + u * TPR) * N, n[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float a[N], b[N];
+                Piece<ET>::unpack(x[u], a);
+                Piece<ET>::unpack(r[u], b);
+#pragma unroll
+                for (int i = 0; i < N; ++i) a[i] += b[i];
+                x[u] = Piece<ET>::pack(a);
+                if (n[u] > 0) store_row_piece<ET, TAIL>(S + base + (c + u * TPR) * N, x[u], n[u]);
+            }
+        }
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float a[N];
+            Piece<ET>::unpack(x[u], a);                    // zeros past the row's end
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[0] += a[i];
+        }
+        row_sums<TPR>(sum, words, turn);
+        const float mean = sum[0] * inv_d;
+        float sq[1] = {0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float a[N];
+            Piece<ET>::unpack(x[u], a);
+            if (n[u] > 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float v = (!TAIL || i < n[u]) ? a[i] - mean : 0.0f;
+                    sq[0] = fmaf(v, v, sq[0]);
+                }
+        }
+        row_sums<TPR>(sq, words, turn);
+        const float rstd = 1.0f / sqrtf(fmaf(sq[0], inv_d, eps));
+        if (mean_out && c == 0) { mean_out[row] = mean; rstd_out[row] = rstd; }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (n[u] <= 0) continue;
+            float a[N], g[N], b[N];
+            Piece<ET>::unpack(x[u], a);
+            load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g);
+#pragma unroll
+            for (int i = 0; i < N; ++i) b[i] = 0.0f;
+            if (beta) load_columns<N, TAIL>(beta + (c + u * TPR) * N, n[u], b);
+#pragma unroll
+            for (int i = 0; i < N; ++i) a[i] = fmaf((a[i] - mean) * rstd, g[i], b[i]);
+            store_row_piece<ET, TAIL>(Y + base + (c + u * TPR) * N, Piece<ET>::pack(a), n[u]);
+        }
+    }
+}
+
+// Columns stay with their thread from row to row, so the parameters' gradients are summed in registers; a block leaves one partial
+// sum of each in `partial`, [block][2][d].
+template <typename ET, int TPR, int U, bool TAIL>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
+    const ET* dY, const ET* __restrict__ S, const float* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
+    const ET* dS, ET* dX, float* __restrict__ partial, int rows, int d)
+{
+    constexpr int N = Piece<ET>::N, RPB = threads_of(TPR) / TPR, COLS = TPR * U * N;
+    __shared__ float words[TPR > 64 ? 4 * (TPR / 64) : 1];
+    __shared__ float join[RPB > 1 ? RPB * COLS : 1];
+    int turn = 0;
+    const int c = threadIdx.x % TPR, in_block = threadIdx.x / TPR;
+    const float inv_d = 1.0f / (float)d;
+    // gamma of more than 16 columns (8 where a wave has 128 registers) is read again for every row: with it the registers would not hold the sums
+    constexpr bool KEEP_GAMMA = U * N <= (TPR > 512 ? 8 : 16);
+    float g[KEEP_GAMMA ? U : 1][N], sg[U][N], sb[U][N];
+    int n[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        n[u] = min(N, max(0, d - (c + u * TPR) * N));
+#pragma unroll
+        for (int i = 0; i < N; ++i) sg[u][i] = sb[u][i] = 0.0f;
+        if constexpr (KEEP_GAMMA) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[u][i] = 0.0f;
+            if (n[u] > 0) load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g[u]);
+        }
+    }
+    auto columns = [&](int u) -> float (&)[N] {
+        if constexpr (KEEP_GAMMA) {
+            return g[u];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[0][i] = 0.0f;
+            if (n[u] > 0) load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g[0]);
+            return g[0];
+        }
+    };
+    for (long row = (long)blockIdx.x * RPB + in_block; row < rows; row += (long)gridDim.x * RPB) {
+        const size_t base = (size_t)row * d;
+        moe_piece_t py[U], ps[U], pr[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            py[u] = ps[u] = pr[u] = moe_piece_t{0, 0, 0, 0};
+            if (n[u] > 0) {
+                py[u] = load_row_piece<ET, TAIL>(dY + base + (c + u * TPR) * N, n[u]);
+                ps[u] = load_row_piece<ET, TAIL>(S + base + (c + u * TPR) * N, n[u]);
+                if (dS) pr[u] = load_row_piece<ET, TAIL>(dS + base + (c + u * TPR) * N, n[u]);
+            }
+        }
+        const float mean = mean_in[row], rstd = rstd_in[row];
+        float c12[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float y[N], s[N];
+            float (&gm)[N] = columns(u);
+            Piece<ET>::unpack(py[u], y);                   // zeros past the row's end, and gamma too
+            Piece<ET>::unpack(ps[u], s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float xh = (s[i] - mean) * rstd, gy = y[i] * gm[i];
+                c12[0] += gy;
+                c12[1] = fmaf(gy, xh, c12[1]);
+                sg[u][i] = fmaf(y[i], xh, sg[u][i]);
+                sb[u][i] += y[i];
+            }
+        }
+        row_sums<TPR>(c12, words, turn);
+        const float c1 = c12[0] * inv_d, c2 = c12[1] * inv_d;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (n[u] <= 0) continue;
+            float y[N], s[N], r[N];
+            float (&gm)[N] = columns(u);
+            Piece<ET>::unpack(py[u], y);
+            Piece<ET>::unpack(ps[u], s);
+            Piece<ET>::unpack(pr[u], r);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float xh = (s[i] - mean) * rstd;
+                r[i] = fmaf(rstd, fmaf(-xh, c2, fmaf(y[i], gm[i], -c1)), r[i]);
+            }
+            store_row_piece<ET, TAIL>(dX + base + (c + u * TPR) * N, Piece<ET>::pack(r), n[u]);
+        }
+    }
+    float* out = partial + (size_t)blockIdx.x * 2 * d;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if constexpr (RPB > 1) {
+            __syncthreads();                               // the rows of a block are joined in LDS
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) join[in_block * COLS + i * (TPR * U) + u * TPR + c] = k ? sb[u][i] : sg[u][i];
+            __syncthreads();
+            for (int j = threadIdx.x; j < COLS; j += threads_of(TPR)) {
+                float s = 0.0f;
+#pragma unroll
+                for (int b = 0; b < RPB; ++b) s += join[b * COLS + j];
+                const int col = (j % (TPR * U)) * N + j / (TPR * U);
+                if (col < d) out[(size_t)k * d + col] = s;
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i < n[u]) out[(size_t)k * d + (c + u * TPR) * N + i] = k ? sb[u][i] : sg[u][i];
+        }
+    }
+}
+
+// The partial sums of 32 columns, 32 lines of them at a time; their order is fixed by the number of blocks.
+constexpr int JOIN_COLS = 32, JOIN_LINES = 32;
+__global__ __launch_bounds__(JOIN_COLS * JOIN_LINES) void norm_join_kernel(const float* __restrict__ partial, int blocks, int d,
+                                                                         float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    __shared__ float words[JOIN_LINES][JOIN_COLS + 1];
+    const int col = blockIdx.x * JOIN_COLS + threadIdx.x % JOIN_COLS, line = threadIdx.x / JOIN_COLS;
+    float s = 0.0f;
+    if (col < 2 * d)
+        for (int b = line; b < blocks; b += JOIN_LINES) s += partial[(size_t)b * 2 * d + col];
+    words[line][threadIdx.x % JOIN_COLS] = s;
+    __syncthreads();
+    if (line != 0 || col >= 2 * d) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < JOIN_LINES; ++i) t += words[i][threadIdx.x];
+    if (col < d) dgamma[col] = t;
+    else if (dbeta) dbeta[col - d] = t;
+}
+
+// Threads of a row and pieces of each, by the width.  Forward: the fewest threads that hold it in four pieces, so that most rows need no
+// barrier and every thread has several requests on their way.  Backward, with the parameters' gradients in registers beside the row:
+// two pieces where the threads are there.
+template <typename ET, bool BWD, typename F> hipError_t by_width(int d, F f)
+{
+    const int nv = (d + Piece<ET>::N - 1) / Piece<ET>::N;
+    const bool tail = d % Piece<ET>::N != 0;
+    auto with = [&](auto TPR, auto U) { return tail ? f(TPR, U, std::true_type{}) : f(TPR, U, std::false_type{}); };
+#define MOE_NORM_CASE(T, UU) if (nv <= T * UU) return with(std::integral_constant<int, T>{}, std::integral_constant<int, UU>{});
+    MOE_NORM_CASE(16, 1)
+    MOE_NORM_CASE(16, 2)
+    MOE_NORM_CASE(16, 4)
+    MOE_NORM_CASE(64, 2)
+    if constexpr (BWD) {
+        MOE_NORM_CASE(256, 1)
+        MOE_NORM_CASE(256, 2)
+        MOE_NORM_CASE(512, 2)
+        MOE_NORM_CASE(512, 4)
+    } else {
+        MOE_NORM_CASE(64, 4)
+        MOE_NORM_CASE(256, 2)
+        MOE_NORM_CASE(256, 4)
+        MOE_NORM_CASE(1024, 2)
+    }
+    if constexpr (Piece<ET>::N == 4) { MOE_NORM_CASE(1024, 4) }
+#undef MOE_NORM_CASE
+    return hipErrorInvalidValue;                           // wider than NORM_MAX_D: the entry points refuse it
+}
+
+inline int blocks_for(int rows, int tpr, int most)
+{
+    const int rpb = threads_of(tpr) / tpr, n = (rows - 1) / rpb + 1;
+    return n < most ? n : most;
+}
+
+template <typename ET>
+hipError_t norm_fwd(const moe_norm_t& c, const void* X, const void* R, const float* gamma, const float* beta, void* S, void* Y,
+                    float* mean, float* rstd, hipStream_t st)
+{
+    return by_width<ET, false>(c.d, [&](auto TPR, auto U, auto TAIL) {
+        constexpr int tpr = decltype(TPR)::value;
+        hipLaunchKernelGGL((norm_fwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value>), dim3(blocks_for(c.rows, tpr, 1 << 20)), dim3(threads_of(tpr)), 0, st,
+                           (const ET*)X, (const ET*)R, gamma, beta, (ET*)S, (ET*)Y, mean, rstd, c.rows, c.d, c.eps);
+        return hipGetLastError();
+    });
+}
+
+template <typename ET>
+hipError_t norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd, const void* dS,
+                    void* dX, float* dgamma, float* dbeta, float* partial, hipStream_t st)
+{
+    int blocks = 0;
+    hipError_t e = c.rows == 0 ? hipSuccess : by_width<ET, true>(c.d, [&](auto TPR, auto U, auto TAIL) {
+        constexpr int tpr = decltype(TPR)::value;
+        blocks = blocks_for(c.rows, tpr, NORM_PARTIALS);
+        hipLaunchKernelGGL((norm_bwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value>), dim3(blocks), dim3(threads_of(tpr)), 0, st,
+                           (const ET*)dY, (const ET*)S, gamma, mean, rstd, (const ET*)dS, (ET*)dX, partial, c.rows, c.d);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(norm_join_kernel, dim3((2 * c.d + JOIN_COLS - 1) / JOIN_COLS), dim3(JOIN_COLS * JOIN_LINES), 0, st, partial, blocks, c.d, dgamma, dbeta);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_fwd(const moe_norm_t& c, const void* X, const void* R, const float* gamma, const float* beta, void* S, void* Y,
+                           float* mean, float* rstd, hipStream_t st)
+{
+    if (c.rows == 0) return hipSuccess;
+    return c.dtype == MOE_F32 ? norm_fwd<float>(c, X, R, gamma, beta, S, Y, mean, rstd, st) : norm_fwd<bf16_t>(c, X, R, gamma, beta, S, Y, mean, rstd, st);
+}
+
+hipError_t launch_norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd, const void* dS,
+                           void* dX, float* dgamma, float* dbeta, float* partial, hipStream_t st)
+{
+    return c.dtype == MOE_F32 ? norm_bwd<float>(c, dY, S, gamma, mean, rstd, dS, dX, dgamma, dbeta, partial, st)
+                              : norm_bwd<bf16_t>(c, dY, S, gamma, mean, rstd, dS, dX, dgamma, dbeta, partial, st);
+}
