@@ -312,6 +312,36 @@ int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes);
 int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd,
                  const void* dS, void* dX, float* dgamma, float* dbeta, void* ws, void* stream);
 
+/* moe_muon_step: the update of expert parameters that comes before they are transferred (Section 5.1), by the Muon rule: momentum,
+ * orthogonalised by a few Newton-Schulz products.  n_tensors (1..8) tensors of `count` matrices each; tensor i holds matrices of
+ * rows x cols, or of cols x rows where transposed[i] is 1 (W1, W3 [G,d,h] and W2 [G,h,d] of the same experts are one call).  Per matrix:
+ *   M <- momentum M + G;   U = G + momentum M where nesterov = 1, else M;   X = U / (|U|_F + eps)
+ *   `steps` times, with X on its long side:  A = X X^T,  X <- a X + (b A + c A A) X
+ *   W <- (1 - lr weight_decay) W - lr scale X
+ * M, |U| and the sums are fp32 or more.  For MOE_BF16 weights the iterates are kept in 11 bits, fp16 with a scale (X is then within some
+ * 1e-3 of what 64 bits give, W within its own rounding); for MOE_F32 weights in 22.
+ * Limits: rows, cols >= 1, rows * cols < 2^30, each <= 65536; n_tensors * count <= 65535; 1 <= steps <= 16; 0 <= momentum < 1; eps > 0;
+ * |a|, |b|, |c| <= 16; lr, weight_decay, scale finite. */
+typedef struct {
+    int n_tensors, count, rows, cols;
+    int transposed[8];
+    moe_dtype_t dtype;          /* of the weights; gradients and momenta are float */
+    int nesterov, steps;
+    float momentum, eps, a, b, c;
+    float lr, weight_decay, scale;
+} moe_muon_t;
+
+/* Bytes of workspace (256-byte aligned device memory) a step of these sizes uses. */
+int moe_muon_workspace_bytes(const moe_muon_t* cfg, size_t* bytes);
+
+/*   in    : on the HOST, arrays of n_tensors device pointers: grads[i] float
+ *   in/out: momenta[i] float, weights[i] of `dtype`; version[count] int32 (device; NULL: none): one is added to each, as moe_trans
+ *           wants it of parameters that were updated
+ *   out   : copies[i] bfloat16 (MOE_F32 only; copies or a copies[i] NULL: none): the new weights rounded, for a layer that reads bf16
+ * Tensors need no alignment beyond an element's and must not overlap. */
+int moe_muon_step(const moe_muon_t* cfg, const float* const* grads, float* const* momenta, void* const* weights,
+                  uint16_t* const* copies, int32_t* version, void* ws, void* stream);
+
 /* ---- planner (Sections 4.2-4.3 and 5.3 of the paper) ------------------------------------------
  *
  * moe_plan runs the paper's greedy search for a lightweight expert placement (Algorithm 1) on the

@@ -30,6 +30,7 @@ EXPORTS = [
     "moe_plan", "moe_gate_bwd_params", "moe_input_grad", "moe_expert_ffn_bwd_acc", "moe_trans", "moe_recv_layout",
     "moe_dispatch_after_counts", "moe_set_act_saved", "moe_expert_counts_static", "moe_agg", "moe_calib_copy", "moe_calib_mfma",
     "moe_calib_round_bf16", "moe_norm_fwd", "moe_norm_workspace_bytes", "moe_norm_bwd",
+    "moe_muon_workspace_bytes", "moe_muon_step",
 ]
 
 
@@ -55,6 +56,12 @@ class _Planner(ctypes.Structure):
 
 class _Norm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class _Muon(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_tensors", "count", "rows", "cols")] + [("transposed", ctypes.c_int * 8)] + \
+               [(n, ctypes.c_int) for n in ("dtype", "nesterov", "steps")] + \
+               [(n, ctypes.c_float) for n in ("momentum", "eps", "a", "b", "c", "lr", "weight_decay", "scale")]
 
 
 class _PlanOut(ctypes.Structure):
@@ -103,6 +110,8 @@ def load() -> ctypes.CDLL:
         lib.moe_norm_fwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 9
         lib.moe_norm_workspace_bytes.argtypes = [ctypes.POINTER(_Norm), ctypes.POINTER(ctypes.c_size_t)]
         lib.moe_norm_bwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 11
+        lib.moe_muon_workspace_bytes.argtypes = [ctypes.POINTER(_Muon), ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_muon_step.argtypes = [ctypes.POINTER(_Muon)] + [ctypes.POINTER(vp)] * 4 + [vp] * 3
         lib.moe_plan.argtypes = [ctypes.POINTER(_Planner), vp, ctypes.POINTER(_PlanOut), vp]
         _lib = lib
     return _lib
@@ -326,6 +335,44 @@ class Norm:
         rc = self._for_rows(dY)[1](dY, S, gamma, mean, rstd, residual_grad, dX, dgamma, dbeta, self.ws.data_ptr(), _stream())
         if rc != 0:
             _checked(rc, "moe_norm_bwd")
+
+
+class Muon:
+    """The update of a set of expert parameters (moe_muon_step), with its workspace: as many tensors as `transposed` has entries, `count` matrices
+    each, rows x cols or, where transposed, cols x rows."""
+
+    def __init__(self, *, count: int, rows: int, cols: int, dtype: str, transposed=(False,), momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                 coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, device="cuda:0", alloc_workspace: bool = True):
+        self.lib = load()
+        self.n = len(transposed)
+        if not 1 <= self.n <= 8:
+            raise ValueError(f"{self.n} tensors: 1 to 8 are taken")
+        self.numel = count * rows * cols
+        self.elt = TORCH_DTYPE[DTYPES[dtype]]
+        self._cfg = _Muon(self.n, count, rows, cols, (ctypes.c_int * 8)(*(int(bool(t)) for t in transposed)), DTYPES[dtype], int(bool(nesterov)), steps,
+                          momentum, eps, *coefficients, 0.0, 0.0, 1.0)
+        n = ctypes.c_size_t()
+        _checked(self.lib.moe_muon_workspace_bytes(ctypes.byref(self._cfg), ctypes.byref(n)), "moe_muon_workspace_bytes")
+        self.workspace_bytes = n.value
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+
+    def _pointers(self, tensors, dtype, name: str):
+        if len(tensors) != self.n:
+            raise ValueError(f"{name}: {len(tensors)} tensors, expected {self.n}")
+        return (ctypes.c_void_p * self.n)(*(_ptr(t, dtype, self.numel, name) for t in tensors))
+
+    def step(self, grads, momenta, weights, *, lr: float, weight_decay: float = 0.0, scale: float = 1.0, copies=None, version=None):
+        """One update of momenta and weights in place, and of copies and version where they are given."""
+        if self.ws is None:
+            raise ValueError("no workspace attached")
+        cfg = self._cfg
+        cfg.lr, cfg.weight_decay, cfg.scale = lr, weight_decay, scale
+        rc = self.lib.moe_muon_step(
+            ctypes.byref(cfg), self._pointers(grads, torch.float32, "grads"), self._pointers(momenta, torch.float32, "momenta"),
+            self._pointers(weights, self.elt, "weights"), None if copies is None else self._pointers(copies, torch.bfloat16, "copies"),
+            _ptr(version, torch.int32, cfg.count, "version"), self.ws.data_ptr(), _stream())
+        if rc != 0:
+            _checked(rc, "moe_muon_step")
 
 
 class Handle:

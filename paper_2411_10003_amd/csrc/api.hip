@@ -392,6 +392,44 @@ int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const flo
     return hip_status(launch_norm_bwd(*cfg, dY, S, gamma, mean, rstd, dS, dX, dgamma, dbeta, (float*)ws, (hipStream_t)stream));
 }
 
+static int check_muon(const moe_muon_t* c)
+{
+    if (!c) return MOE_ERR_NULL;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    if (c->n_tensors < 1 || c->n_tensors > MUON_MAX_TENSORS || c->count < 1 || (long long)c->count * c->n_tensors > 65535) return MOE_ERR_SHAPE;
+    if (c->rows < 1 || c->cols < 1 || c->rows > 65536 || c->cols > 65536 || (long long)c->rows * c->cols >= (1ll << 30)) return MOE_ERR_SHAPE;
+    for (int i = 0; i < c->n_tensors; ++i)
+        if (c->transposed[i] != 0 && c->transposed[i] != 1) return MOE_ERR_SHAPE;
+    if (c->nesterov != 0 && c->nesterov != 1) return MOE_ERR_SHAPE;
+    if (c->steps < 1 || c->steps > 16) return MOE_ERR_SHAPE;
+    if (!(c->momentum >= 0.0f && c->momentum < 1.0f) || !(c->eps > 0.0f) || !std::isfinite(c->eps)) return MOE_ERR_SHAPE;
+    for (float v : {c->a, c->b, c->c}) if (!(std::fabs(v) <= 16.0f)) return MOE_ERR_SHAPE;
+    for (float v : {c->lr, c->weight_decay, c->scale}) if (!std::isfinite(v)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+int moe_muon_workspace_bytes(const moe_muon_t* cfg, size_t* bytes)
+{
+    const int rc = check_muon(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!bytes) return MOE_ERR_NULL;
+    *bytes = muon_workspace_bytes(*cfg);
+    return MOE_OK;
+}
+
+int moe_muon_step(const moe_muon_t* cfg, const float* const* grads, float* const* momenta, void* const* weights,
+                  uint16_t* const* copies, int32_t* version, void* ws, void* stream)
+{
+    const int rc = check_muon(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!grads || !momenta || !weights) return MOE_ERR_NULL;
+    for (int i = 0; i < cfg->n_tensors; ++i)
+        if (!grads[i] || !momenta[i] || !weights[i]) return MOE_ERR_NULL;
+    if (copies && cfg->dtype != MOE_F32) return MOE_ERR_DTYPE;                 // bf16 weights are their own copy
+    if (!ws || misaligned(ws)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_muon_step(*cfg, grads, momenta, weights, copies, version, ws, (hipStream_t)stream));
+}
+
 int moe_plan(const moe_planner_t* cfg, const int32_t* gating, const moe_plan_out_t* out, void* stream)
 {
     if (!cfg || !gating || !out) return MOE_ERR_NULL;

@@ -125,6 +125,11 @@ hipError_t launch_norm_fwd(const moe_norm_t& c, const void* X, const void* R, co
 hipError_t launch_norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd, const void* dS,
                            void* dX, float* dgamma, float* dbeta, float* partial, hipStream_t st);
 
+constexpr int MUON_MAX_TENSORS = 8;
+size_t muon_workspace_bytes(const moe_muon_t& c);
+hipError_t launch_muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
+                            int32_t* version, void* ws, hipStream_t st);
+
 constexpr int SPLIT_UNITS = 320;       // partial tiles the K-split of a last round may need: at most one per block
 constexpr int UNEVEN_UNITS = 512;      // and an uneven cut: two for each of fewer tiles than there are blocks
 constexpr int SPLIT_COUNTERS = 1024;   // a counter for each of them, in the smaller tiles

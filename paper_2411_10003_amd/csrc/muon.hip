@@ -1,0 +1,693 @@
+// The update of the experts' parameters: momentum, orthogonalised by Newton-Schulz products (the Muon rule), applied to the
+// weights.  Per matrix (short side m, long side n):
+//
+//   M <- mu M + G,  U = G + mu M (nesterov) or M,  X = U / (|U|_F + eps)
+//   steps times, X lying on its long side:  A = X X^T,  X <- a X + (b A + c A A) X
+//   W <- (1 - lr wd) W - lr scale X
+//
+// All matrices of a call, of all its tensors, are one batch: they have the same two sides and lie on the long one here.
+//
+// What X, A and the polynomial are kept in.  The products take 16-bit operands and add in fp32.  fp16, with its 11 bits, at the rate of
+// bf16 with 8; its range is made up for by powers of two: |X|_F <= 1.3 or so is stored times the root mean square of its elements' size
+// (S = 2^floor(log2 sqrt(mn)), at most 2^14), A, whose eigenvalues are at most 1.5, times 2^10, the polynomial, at most 12, times 2^8.
+// What a rounding to 11 bits leaves off the orthogonal factor is 1.5e-3 of it for a dense spectrum and 3.5e-3 for one of a quarter of the
+// rank with a tail (bf16: eight times that), and the factor changes a weight by a few per cent of it: nothing that a bf16 weight resolves.
+// fp32 weights do resolve it: for them every operand is two fp16 numbers, the second the rounding error of the first (22 bits), and a
+// product is three, hi hi + hi lo + lo hi, segments of one contraction (6e-7 and less off the factor).
+#include "tile.h"
+
+#include <cmath>
+#include <type_traits>
+
+namespace {
+
+typedef _Float16 f16;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef float quad_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned oct_t __attribute__((ext_vector_type(4), aligned(2)));        // 8 numbers of 16 bits that begin anywhere
+
+constexpr int MAX_SEGMENTS = 3;
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
+{
+    const f16x2 v = {(f16)lo, (f16)hi};
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ u32x4 pack_f16x8(const float* v)
+{
+    return u32x4{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]), pack_f16x2(v[4], v[5]), pack_f16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void unpack_f16x8(const u32x4& w, float* v)
+{
+    const f16x8 h = __builtin_bit_cast(f16x8, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+}
+// What the first number leaves of the value.
+__device__ __forceinline__ u32x4 pack_rest(const float* v, const u32x4& first)
+{
+    float f[8], r[8];
+    unpack_f16x8(first, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v[i] - f[i];
+    return pack_f16x8(r);
+}
+
+// ---- momentum, and the sum of U^2 in parts ----------------------------------------------------------
+// Bound by HBM: G read, M read and written.  Squares are added in 64 bits: fp32 ones of a gradient of 1e-25 or 1e25 are none.
+struct Tensors {
+    const float* grad[MUON_MAX_TENSORS];
+    float* momentum[MUON_MAX_TENSORS];
+    int transposed[MUON_MAX_TENSORS];                      // lies on its short side
+};
+
+__device__ __forceinline__ float direction(float g, float m, float mu, int nesterov) { return nesterov ? fmaf(mu, m, g) : m; }
+
+constexpr int MOMENTUM_UNROLL = 4;
+__global__ __launch_bounds__(256) void momentum_kernel(const Tensors t, int count, size_t elements, int chunks, float mu, int nesterov,
+                                                       double* __restrict__ partial)
+{
+    const int matrix = blockIdx.y, tensor = matrix / count;
+    const size_t base = (size_t)(matrix % count) * elements;
+    const float* __restrict__ G = t.grad[tensor] + base;
+    float* __restrict__ M = t.momentum[tensor] + base;
+    const size_t quads = elements / 4, step = (size_t)chunks * 256;
+    double sum = 0.0;
+    auto add = [&](float u) { sum = fma((double)u, (double)u, sum); };
+    for (size_t q0 = (size_t)blockIdx.x * 256 + threadIdx.x; q0 < quads; q0 += step * MOMENTUM_UNROLL) {
+        quad_t g[MOMENTUM_UNROLL], m[MOMENTUM_UNROLL];
+#pragma unroll
+        for (int i = 0; i < MOMENTUM_UNROLL; ++i) {
+            const size_t q = q0 + i * step < quads ? q0 + i * step : quads - 1;      // past the end: the last ones again
+            g[i] = *reinterpret_cast<const quad_t*>(G + 4 * q);
+            m[i] = *reinterpret_cast<const quad_t*>(M + 4 * q);
+        }
+#pragma unroll
+        for (int i = 0; i < MOMENTUM_UNROLL; ++i) {
+            const size_t q = q0 + i * step;
+            if (q >= quads) break;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { m[i][k] = fmaf(mu, m[i][k], g[i][k]); add(direction(g[i][k], m[i][k], mu, nesterov)); }
+            *reinterpret_cast<quad_t*>(M + 4 * q) = m[i];
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x < elements % 4) {
+        const size_t i = quads * 4 + threadIdx.x;
+        const float g = G[i], m = fmaf(mu, M[i], g);
+        M[i] = m;
+        add(direction(g, m, mu, nesterov));
+    }
+    __shared__ double words[4];
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) partial[(size_t)matrix * chunks + blockIdx.x] = (words[0] + words[1]) + (words[2] + words[3]);
+}
+
+// ---- the first X, in fp16, on its long side, with zeros up to multiples of 64 ---------------------------
+// U is formed again from G and M: half of what writing and reading it would move.  64 rows x 256 columns of X per block, by way of LDS
+// where the tensor lies on its short side.
+constexpr int START_COLS = 256;
+__global__ __launch_bounds__(256) void start_kernel(const Tensors t, int count, int m, int n, int mp, int np, int chunks, float mu, int nesterov,
+                                                    float eps, float S, const double* __restrict__ partial, f16* __restrict__ X, f16* __restrict__ X_rest)
+{
+    __shared__ double words[4];
+    __shared__ float tile[64][65];
+    const int matrix = blockIdx.z, tensor = matrix / count, lane = threadIdx.x & 63;
+    const size_t base = (size_t)(matrix % count) * ((size_t)m * n);
+    const float* __restrict__ G = t.grad[tensor] + base;
+    const float* __restrict__ M = t.momentum[tensor] + base;
+    double sum = threadIdx.x < chunks ? partial[(size_t)matrix * chunks + threadIdx.x] : 0.0;
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (lane == 0) words[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    const double factor = (double)S / (sqrt((words[0] + words[1]) + (words[2] + words[3])) + (double)eps);
+    const bool tall = t.transposed[tensor] != 0;
+    const int r0 = blockIdx.y * 64, src_cols = tall ? m : n, src_rows = tall ? n : m;
+    for (int c0 = blockIdx.x * START_COLS; c0 < min(np, (int)(blockIdx.x + 1) * START_COLS); c0 += 64) {
+        const int sr0 = tall ? c0 : r0, sc0 = tall ? r0 : c0;
+        __syncthreads();
+#pragma unroll
+        for (int pass = 0; pass < 4; ++pass) {
+            const int r = pass * 16 + threadIdx.x / 16, c = threadIdx.x % 16 * 4;
+            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (sr0 + r < src_rows && sc0 + c < src_cols) {
+                const size_t at = (size_t)(sr0 + r) * src_cols + sc0 + c;
+                const int there = min(4, src_cols - sc0 - c);
+                float gv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, mv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (there == 4) {
+                    const quad_t mq = *reinterpret_cast<const quad_t*>(M + at);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mv[k] = mq[k];
+                    if (nesterov) {
+                        const quad_t gq = *reinterpret_cast<const quad_t*>(G + at);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) gv[k] = gq[k];
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < there) { mv[k] = M[at + k]; gv[k] = nesterov ? G[at + k] : 0.0f; }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) u[k] = (float)((double)direction(gv[k], mv[k], mu, nesterov) * factor);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (tall) tile[c + k][r] = u[k];
+                else tile[r][c + k] = u[k];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+            const int r = pass * 32 + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = tile[r][c + k];
+            const size_t at = ((size_t)matrix * mp + r0 + r) * np + c0 + c;
+            const u32x4 first = pack_f16x8(v);
+            *reinterpret_cast<u32x4*>(X + at) = first;
+            if (X_rest) *reinterpret_cast<u32x4*>(X_rest + at) = pack_rest(v, first);
+        }
+    }
+}
+
+// ---- the products --------------------------------------------------------------------------------------
+// out = alpha sum_k A[i][k] B[k][j] + beta D + diag I, per matrix of the batch, B symmetric or given by its rows as B^T:
+//   ROWS  B is read along its rows' contraction (A B^T: X X^T, and products of symmetric matrices)
+//   COLS  B lies with the contraction as its slow index (the polynomial times X)
+// Sides and contractions are multiples of 64 (of zeros past the matrix), in tiles of 256 or 128 that may hang over.
+enum Operand { ROWS = 0, COLS = 1 };
+enum Output { STORE = 0, UPDATE = 1 };
+
+struct Product {
+    const f16 *A[MAX_SEGMENTS], *B[MAX_SEGMENTS];          // the contraction's segments, one after the other
+    int n_seg, K;                                          // contraction of a segment
+    long a_stride, b_stride, o_stride;                     // numbers from a matrix to the next
+    int lda, ldb, ldo;
+    int M, N;                                              // output
+    int symmetric;                                         // the output is: tiles on and above the diagonal, each stored twice
+    int row_tiles, col_tiles, tiles, items, per_xcd;
+    float alpha, beta, diag;
+    const f16 *D, *D_rest;                                 // addend, laid out like the output; null: none
+    f16 *O, *O_rest;                                       // STORE; O_rest null: 11 bits are kept
+    // UPDATE: the weights, as the caller has them
+    int count, m, n;
+    int transposed[MUON_MAX_TENSORS];
+    void* W[MUON_MAX_TENSORS];
+    uint16_t* copies[MUON_MAX_TENSORS];                    // bf16 copies of fp32 weights, or null
+    float keep, rate;                                      // w <- keep w - rate out
+    int32_t* version;                                      // a counter per matrix of a tensor, or null
+};
+
+// WT: type of the weights (UPDATE).
+template <typename WT> struct WeightOps;
+template <> struct WeightOps<bf16_t> {
+    static __device__ __forceinline__ void load8(const bf16_t* p, float* w)
+    {
+        const oct_t v = *reinterpret_cast<const oct_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[2 * i] = __uint_as_float(v[i] << 16); w[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ void store8(bf16_t* p, const float* w)
+    {
+        *reinterpret_cast<oct_t*>(p) = oct_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
+    }
+    static __device__ __forceinline__ float load(const bf16_t* p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ void store(bf16_t* p, float w) { *p = f32_to_bf16(w); }
+};
+template <> struct WeightOps<float> {
+    static __device__ __forceinline__ void load8(const float* p, float* w)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const quad_t v = *reinterpret_cast<const quad_t*>(p + 4 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
+        }
+    }
+    static __device__ __forceinline__ void store8(float* p, const float* w)
+    {
+        *reinterpret_cast<quad_t*>(p) = quad_t{w[0], w[1], w[2], w[3]};
+        *reinterpret_cast<quad_t*>(p + 4) = quad_t{w[4], w[5], w[6], w[7]};
+    }
+    static __device__ __forceinline__ float load(const float* p) { return *p; }
+    static __device__ __forceinline__ void store(float* p, float w) { *p = w; }
+};
+// Weights at[0 .. there) and their copies.
+template <typename WT> __device__ __forceinline__ void update8(WT* W, uint16_t* copy, size_t at, int there, const float* x, float keep, float rate)
+{
+    typedef WeightOps<WT> Ops;
+    if (there >= 8) {
+        float w[8];
+        Ops::load8(W + at, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fmaf(-rate, x[e], keep * w[e]);
+        Ops::store8(W + at, w);
+        if (copy) WeightOps<bf16_t>::store8(copy + at, w);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < there) {
+            const float w = fmaf(-rate, x[e], keep * Ops::load(W + at + e));
+            Ops::store(W + at + e, w);
+            if (copy) WeightOps<bf16_t>::store(copy + at + e, w);
+        }
+}
+
+// The loop is that of the grouped FFN (ffn_bf16.hip): slices of 32 straight from memory into a ring of LDS buffers, an operand read along its
+// rows in whole 128-byte lines, two slices of half of the tile's rows at a time; in the 256 x 256 tile the two rows of waves
+// alternate between fetching fragments and multiplying.  One tile per block; consecutive items go to one XCD, so that the tiles in flight
+// there share operands of one matrix in its L2.
+template <int KIND, int OUT, typename WT, class GEO>
+__global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void product_kernel(const Product p)
+{
+    constexpr int WGN = GEO::WGN, NWAVES = GEO::NWAVES, WM = GEO::WM, WN = GEO::WN, BM = GEO::BM, BN = GEO::BN, TM = GEO::TM, TN = GEO::TN;
+    constexpr int STAGES = GEO::STAGES, PA = GEO::PA, PB = GEO::PB, FM = 2 * TM, FN = 2 * TN, SLICE_OPS = PA + PB;
+    constexpr uint32_t A_BYTES = GEO::A_BYTES, STAGE_BYTES = GEO::STAGE_BYTES;
+    constexpr bool B_COLS = KIND == COLS;
+
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(unsigned char))smem;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WGN, wn = wave % WGN;
+
+    // ---- which tile
+    const int item = (blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3);
+    if (item >= p.items) return;
+    const int matrix = item / p.tiles, t = item - matrix * p.tiles;
+    int rt, ct;
+    if (p.symmetric) {                                     // columns of the upper triangle, one after the other
+        ct = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while ((ct + 1) * (ct + 2) / 2 <= t) ++ct;
+        while (ct * (ct + 1) / 2 > t) --ct;
+        rt = t - ct * (ct + 1) / 2;
+    } else {                                               // bands of 8 row tiles, column by column
+        const int band = t / (8 * p.col_tiles), in_band = t - band * 8 * p.col_tiles, band_rows = min(8, p.row_tiles - band * 8);
+        rt = band * 8 + in_band % band_rows;
+        ct = in_band / band_rows;
+    }
+    const int m0 = rt * BM, n0 = ct * BN;
+
+    // ---- requests: what lies past the operand's last row reads as zero
+    uint32_t voffA[PA], voffB[PB], ldsA[PA], ldsB[PB];
+    auto line_source = [&](int blk, long ld) {
+        const int row = blk * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
+        return (uint32_t)((row * ld + piece * 8) * 2);
+    };
+#pragma unroll
+    for (int i = 0; i < PA; ++i) { ldsA[i] = (wave + NWAVES * i) * 1024; voffA[i] = line_source(wave + NWAVES * i, p.lda); }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+        ldsB[i] = (wave + NWAVES * i) * 1024;
+        voffB[i] = B_COLS ? kmajor_source<BN>((wave + NWAVES * i) * 64 + lane, p.ldb) : line_source(wave + NWAVES * i, p.ldb);
+    }
+    rsrc_t ra, rb;
+    int seg = 0;
+    auto open_segment = [&]() {
+        const f16* a = p.A[seg] + (size_t)matrix * p.a_stride;
+        const f16* b = p.B[seg] + (size_t)matrix * p.b_stride;
+        ra = make_rsrc(a + (size_t)m0 * p.lda, (long long)(p.M - m0) * p.lda * 2);
+        rb = B_COLS ? make_rsrc(b + n0, ((long long)p.K * p.ldb - n0) * 2) : make_rsrc(b + (size_t)n0 * p.ldb, (long long)(p.N - n0) * p.ldb * 2);
+    };
+    open_segment();
+    const rsrc_t rnull = make_rsrc(p.A[0], 0);
+    const uint32_t stepA = BK * 2, stepB = B_COLS ? (uint32_t)(BK * p.ldb * 2) : BK * 2;
+    const uint32_t halfA = (uint32_t)(BM / 2 * p.lda * 2), halfB = (uint32_t)(BN / 2 * p.ldb * 2);
+    const int k_per_seg = p.K / BK, k_cnt = p.n_seg * k_per_seg;           // an even number, at least two
+    int iss_stage = 0, iss_in_seg = 0;
+    uint32_t soffA = 0, soffB = 0;
+    auto request_piece = [&](int n, uint32_t st, const rsrc_t a, const rsrc_t b, uint32_t oa, uint32_t ob) {
+        if (n < PA) dma16(a, st + ldsA[n], voffA[n], oa);
+        else dma16(b, st + A_BYTES + ldsB[n - PA], voffB[n - PA], ob);
+    };
+    auto group_offsets = [&](auto PAR, uint32_t& oa, uint32_t& ob) {
+        constexpr int par = decltype(PAR)::value;
+        oa = par ? soffA + halfA : soffA;
+        ob = (!B_COLS && par) ? soffB + halfB : soffB;
+    };
+    auto group_done = [&](auto PAR) {
+        constexpr int par = decltype(PAR)::value;
+        iss_stage = iss_stage + 1 == STAGES ? 0 : iss_stage + 1;
+        ++iss_in_seg;
+        if (par) soffA += 2 * stepA;
+        if (B_COLS || par) soffB += B_COLS ? stepB : 2 * stepB;
+    };
+    auto issue_group = [&](auto PAR, const rsrc_t a, const rsrc_t b) {
+        const uint32_t st = lds0 + (uint32_t)iss_stage * STAGE_BYTES;
+        uint32_t oa, ob;
+        group_offsets(PAR, oa, ob);
+#pragma unroll
+        for (int n = 0; n < SLICE_OPS; ++n) request_piece(n, st, a, b, oa, ob);
+        group_done(PAR);
+    };
+    auto group_fixups = [&]() {                            // after an odd group: the next segment, if there is one
+        if (iss_in_seg != k_per_seg) return;
+        iss_in_seg = 0; soffA = 0; soffB = 0;
+        if (++seg < p.n_seg) open_segment();
+    };
+
+    // ---- fragment addresses inside a ring buffer
+    uint32_t fk_addr[4], fpa[2], fpb[2];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) fk_addr[c] = kmajor_off<BN>(8 * (lane >> 4) + ((lane & 15) >> 2), c * 16 + 4 * (lane & 3));
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        fpa[v] = halfpair_off(lane & 15, lane >> 4) ^ (uint32_t)(v << 6);
+        fpb[v] = A_BYTES + (halfpair_off((wn % (WGN / 2)) * WN + (lane & 15), lane >> 4) ^ (uint32_t)(v << 6));
+    }
+    f32x4 acc[FM][FN];
+    f16x8 fa[FM], fb[FN];
+    auto goes_out = [](int n) { return (n + 1) % ((FM + FN) / SLICE_OPS) == 0 ? (n + 1) / ((FM + FN) / SLICE_OPS) - 1 : -1; };
+    auto load_frags = [&](uint32_t stA, uint32_t stB, auto PAR, auto after) {
+        constexpr int par = decltype(PAR)::value;
+        const uint32_t a = stA + fpa[par];
+        auto frag_a = [&](auto I) { lds_frag_kcontig_at<decltype(I)::value * 2048>(fa[decltype(I)::value], a); after(decltype(I)::value); };
+        frag_a(std::integral_constant<int, 0>{}); frag_a(std::integral_constant<int, 1>{});
+        frag_a(std::integral_constant<int, 2>{}); frag_a(std::integral_constant<int, 3>{});
+        if constexpr (FM == 8) {
+            frag_a(std::integral_constant<int, 4>{}); frag_a(std::integral_constant<int, 5>{});
+            frag_a(std::integral_constant<int, 6>{}); frag_a(std::integral_constant<int, 7>{});
+        }
+        if constexpr (B_COLS) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) { lds_frag_kmajor_at<BN * 8, 0>(fb[j], stB + A_BYTES + wn * 256 + fk_addr[j]); after(FM + j); }
+        } else {
+            const uint32_t b = stB + fpb[par];
+            auto frag_b = [&](auto J) { lds_frag_kcontig_at<decltype(J)::value * 2048>(fb[decltype(J)::value], b); after(FM + decltype(J)::value); };
+            frag_b(std::integral_constant<int, 0>{}); frag_b(std::integral_constant<int, 1>{});
+            frag_b(std::integral_constant<int, 2>{}); frag_b(std::integral_constant<int, 3>{});
+        }
+    };
+    auto mma_first = [&]() {                               // the first products take zero as their addend
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int jj = 0; jj < FN; ++jj) {
+                const int j = (i & 1) ? FN - 1 - jj : jj;
+                asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(fb[j]), "v"(fa[i]));
+            }
+    };
+    auto mma = [&]() {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int jj = 0; jj < FN; ++jj) {
+                const int j = (i & 1) ? FN - 1 - jj : jj;
+                asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(fb[j]), "v"(fa[i]));
+            }
+    };
+
+    // ---- main loop: slice t reads the groups of its pair and requests group t + 3
+    constexpr int L = 3;
+    typedef std::integral_constant<int, 0> even_t;
+    typedef std::integral_constant<int, 1> odd_t;
+    issue_group(even_t{}, ra, rb);
+    issue_group(odd_t{}, ra, rb);
+    group_fixups();
+    if (k_cnt > 2) issue_group(even_t{}, ra, rb); else issue_group(even_t{}, rnull, rnull);
+    WAIT_VMCNT(SLICE_OPS);                                 // groups 0 and 1 have landed: slices 0 and 1
+    BLOCK_BARRIER();
+    if (GEO::TWO_PHASE && wm == 1) BLOCK_BARRIER();
+    int cur = 0, pair0 = 0;                                // ring slots of the slice's own group, of the even group of its pair
+    const int hA = wm, hB = wn / (WGN / 2);                // which group of a pair holds this wave's rows of A and of B
+    auto slot_base = [&](int slot) { return lds0 + (uint32_t)(slot >= STAGES ? slot - STAGES : slot) * STAGE_BYTES; };
+    auto slice = [&](auto PAR, auto FIRST, const rsrc_t a, const rsrc_t b) {
+        constexpr int par = decltype(PAR)::value;
+        typedef std::integral_constant<int, 1 - par> other_t;
+        const uint32_t stA = slot_base(pair0 + hA), stB = B_COLS ? slot_base(cur) : slot_base(pair0 + hB);
+        const uint32_t to = lds0 + (uint32_t)iss_stage * STAGE_BYTES;
+        uint32_t oa, ob;
+        group_offsets(other_t{}, oa, ob);
+        load_frags(stA, stB, PAR, [&](int n) { if (goes_out(n) >= 0) { __builtin_amdgcn_sched_barrier(0); request_piece(goes_out(n), to, a, b, oa, ob); __builtin_amdgcn_sched_barrier(0); } });
+        group_done(other_t{});
+        WAIT_VMCNT(par ? SLICE_OPS : 2 * SLICE_OPS);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);                 // no product moves above the wait
+        BLOCK_BARRIER();
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (decltype(FIRST)::value) mma_first(); else mma();
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (GEO::TWO_PHASE) BLOCK_BARRIER();
+        cur = (cur + 1 == STAGES) ? 0 : cur + 1;
+        if (par) pair0 = (pair0 + 2 >= STAGES) ? pair0 + 2 - STAGES : pair0 + 2;
+    };
+    if (k_cnt > 2) { slice(even_t{}, std::true_type{}, ra, rb); group_fixups(); }
+    else slice(even_t{}, std::true_type{}, rnull, rnull);
+    int s = 1;
+    while (s < k_cnt - 1) {
+        const bool more = s + L < k_cnt;                   // the pair of slices s + 3, s + 4 exists
+        const int n = more ? min((k_cnt - L - s + 1) / 2, (k_per_seg - iss_in_seg) / 2) : (k_cnt - 1 - s) / 2;
+        const rsrc_t a = more ? ra : rnull, b = more ? rb : rnull;
+        for (int i = 0; i < n; ++i) {
+            slice(odd_t{}, std::false_type{}, a, b);
+            slice(even_t{}, std::false_type{}, a, b);
+        }
+        s += 2 * n;
+        if (more) group_fixups();
+    }
+    slice(odd_t{}, std::false_type{}, rnull, rnull);       // the last one
+    WAIT_VMCNT(0);                                         // the empty requests too: the epilogue reuses the ring
+    if (GEO::TWO_PHASE && wm == 0) BLOCK_BARRIER();        // both rows have passed the same number of barriers
+    BLOCK_BARRIER();
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");     // the last products have written back before they are read
+
+    // ---- epilogue: 64 x 64 results at a time through a patch of LDS of the wave's own, so that memory sees whole lines along the rows
+    // and, where the result is wanted the other way round too, along the columns.
+    constexpr int PITCH = WN * 4 + 16, PATCH = 64 * PITCH;
+    static_assert(WN == 64 && WM % 64 == 0 && NWAVES * PATCH <= (int)GEO::LDS_BYTES, "patches inside the ring");
+    unsigned char* patch = smem + wave * PATCH;
+    const int lrow = lane & 15, lcol = (lane >> 4) * 4;
+    const int col0 = n0 + wn * WN;
+    const int tensor = OUT == UPDATE ? matrix / p.count : 0;
+    const bool tall = OUT == UPDATE && p.transposed[tensor] != 0;
+    WT* W = nullptr;
+    uint16_t* copy = nullptr;
+    if constexpr (OUT == UPDATE) {
+        const size_t base = (size_t)(matrix % p.count) * ((size_t)p.m * p.n);
+        W = (WT*)p.W[tensor] + base;
+        copy = p.copies[tensor] ? p.copies[tensor] + base : nullptr;
+        if (p.version && item == matrix * p.tiles && tensor == 0 && tid == 0) p.version[matrix] += 1;
+    }
+#pragma unroll
+    for (int part = 0; part < WM / 64; ++part) {
+        const int row0 = m0 + wm * WM + part * 64;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const f32x4& v = acc[part * 4 + i][j];
+                *reinterpret_cast<float4*>(patch + (i * 16 + lrow) * PITCH + (j * 16 + lcol) * 4) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        if (row0 >= p.M || col0 >= p.N) continue;          // sides are multiples of 64: all of it or none
+        const bool mirror = OUT == UPDATE ? tall : (p.symmetric && rt != ct);
+#pragma unroll
+        for (int pass = 0; pass < 8; ++pass) {
+            const int r = pass * 8 + (lane >> 3), c = (lane & 7) * 8;
+            float* at = reinterpret_cast<float*>(patch + r * PITCH + c * 4);
+            float v[8];
+            *reinterpret_cast<float4*>(v) = *reinterpret_cast<float4*>(at);
+            *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<float4*>(at + 4);
+            const size_t o = (size_t)matrix * p.o_stride + (size_t)(row0 + r) * p.ldo + col0 + c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
+            if (p.D) {
+                float d[8];
+                unpack_f16x8(*reinterpret_cast<const u32x4*>(p.D + o), d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, d[e], v[e]);
+                if (p.D_rest) {
+                    unpack_f16x8(*reinterpret_cast<const u32x4*>(p.D_rest + o), d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, d[e], v[e]);
+                }
+            }
+            if constexpr (OUT == STORE) {
+                if (p.symmetric && rt == ct)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += row0 + r == col0 + c + e ? p.diag : 0.0f;
+                const u32x4 first = pack_f16x8(v);
+                *reinterpret_cast<u32x4*>(p.O + o) = first;
+                if (p.O_rest) *reinterpret_cast<u32x4*>(p.O_rest + o) = pack_rest(v, first);
+            } else if (!tall) {
+                if (row0 + r < p.m && col0 + c < p.n) update8(W, copy, (size_t)(row0 + r) * p.n + col0 + c, p.n - col0 - c, v, p.keep, p.rate);
+            }
+            if (mirror) {
+                *reinterpret_cast<float4*>(at) = *reinterpret_cast<float4*>(v);
+                *reinterpret_cast<float4*>(at + 4) = *reinterpret_cast<float4*>(v + 4);
+            }
+        }
+        if (!mirror) continue;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int pass = 0; pass < 8; ++pass) {
+            const int c = pass * 8 + (lane >> 3), r = (lane & 7) * 8;      // column of the tile, its rows r .. r + 7
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<float*>(patch + (r + e) * PITCH + c * 4);
+            if constexpr (OUT == STORE) {
+                const size_t o = (size_t)matrix * p.o_stride + (size_t)(col0 + c) * p.ldo + row0 + r;
+                const u32x4 first = pack_f16x8(v);
+                *reinterpret_cast<u32x4*>(p.O + o) = first;
+                if (p.O_rest) *reinterpret_cast<u32x4*>(p.O_rest + o) = pack_rest(v, first);
+            } else {
+                if (col0 + c < p.n && row0 + r < p.m) update8(W, copy, (size_t)(col0 + c) * p.m + row0 + r, p.m - row0 - r, v, p.keep, p.rate);
+            }
+        }
+    }
+}
+
+template <int KIND, int OUT, typename WT, class GEO>
+hipError_t launch_tiles(Product p, int matrices, hipStream_t st)
+{
+    p.row_tiles = (p.M + GEO::BM - 1) / GEO::BM;
+    p.col_tiles = (p.N + GEO::BN - 1) / GEO::BN;
+    p.tiles = p.symmetric ? p.row_tiles * (p.row_tiles + 1) / 2 : p.row_tiles * p.col_tiles;
+    p.items = p.tiles * matrices;
+    p.per_xcd = (p.items + 7) / 8;
+    static PerDeviceOnce once;
+    const int dev = current_device();
+    auto kern = product_kernel<KIND, OUT, WT, GEO>;
+    if (!once.is_done(dev)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)GEO::LDS_BYTES);
+        if (e != hipSuccess) return e;
+        once.mark(dev);
+    }
+    hipLaunchKernelGGL(kern, dim3(8 * p.per_xcd), dim3(GEO::THREADS), GEO::LDS_BYTES, st, p);
+    return hipGetLastError();
+}
+
+// 256 x 256 tiles where they fill the chip.
+template <int KIND, int OUT, typename WT> hipError_t launch_product(const Product& p, int matrices, hipStream_t st)
+{
+    const long rt = (p.M + Large::BM - 1) / Large::BM, ct = (p.N + Large::BN - 1) / Large::BN;
+    const long tiles = (p.symmetric ? rt * (rt + 1) / 2 : rt * ct) * matrices;
+    return tiles >= 256 ? launch_tiles<KIND, OUT, WT, Large>(p, matrices, st) : launch_tiles<KIND, OUT, WT, Small>(p, matrices, st);
+}
+
+inline int round_up64(int x) { return (x + 63) / 64 * 64; }
+inline size_t align_ws(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int MAX_CHUNKS = 256;                            // parts of a matrix' sum of squares: one per thread of the block that adds them
+struct MuonPlan {
+    int matrices, m, n, mp, np, planes, chunks;
+    size_t x_numbers, a_numbers;                           // of all matrices
+    size_t off_partial, off_x[2], off_a[2], bytes;         // a second plane, where there is one, follows the first
+};
+MuonPlan plan_of(const moe_muon_t& c)
+{
+    MuonPlan p{};
+    p.matrices = c.n_tensors * c.count;
+    p.m = c.rows < c.cols ? c.rows : c.cols;
+    p.n = c.rows < c.cols ? c.cols : c.rows;
+    p.mp = round_up64(p.m);
+    p.np = round_up64(p.n);
+    p.planes = c.dtype == MOE_F32 ? 2 : 1;
+    const size_t chunks = ((size_t)p.m * p.n + 8191) / 8192;
+    p.chunks = (int)(chunks < MAX_CHUNKS ? chunks : MAX_CHUNKS);
+    p.x_numbers = (size_t)p.matrices * p.mp * p.np;
+    p.a_numbers = (size_t)p.matrices * p.mp * p.mp;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += align_ws(bytes); return at; };
+    p.off_partial = take((size_t)p.matrices * p.chunks * sizeof(double));
+    for (size_t& x : p.off_x) x = take(p.x_numbers * sizeof(f16) * p.planes);
+    for (size_t& a : p.off_a) a = take(p.a_numbers * sizeof(f16) * p.planes);
+    p.bytes = off;
+    return p;
+}
+
+// A batch of matrices in the workspace: its numbers and, with two planes, what they leave off.
+struct Stored { f16 *first, *rest; };
+
+template <typename WT>
+hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
+                     int32_t* version, void* ws, hipStream_t st)
+{
+    const MuonPlan P = plan_of(c);
+    char* base = (char*)ws;
+    double* partial = (double*)(base + P.off_partial);
+    auto stored = [&](size_t off, size_t numbers) { f16* f = (f16*)(base + off); return Stored{f, P.planes == 2 ? f + numbers : nullptr}; };
+    Stored X = stored(P.off_x[0], P.x_numbers), X2 = stored(P.off_x[1], P.x_numbers);
+    const Stored A = stored(P.off_a[0], P.a_numbers), B = stored(P.off_a[1], P.a_numbers);
+    const float S = exp2f(fminf(14.0f, floorf(log2f(sqrtf((float)P.m * (float)P.n))))), SA = 1024.0f, SB = 256.0f;
+
+    Tensors t{};
+    for (int i = 0; i < c.n_tensors; ++i) {
+        t.grad[i] = grads[i];
+        t.momentum[i] = momenta[i];
+        t.transposed[i] = (c.rows <= c.cols) == (c.transposed[i] != 0) && c.rows != c.cols ? 1 : 0;
+    }
+    hipLaunchKernelGGL(momentum_kernel, dim3(P.chunks, P.matrices), dim3(256), 0, st, t, c.count, (size_t)P.m * P.n, P.chunks, c.momentum, c.nesterov, partial);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(start_kernel, dim3((P.np + START_COLS - 1) / START_COLS, P.mp / 64, P.matrices), dim3(256), 0, st, t, c.count, P.m, P.n, P.mp, P.np,
+                       P.chunks, c.momentum, c.nesterov, c.eps, S, partial, X.first, X.rest);
+    e = hipGetLastError();
+
+    const long xs = (long)P.mp * P.np, as = (long)P.mp * P.mp;
+    auto operands = [&](Product& p, const Stored& a, long a_stride, int lda, const Stored& b, long b_stride, int ldb, int K) {
+        p.n_seg = 1;
+        p.A[0] = a.first; p.B[0] = b.first;
+        if (a.rest) {
+            p.n_seg = 3;
+            p.A[1] = a.first; p.B[1] = b.rest;
+            p.A[2] = a.rest; p.B[2] = b.first;
+        }
+        p.a_stride = a_stride; p.lda = lda;
+        p.b_stride = b_stride; p.ldb = ldb;
+        p.K = K;
+    };
+    for (int step = 0; step < c.steps && e == hipSuccess; ++step) {
+        const bool last = step + 1 == c.steps;
+        Product p{};
+        operands(p, X, xs, P.np, X, xs, P.np, P.np);       // A = X X^T
+        p.M = p.N = p.ldo = P.mp; p.o_stride = as; p.symmetric = 1;
+        p.alpha = SA / (S * S); p.O = A.first; p.O_rest = A.rest;
+        e = launch_product<ROWS, STORE, float>(p, P.matrices, st);
+        if (e != hipSuccess) break;
+        operands(p, A, as, P.mp, A, as, P.mp, P.mp);       // B = b A + c A A
+        p.alpha = c.c * SB / (SA * SA); p.beta = c.b * SB / SA; p.D = A.first; p.D_rest = A.rest;
+        p.O = B.first; p.O_rest = B.rest;
+        e = launch_product<ROWS, STORE, float>(p, P.matrices, st);
+        if (e != hipSuccess) break;
+        Product q{};                                       // X = a X + B X
+        operands(q, B, as, P.mp, X, xs, P.np, P.mp);
+        q.M = P.mp; q.N = q.ldo = P.np; q.o_stride = xs;
+        q.alpha = 1.0f / SB; q.beta = c.a; q.D = X.first; q.D_rest = X.rest;
+        if (!last) {
+            q.O = X2.first; q.O_rest = X2.rest;
+            e = launch_product<COLS, STORE, float>(q, P.matrices, st);
+            const Stored x = X; X = X2; X2 = x;
+        } else {
+            q.count = c.count; q.m = P.m; q.n = P.n;
+            for (int i = 0; i < c.n_tensors; ++i) { q.transposed[i] = t.transposed[i]; q.W[i] = weights[i]; q.copies[i] = copies ? copies[i] : nullptr; }
+            q.keep = (float)(1.0 - (double)c.lr * c.weight_decay);
+            q.rate = (float)((double)c.lr * c.scale / S);
+            q.version = version;
+            e = launch_product<COLS, UPDATE, WT>(q, P.matrices, st);
+        }
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t muon_workspace_bytes(const moe_muon_t& c) { return plan_of(c).bytes; }
+
+hipError_t launch_muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
+                            int32_t* version, void* ws, hipStream_t st)
+{
+    return c.dtype == MOE_F32 ? muon_step<float>(c, grads, momenta, weights, copies, version, ws, st)
+                              : muon_step<bf16_t>(c, grads, momenta, weights, copies, version, ws, st);
+}
