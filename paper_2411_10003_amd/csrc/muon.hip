@@ -7,13 +7,21 @@
 //
 // All matrices of a call, of all its tensors, are one batch: they have the same two sides and lie on the long one here.
 //
+// Every X is Q X0 with Q a polynomial in A0 = X0 X0^T, so the steps can be taken on the short side: B = a + b A + c A A,  Q <- B Q,
+// A <- B A B (all of them polynomials in A0: they commute and are symmetric, half of each product is the other half), and X = Q X0 at
+// the end.  Five steps: 6 m^2 n + 14 m^3 multiply-adds where the form above takes 15 m^2 n + 5 m^3; as many at n = m, 0.58 of it at n = 4 m.  A
+// carries the squares of the singular values, and what a rounding adds to those near zero grows by a^2 = 11.9 a step that goes on
+// with the same A: after three steps (each, where the short side is 64 or less) A is formed again from X.  Off the factor that 64 bits give, 11 bits kept, 256 x 1024 of a falling spectrum:
+// the form above 3.4e-3; all five steps on one A 1.2e-1; two, then three 1.5e-2; three, then two 3.5e-3.
+//
 // What X, A and the polynomial are kept in.  The products take 16-bit operands and add in fp32.  fp16, with its 11 bits, at the rate of
 // bf16 with 8; its range is made up for by powers of two: |X|_F <= 1.3 or so is stored times the root mean square of its elements' size
-// (S = 2^floor(log2 sqrt(mn)), at most 2^14), A, whose eigenvalues are at most 1.5, times 2^10, the polynomial, at most 12, times 2^8.
+// (S = 2^floor(log2 sqrt(mn)), at most 2^14), A, whose eigenvalues are at most 1.5, times 2^10, B, at most a, times 2^6,
+// Q, at most a^3, times 2^3.
 // What a rounding to 11 bits leaves off the orthogonal factor is 1.5e-3 of it for a dense spectrum and 3.5e-3 for one of a quarter of the
 // rank with a tail (bf16: eight times that), and the factor changes a weight by a few per cent of it: nothing that a bf16 weight resolves.
 // fp32 weights do resolve it: for them every operand is two fp16 numbers, the second the rounding error of the first (22 bits), and a
-// product is three, hi hi + hi lo + lo hi, segments of one contraction (6e-7 and less off the factor).
+// product is three, hi lo + lo hi + hi hi, segments of one contraction (2e-6 to 4e-6 off the factor, as fp32 throughout is).
 #include "tile.h"
 
 #include <cmath>
@@ -576,6 +584,12 @@ template <int KIND, int OUT, typename WT> hipError_t launch_product(const Produc
     return tiles >= 256 ? launch_tiles<KIND, OUT, WT, Large>(p, matrices, st) : launch_tiles<KIND, OUT, WT, Small>(p, matrices, st);
 }
 
+// Steps that are taken on one Gram matrix, see the head of this file.  What a rounding of A amounts to in one direction grows with the share of A
+// that one element is, and where the short side is one tile a step costs its launches, of which the form above has fewer (15 for five
+// steps, 18).  Off the factor with one | three steps, 11 bits, 8 x 8 3.9e-3 | 3.9e-2, 64 x 64 4.4e-3 | 5.2e-3, 1024 x 1024 4.0e-3 | 4.7e-3;
+// 22 bits 1.1e-6 | 1.6e-5, 1.7e-6 | 2.4e-6, 3.3e-6 | 3.7e-6 (fp32 throughout: 0.8e-6, 1.5e-6, 3.6e-6).
+inline int steps_per_gram(int m) { return m <= 64 ? 1 : 3; }
+
 inline int round_up64(int x) { return (x + 63) / 64 * 64; }
 inline size_t align_ws(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -583,7 +597,7 @@ constexpr int MAX_CHUNKS = 256;                            // parts of a matrix'
 struct MuonPlan {
     int matrices, m, n, mp, np, planes, chunks;
     size_t x_numbers, a_numbers;                           // of all matrices
-    size_t off_partial, off_x[2], off_a[2], bytes;         // a second plane, where there is one, follows the first
+    size_t off_partial, off_x[2], off_a[4], bytes;         // a second plane, where there is one, follows the first
 };
 MuonPlan plan_of(const moe_muon_t& c)
 {
@@ -619,8 +633,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
     double* partial = (double*)(base + P.off_partial);
     auto stored = [&](size_t off, size_t numbers) { f16* f = (f16*)(base + off); return Stored{f, P.planes == 2 ? f + numbers : nullptr}; };
     Stored X = stored(P.off_x[0], P.x_numbers), X2 = stored(P.off_x[1], P.x_numbers);
-    const Stored A = stored(P.off_a[0], P.a_numbers), B = stored(P.off_a[1], P.a_numbers);
-    const float S = exp2f(fminf(14.0f, floorf(log2f(sqrtf((float)P.m * (float)P.n))))), SA = 1024.0f, SB = 256.0f;
+    const float S = exp2f(fminf(14.0f, floorf(log2f(sqrtf((float)P.m * (float)P.n))))), SA = 1024.0f, SB = 64.0f, SQ = 8.0f;
 
     Tensors t{};
     for (int i = 0; i < c.n_tensors; ++i) {
@@ -637,35 +650,51 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
 
     const long xs = (long)P.mp * P.np, as = (long)P.mp * P.mp;
     auto operands = [&](Product& p, const Stored& a, long a_stride, int lda, const Stored& b, long b_stride, int ldb, int K) {
-        p.n_seg = 1;
-        p.A[0] = a.first; p.B[0] = b.first;
+        p.n_seg = a.rest ? 3 : 1;                          // the small ones first: the sum is rounded at its size in the last segment only
+        p.A[p.n_seg - 1] = a.first; p.B[p.n_seg - 1] = b.first;
         if (a.rest) {
-            p.n_seg = 3;
-            p.A[1] = a.first; p.B[1] = b.rest;
-            p.A[2] = a.rest; p.B[2] = b.first;
+            p.A[0] = a.first; p.B[0] = b.rest;
+            p.A[1] = a.rest; p.B[1] = b.first;
         }
         p.a_stride = a_stride; p.lda = lda;
         p.b_stride = b_stride; p.ldb = ldb;
         p.K = K;
     };
-    for (int step = 0; step < c.steps && e == hipSuccess; ++step) {
-        const bool last = step + 1 == c.steps;
+    // out = alpha A B + beta add + diag I, a symmetric matrix of the short side
+    auto square = [&](const Stored& out, const Stored& a, const Stored& b, long stride, int ld, float alpha, const Stored* add, float beta, float diag) {
+        if (e != hipSuccess) return;
         Product p{};
-        operands(p, X, xs, P.np, X, xs, P.np, P.np);       // A = X X^T
+        operands(p, a, stride, ld, b, stride, ld, ld);
         p.M = p.N = p.ldo = P.mp; p.o_stride = as; p.symmetric = 1;
-        p.alpha = SA / (S * S); p.O = A.first; p.O_rest = A.rest;
+        p.alpha = alpha; p.beta = beta; p.diag = diag;
+        if (add) { p.D = add->first; p.D_rest = add->rest; }
+        p.O = out.first; p.O_rest = out.rest;
         e = launch_product<ROWS, STORE, float>(p, P.matrices, st);
+    };
+    const Stored A = stored(P.off_a[0], P.a_numbers);
+    for (int left = c.steps, of = 0; left > 0 && e == hipSuccess; left -= of) {
+        of = left < steps_per_gram(P.m) ? left : steps_per_gram(P.m);
+        Stored B = stored(P.off_a[1], P.a_numbers), Q = B, free0 = stored(P.off_a[2], P.a_numbers), free1 = stored(P.off_a[3], P.a_numbers);
+        float q_scale = SB;
+        square(A, X, X, xs, P.np, SA / (S * S), nullptr, 0.0f, 0.0f);
+        square(B, A, A, as, P.mp, c.c * SB / (SA * SA), &A, c.b * SB / SA, c.a * SB);          // B = a + b A + c A A
+        for (int step = 1; step < of; ++step) {
+            square(free0, B, A, as, P.mp, 1.0f / SB, nullptr, 0.0f, 0.0f);                     // A <- B A B
+            square(A, free0, B, as, P.mp, 1.0f / SB, nullptr, 0.0f, 0.0f);
+            const Stored last_B = B, last_Q = Q;
+            B = free0;
+            square(B, A, A, as, P.mp, c.c * SB / (SA * SA), &A, c.b * SB / SA, c.a * SB);
+            Q = step == 1 ? free1 : last_B;                // the first Q is B itself: there is one buffer more to spare then
+            square(Q, B, last_Q, as, P.mp, SQ / (SB * q_scale), nullptr, 0.0f, 0.0f);          // Q <- B Q
+            q_scale = SQ;
+            free0 = last_Q;
+        }
         if (e != hipSuccess) break;
-        operands(p, A, as, P.mp, A, as, P.mp, P.mp);       // B = b A + c A A
-        p.alpha = c.c * SB / (SA * SA); p.beta = c.b * SB / SA; p.D = A.first; p.D_rest = A.rest;
-        p.O = B.first; p.O_rest = B.rest;
-        e = launch_product<ROWS, STORE, float>(p, P.matrices, st);
-        if (e != hipSuccess) break;
-        Product q{};                                       // X = a X + B X
-        operands(q, B, as, P.mp, X, xs, P.np, P.mp);
+        Product q{};                                       // X <- Q X
+        operands(q, Q, as, P.mp, X, xs, P.np, P.mp);
         q.M = P.mp; q.N = q.ldo = P.np; q.o_stride = xs;
-        q.alpha = 1.0f / SB; q.beta = c.a; q.D = X.first; q.D_rest = X.rest;
-        if (!last) {
+        q.alpha = 1.0f / q_scale;
+        if (of < left) {
             q.O = X2.first; q.O_rest = X2.rest;
             e = launch_product<COLS, STORE, float>(q, P.matrices, st);
             const Stored x = X; X = X2; X2 = x;
