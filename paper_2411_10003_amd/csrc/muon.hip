@@ -36,6 +36,7 @@ typedef float quad_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned oct_t __attribute__((ext_vector_type(4), aligned(2)));        // 8 numbers of 16 bits that begin anywhere
 
 constexpr int MAX_SEGMENTS = 3;
+constexpr int MAX_CUT = 512;                               // tiles of a launch that are cut: fewer than there are places for blocks
 
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
@@ -74,8 +75,11 @@ __device__ __forceinline__ float direction(float g, float m, float mu, int neste
 
 constexpr int MOMENTUM_UNROLL = 4;
 __global__ __launch_bounds__(256) void momentum_kernel(const Tensors t, int count, size_t elements, int chunks, float mu, int nesterov,
-                                                       double* __restrict__ partial)
+                                                       double* __restrict__ partial, int* __restrict__ arrived)
 {
+    // the counters of the products' cut tiles, whatever the workspace held; from here on every use leaves them zero
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < MAX_CUT; i += 256) arrived[i] = 0;
     const int matrix = blockIdx.y, tensor = matrix / count;
     const size_t base = (size_t)(matrix % count) * elements;
     const float* __restrict__ G = t.grad[tensor] + base;
@@ -197,7 +201,11 @@ struct Product {
     int lda, ldb, ldo;
     int M, N;                                              // output
     int symmetric;                                         // the output is: tiles on and above the diagonal, each stored twice
-    int row_tiles, col_tiles, tiles, items, per_xcd;
+    int row_tiles, col_tiles, tiles;                       // of a matrix
+    // Tiles [0, whole) are computed by a block each; the `cut` tiles after them by `parts` blocks, one after the other along the contraction
+    int whole, whole_per_xcd, cut, parts, part_per_xcd;
+    float* part_ws;                                        // what a part leaves: [cut tile][part][wave][fragment][lane] as float4
+    int* arrived;                                          // parts of a cut tile that have been stored; all zero between two launches
     float alpha, beta, diag;
     const f16 *D, *D_rest;                                 // addend, laid out like the output; null: none
     f16 *O, *O_rest;                                       // STORE; O_rest null: 11 bits are kept
@@ -284,9 +292,20 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WGN, wn = wave % WGN;
 
-    // ---- which tile
-    const int item = (blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3);
-    if (item >= p.items) return;
+    // ---- which tile, and which part of it
+    const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
+    int item = xcd * p.whole_per_xcd + turn, part = 0, unit = 0;
+    const bool cut = turn >= p.whole_per_xcd;
+    if (cut) {
+        const int i = xcd * p.part_per_xcd + turn - p.whole_per_xcd;
+        if (i >= p.cut * p.parts) return;
+        part = i / p.cut;                                  // neighbours work on the same stretch of the contraction
+        unit = i - part * p.cut;
+        item = p.whole + unit;
+    } else if (item >= p.whole) {
+        return;
+    }
+    const int parts = cut ? p.parts : 1;
     const int matrix = item / p.tiles, t = item - matrix * p.tiles;
     int rt, ct;
     if (p.symmetric) {                                     // columns of the upper triangle, one after the other
@@ -314,8 +333,11 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         ldsB[i] = (wave + NWAVES * i) * 1024;
         voffB[i] = B_COLS ? kmajor_source<BN>((wave + NWAVES * i) * 64 + lane, p.ldb) : line_source(wave + NWAVES * i, p.ldb);
     }
+    const int k_per_seg = p.K / BK;
+    auto part_begin = [&](int i) { return (int)((long)i * (p.n_seg * k_per_seg) / parts) & ~1; };     // parts begin at even slices
+    const int k_lo = part_begin(part), k_cnt = (part + 1 == parts ? p.n_seg * k_per_seg : part_begin(part + 1)) - k_lo;    // an even number, at least two
     rsrc_t ra, rb;
-    int seg = 0;
+    int seg = k_lo / k_per_seg;
     auto open_segment = [&]() {
         const f16* a = p.A[seg] + (size_t)matrix * p.a_stride;
         const f16* b = p.B[seg] + (size_t)matrix * p.b_stride;
@@ -326,9 +348,8 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     const rsrc_t rnull = make_rsrc(p.A[0], 0);
     const uint32_t stepA = BK * 2, stepB = B_COLS ? (uint32_t)(BK * p.ldb * 2) : BK * 2;
     const uint32_t halfA = (uint32_t)(BM / 2 * p.lda * 2), halfB = (uint32_t)(BN / 2 * p.ldb * 2);
-    const int k_per_seg = p.K / BK, k_cnt = p.n_seg * k_per_seg;           // an even number, at least two
-    int iss_stage = 0, iss_in_seg = 0;
-    uint32_t soffA = 0, soffB = 0;
+    int iss_stage = 0, iss_in_seg = k_lo - seg * k_per_seg;
+    uint32_t soffA = (uint32_t)iss_in_seg * stepA, soffB = (uint32_t)iss_in_seg * stepB;
     auto request_piece = [&](int n, uint32_t st, const rsrc_t a, const rsrc_t b, uint32_t oa, uint32_t ob) {
         if (n < PA) dma16(a, st + ldsA[n], voffA[n], oa);
         else dma16(b, st + A_BYTES + ldsB[n - PA], voffB[n - PA], ob);
@@ -466,6 +487,41 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     BLOCK_BARRIER();
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");     // the last products have written back before they are read
 
+    // ---- a part of a tile.  All of its parts but the last to be done leave their sums in the workspace; the last adds them, itself among them, in
+    // the order of the contraction (the same bits whichever part is last) and goes on with the tile.  Nobody waits for another block.
+    // The sums and the count go past the L2 of the XCD (sc1), of which every XCD has its own.
+    constexpr int AT_DEVICE = 16, UNIT_FLOATS = GEO::BM * GEO::BN;
+    static_assert(NWAVES * FM * FN * 64 * 4 == UNIT_FLOATS, "a part fills its unit");
+    auto part_rsrc = [&](int i) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(p.part_ws + ((size_t)unit * parts + i) * UNIT_FLOATS), 0, UNIT_FLOATS * 4, 0x00020000);
+    };
+    const int part_ofs = (wave * (FM * FN) * 64 + lane) * 16;
+    if (parts > 1) {
+        auto tell = [&](int v) {                           // what thread 0 knows, to all
+            int* word = reinterpret_cast<int*>(smem);
+            if (tid == 0) *word = v;
+            __syncthreads();
+            const int r = __builtin_amdgcn_readfirstlane(*word);
+            __syncthreads();
+            return r;
+        };
+        int* counter = p.arrived + unit;
+        int before = tell(tid == 0 ? __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0);
+        if (before != parts - 1) {                         // else all the others are there already
+            const buf_rsrc_t to = part_rsrc(part);
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), to, part_ofs + (i * FN + j) * 1024, 0, AT_DEVICE);
+            WAIT_VMCNT(0);                                 // every wave's stores are complete before the count
+            __syncthreads();
+            before = tell(tid == 0 ? __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0);
+            if (before != parts - 1) return;
+        }
+        if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+
     // ---- epilogue: 64 x 64 results at a time through a patch of LDS of the wave's own, so that memory sees whole lines along the rows
     // and, where the result is wanted the other way round too, along the columns.
     constexpr int PITCH = WN * 4 + 16, PATCH = 64 * PITCH;
@@ -481,20 +537,54 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         const size_t base = (size_t)(matrix % p.count) * ((size_t)p.m * p.n);
         W = (WT*)p.W[tensor] + base;
         copy = p.copies[tensor] ? p.copies[tensor] + base : nullptr;
-        if (p.version && item == matrix * p.tiles && tensor == 0 && tid == 0) p.version[matrix] += 1;
+        if (p.version && t == 0 && tensor == 0 && tid == 0) p.version[matrix] += 1;
     }
 #pragma unroll
-    for (int part = 0; part < WM / 64; ++part) {
-        const int row0 = m0 + wm * WM + part * 64;
+    for (int block = 0; block < WM / 64; ++block) {
+        const int row0 = m0 + wm * WM + block * 64;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
+        // rows of fragments at a time: all loads of a part are on their way before the first is added, as far as there are registers for them
+        constexpr int ROWS_AT_ONCE = GEO::BLOCKS == 1 ? 2 : 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i0 = 0; i0 < 4; i0 += ROWS_AT_ONCE) {
+            f32x4 val[ROWS_AT_ONCE][FN];
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const f32x4& v = acc[part * 4 + i][j];
-                *reinterpret_cast<float4*>(patch + (i * 16 + lrow) * PITCH + (j * 16 + lcol) * 4) = make_float4(v[0], v[1], v[2], v[3]);
-            }
+            for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) val[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            auto add_parts = [&](int q0, int q1) {
+#pragma unroll 1
+                for (int q = q0; q < q1; ++q) {
+                    f32x4 x[ROWS_AT_ONCE][FN];
+                    const buf_rsrc_t from = part_rsrc(q);
+#pragma unroll
+                    for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j)
+                            x[i][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, part_ofs + ((block * 4 + i0 + i) * FN + j) * 1024, 0, AT_DEVICE));
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) val[i][j] += x[i][j];
+                }
+            };
+            add_parts(0, part);
+#pragma unroll
+            for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    asm volatile("" : "+a"(acc[block * 4 + i0 + i][j]));   // they stay where they are until here: read earlier, all at once, they would not fit
+                    val[i][j] += acc[block * 4 + i0 + i][j];
+                }
+            add_parts(part + 1, parts);
+#pragma unroll
+            for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    *reinterpret_cast<float4*>(patch + ((i0 + i) * 16 + lrow) * PITCH + (j * 16 + lcol) * 4) = make_float4(val[i][j][0], val[i][j][1], val[i][j][2], val[i][j][3]);
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
         if (row0 >= p.M || col0 >= p.N) continue;          // sides are multiples of 64: all of it or none
@@ -556,14 +646,37 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     }
 }
 
+// How a product is laid out: the geometry, and into how many parts the tiles after the last full round of the chip's places are cut.
+// Times in us of a slice with one block of 4 waves on a CU and with two (8 waves: one fits), of what a tile costs beside its slices, and of
+// joining parts, as measured where they are the same for all tiles: COSTS
+struct GeometryTime { float alone, slice, over, join; int least; };    // least: slices of a part
+constexpr GeometryTime LARGE_TIME{0.70f, 0.70f, 11.0f, 12.0f, 24}, SMALL_TIME{0.28f, 0.55f, 7.0f, 4.0f, 8};
+constexpr int MAX_PARTS = 8;
+struct Layout { float us; int whole, cut, parts; };
+template <class GEO> Layout layout_of(const GeometryTime& g, int tiles, int slices, int cus)
+{
+    const int places = cus * GEO::BLOCKS;
+    const int whole = tiles / places * places, rem = tiles - whole;
+    const float rounds = (float)(whole / places) * (slices * g.slice + g.over);
+    Layout best{rounds + (rem ? slices * (rem <= cus ? g.alone : g.slice) + g.over : 0.0f), tiles, 0, 1};
+    for (int n = 2; n <= MAX_PARTS && rem > 0 && rem * n <= places && rem < MAX_CUT && slices / n >= g.least; ++n) {
+        const float us = rounds + (float)((slices + n - 1) / n) * (rem * n <= cus ? g.alone : g.slice) + g.over + g.join * (1.0f + 0.25f * (n - 2));
+        if (us < best.us) best = Layout{us, whole, rem, n};
+    }
+    return best;
+}
+
 template <int KIND, int OUT, typename WT, class GEO>
-hipError_t launch_tiles(Product p, int matrices, hipStream_t st)
+hipError_t launch_tiles(Product p, const Layout& l, hipStream_t st)
 {
     p.row_tiles = (p.M + GEO::BM - 1) / GEO::BM;
     p.col_tiles = (p.N + GEO::BN - 1) / GEO::BN;
     p.tiles = p.symmetric ? p.row_tiles * (p.row_tiles + 1) / 2 : p.row_tiles * p.col_tiles;
-    p.items = p.tiles * matrices;
-    p.per_xcd = (p.items + 7) / 8;
+    p.whole = l.whole;
+    p.whole_per_xcd = (l.whole + 7) / 8;                   // with cut tiles after them they are full rounds: a multiple of 8
+    p.cut = l.cut;
+    p.parts = l.parts;
+    p.part_per_xcd = (l.cut * l.parts + 7) / 8;
     static PerDeviceOnce once;
     const int dev = current_device();
     auto kern = product_kernel<KIND, OUT, WT, GEO>;
@@ -572,16 +685,35 @@ hipError_t launch_tiles(Product p, int matrices, hipStream_t st)
         if (e != hipSuccess) return e;
         once.mark(dev);
     }
-    hipLaunchKernelGGL(kern, dim3(8 * p.per_xcd), dim3(GEO::THREADS), GEO::LDS_BYTES, st, p);
+    hipLaunchKernelGGL(kern, dim3(8 * (p.whole_per_xcd + p.part_per_xcd)), dim3(GEO::THREADS), GEO::LDS_BYTES, st, p);
     return hipGetLastError();
 }
 
-// 256 x 256 tiles where they fill the chip.
-template <int KIND, int OUT, typename WT> hipError_t launch_product(const Product& p, int matrices, hipStream_t st)
+template <class GEO> int tiles_of(const Product& p, int matrices)
 {
-    const long rt = (p.M + Large::BM - 1) / Large::BM, ct = (p.N + Large::BN - 1) / Large::BN;
-    const long tiles = (p.symmetric ? rt * (rt + 1) / 2 : rt * ct) * matrices;
-    return tiles >= 256 ? launch_tiles<KIND, OUT, WT, Large>(p, matrices, st) : launch_tiles<KIND, OUT, WT, Small>(p, matrices, st);
+    const int rt = (p.M + GEO::BM - 1) / GEO::BM, ct = (p.N + GEO::BN - 1) / GEO::BN;
+    return (p.symmetric ? rt * (rt + 1) / 2 : rt * ct) * matrices;
+}
+
+template <int KIND, int OUT, typename WT> hipError_t launch_product(const Product& p, int matrices, int cus, hipStream_t st)
+{
+    const int slices = p.n_seg * (p.K / BK);
+    const Layout l = layout_of<Large>(LARGE_TIME, tiles_of<Large>(p, matrices), slices, cus), m = layout_of<Small>(SMALL_TIME, tiles_of<Small>(p, matrices), slices, cus);
+    return l.us < m.us ? launch_tiles<KIND, OUT, WT, Large>(p, l, st) : launch_tiles<KIND, OUT, WT, Small>(p, m, st);
+}
+
+// Compute units of the current device, a multiple of 8 (blocks are dealt to 8 XCDs); 256 at most, which the workspace for parts is sized for.
+inline int device_cus()
+{
+    static std::atomic<int> of[64];
+    const int dev = current_device();
+    int n = (dev >= 0 && dev < 64) ? of[dev].load(std::memory_order_acquire) : 0;
+    if (n == 0) {
+        if (dev < 0 || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8) n = 256;
+        n = n > 256 ? 256 : n / 8 * 8;
+        if (dev >= 0 && dev < 64) of[dev].store(n, std::memory_order_release);
+    }
+    return n;
 }
 
 // Steps that are taken on one Gram matrix, see the head of this file.  What a rounding of A amounts to in one direction grows with the share of A
@@ -597,7 +729,7 @@ constexpr int MAX_CHUNKS = 256;                            // parts of a matrix'
 struct MuonPlan {
     int matrices, m, n, mp, np, planes, chunks;
     size_t x_numbers, a_numbers;                           // of all matrices
-    size_t off_partial, off_x[2], off_a[4], bytes;         // a second plane, where there is one, follows the first
+    size_t off_partial, off_arrived, off_parts, off_x[2], off_a[4], bytes;         // a second plane, where there is one, follows the first
 };
 MuonPlan plan_of(const moe_muon_t& c)
 {
@@ -615,6 +747,8 @@ MuonPlan plan_of(const moe_muon_t& c)
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align_ws(bytes); return at; };
     p.off_partial = take((size_t)p.matrices * p.chunks * sizeof(double));
+    p.off_arrived = take(MAX_CUT * sizeof(int));
+    p.off_parts = take((size_t)256 * Large::UNIT_BYTES);                   // a tile of 256 x 256 for each CU, or two of 128 x 128
     for (size_t& x : p.off_x) x = take(p.x_numbers * sizeof(f16) * p.planes);
     for (size_t& a : p.off_a) a = take(p.a_numbers * sizeof(f16) * p.planes);
     p.bytes = off;
@@ -631,6 +765,8 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
     const MuonPlan P = plan_of(c);
     char* base = (char*)ws;
     double* partial = (double*)(base + P.off_partial);
+    int* arrived = (int*)(base + P.off_arrived);
+    const int cus = device_cus();
     auto stored = [&](size_t off, size_t numbers) { f16* f = (f16*)(base + off); return Stored{f, P.planes == 2 ? f + numbers : nullptr}; };
     Stored X = stored(P.off_x[0], P.x_numbers), X2 = stored(P.off_x[1], P.x_numbers);
     const float S = exp2f(fminf(14.0f, floorf(log2f(sqrtf((float)P.m * (float)P.n))))), SA = 1024.0f, SB = 64.0f, SQ = 8.0f;
@@ -641,7 +777,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         t.momentum[i] = momenta[i];
         t.transposed[i] = (c.rows <= c.cols) == (c.transposed[i] != 0) && c.rows != c.cols ? 1 : 0;
     }
-    hipLaunchKernelGGL(momentum_kernel, dim3(P.chunks, P.matrices), dim3(256), 0, st, t, c.count, (size_t)P.m * P.n, P.chunks, c.momentum, c.nesterov, partial);
+    hipLaunchKernelGGL(momentum_kernel, dim3(P.chunks, P.matrices), dim3(256), 0, st, t, c.count, (size_t)P.m * P.n, P.chunks, c.momentum, c.nesterov, partial, arrived);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(start_kernel, dim3((P.np + START_COLS - 1) / START_COLS, P.mp / 64, P.matrices), dim3(256), 0, st, t, c.count, P.m, P.n, P.mp, P.np,
@@ -666,10 +802,11 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         Product p{};
         operands(p, a, stride, ld, b, stride, ld, ld);
         p.M = p.N = p.ldo = P.mp; p.o_stride = as; p.symmetric = 1;
+        p.part_ws = (float*)(base + P.off_parts); p.arrived = arrived;
         p.alpha = alpha; p.beta = beta; p.diag = diag;
         if (add) { p.D = add->first; p.D_rest = add->rest; }
         p.O = out.first; p.O_rest = out.rest;
-        e = launch_product<ROWS, STORE, float>(p, P.matrices, st);
+        e = launch_product<ROWS, STORE, float>(p, P.matrices, cus, st);
     };
     const Stored A = stored(P.off_a[0], P.a_numbers);
     for (int left = c.steps, of = 0; left > 0 && e == hipSuccess; left -= of) {
@@ -693,10 +830,11 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         Product q{};                                       // X <- Q X
         operands(q, Q, as, P.mp, X, xs, P.np, P.mp);
         q.M = P.mp; q.N = q.ldo = P.np; q.o_stride = xs;
+        q.part_ws = (float*)(base + P.off_parts); q.arrived = arrived;
         q.alpha = 1.0f / q_scale;
         if (of < left) {
             q.O = X2.first; q.O_rest = X2.rest;
-            e = launch_product<COLS, STORE, float>(q, P.matrices, st);
+            e = launch_product<COLS, STORE, float>(q, P.matrices, cus, st);
             const Stored x = X; X = X2; X2 = x;
         } else {
             q.count = c.count; q.m = P.m; q.n = P.n;
@@ -704,7 +842,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
             q.keep = (float)(1.0 - (double)c.lr * c.weight_decay);
             q.rate = (float)((double)c.lr * c.scale / S);
             q.version = version;
-            e = launch_product<COLS, UPDATE, WT>(q, P.matrices, st);
+            e = launch_product<COLS, UPDATE, WT>(q, P.matrices, cus, st);
         }
     }
     return e;
