@@ -40,8 +40,8 @@ constexpr int MAX_CUT = 512;                               // tiles of a launch 
 
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
-    const f16x2 v = {(f16)lo, (f16)hi};
-    return __builtin_bit_cast(uint32_t, v);
+    const moe_f32x2_t v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
 __device__ __forceinline__ u32x4 pack_f16x8(const float* v)
 {
@@ -207,8 +207,8 @@ struct Product {
     float* part_ws;                                        // what a part leaves: [cut tile][part][wave][fragment][lane] as float4
     int* arrived;                                          // parts of a cut tile that have been stored; all zero between two launches
     float alpha, beta, diag;
-    const f16 *D, *D_rest;                                 // addend, laid out like the output; null: none
-    f16 *O, *O_rest;                                       // STORE; O_rest null: 11 bits are kept
+    const f16 *D, *D_rest;                                 // addend, laid out like the output
+    f16 *O, *O_rest;                                       // STORE
     // UPDATE: the weights, as the caller has them
     int count, m, n;
     int transposed[MUON_MAX_TENSORS];
@@ -218,12 +218,13 @@ struct Product {
     int32_t* version;                                      // a counter per matrix of a tensor, or null
 };
 
-// WT: type of the weights (UPDATE).
+// Eight weights in a row, as they lie in memory (raw_t) and as numbers.
 template <typename WT> struct WeightOps;
 template <> struct WeightOps<bf16_t> {
-    static __device__ __forceinline__ void load8(const bf16_t* p, float* w)
+    typedef oct_t raw_t;
+    static __device__ __forceinline__ raw_t load8(const bf16_t* p) { return *reinterpret_cast<const oct_t*>(p); }
+    static __device__ __forceinline__ void numbers(const raw_t& v, float* w)
     {
-        const oct_t v = *reinterpret_cast<const oct_t*>(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { w[2 * i] = __uint_as_float(v[i] << 16); w[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
     }
@@ -235,14 +236,15 @@ template <> struct WeightOps<bf16_t> {
     static __device__ __forceinline__ void store(bf16_t* p, float w) { *p = f32_to_bf16(w); }
 };
 template <> struct WeightOps<float> {
-    static __device__ __forceinline__ void load8(const float* p, float* w)
+    struct raw_t { quad_t q[2]; };
+    static __device__ __forceinline__ raw_t load8(const float* p)
+    {
+        return raw_t{{*reinterpret_cast<const quad_t*>(p), *reinterpret_cast<const quad_t*>(p + 4)}};
+    }
+    static __device__ __forceinline__ void numbers(const raw_t& v, float* w)
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const quad_t v = *reinterpret_cast<const quad_t*>(p + 4 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
-        }
+        for (int i = 0; i < 8; ++i) w[i] = v.q[i / 4][i % 4];
     }
     static __device__ __forceinline__ void store8(float* p, const float* w)
     {
@@ -252,33 +254,18 @@ template <> struct WeightOps<float> {
     static __device__ __forceinline__ float load(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, float w) { *p = w; }
 };
-// Weights at[0 .. there) and their copies.
-template <typename WT> __device__ __forceinline__ void update8(WT* W, uint16_t* copy, size_t at, int there, const float* x, float keep, float rate)
-{
-    typedef WeightOps<WT> Ops;
-    if (there >= 8) {
-        float w[8];
-        Ops::load8(W + at, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = fmaf(-rate, x[e], keep * w[e]);
-        Ops::store8(W + at, w);
-        if (copy) WeightOps<bf16_t>::store8(copy + at, w);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < there) {
-            const float w = fmaf(-rate, x[e], keep * Ops::load(W + at + e));
-            Ops::store(W + at + e, w);
-            if (copy) WeightOps<bf16_t>::store(copy + at + e, w);
-        }
-}
 
+// Where a CU gets one tile of 128 x 128 at most it has all of LDS for it, and what the loop waits for is the way of a request: seven slices
+// ahead instead of three.
+typedef Geometry<2, 2, 2, 2, 9, 1> Deep;
+
+// ADD: there is an addend (and a diagonal); PLANES: numbers an operand is kept in; CUT: some of the tiles are.  Everything past the loop runs once per tile, from code that is
+// not in the instruction cache: what a product does not need is not in its kernel.
 // The loop is that of the grouped FFN (ffn_bf16.hip): slices of 32 straight from memory into a ring of LDS buffers, an operand read along its
 // rows in whole 128-byte lines, two slices of half of the tile's rows at a time; in the 256 x 256 tile the two rows of waves
 // alternate between fetching fragments and multiplying.  One tile per block; consecutive items go to one XCD, so that the tiles in flight
 // there share operands of one matrix in its L2.
-template <int KIND, int OUT, typename WT, class GEO>
+template <int KIND, int OUT, bool ADD, int PLANES, typename WT, class GEO, bool CUT>
 __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void product_kernel(const Product p)
 {
     constexpr int WGN = GEO::WGN, NWAVES = GEO::NWAVES, WM = GEO::WM, WN = GEO::WN, BM = GEO::BM, BN = GEO::BN, TM = GEO::TM, TN = GEO::TN;
@@ -295,17 +282,17 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     // ---- which tile, and which part of it
     const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
     int item = xcd * p.whole_per_xcd + turn, part = 0, unit = 0;
-    const bool cut = turn >= p.whole_per_xcd;
-    if (cut) {
+    int parts = 1;
+    if (CUT && turn >= p.whole_per_xcd) {
         const int i = xcd * p.part_per_xcd + turn - p.whole_per_xcd;
         if (i >= p.cut * p.parts) return;
+        parts = p.parts;
         part = i / p.cut;                                  // neighbours work on the same stretch of the contraction
         unit = i - part * p.cut;
         item = p.whole + unit;
     } else if (item >= p.whole) {
         return;
     }
-    const int parts = cut ? p.parts : 1;
     const int matrix = item / p.tiles, t = item - matrix * p.tiles;
     int rt, ct;
     if (p.symmetric) {                                     // columns of the upper triangle, one after the other
@@ -431,15 +418,20 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
             }
     };
 
-    // ---- main loop: slice t reads the groups of its pair and requests group t + 3
-    constexpr int L = 3;
+    // ---- main loop: slice t reads the groups of its pair and requests group t + L
+    constexpr int L = STAGES - 2;                          // into the slot of group t - 2, last read in slice t - 1
+    static_assert(L % 2 == 1, "the group a slice requests is of the other parity");
     typedef std::integral_constant<int, 0> even_t;
     typedef std::integral_constant<int, 1> odd_t;
-    issue_group(even_t{}, ra, rb);
-    issue_group(odd_t{}, ra, rb);
-    group_fixups();
-    if (k_cnt > 2) issue_group(even_t{}, ra, rb); else issue_group(even_t{}, rnull, rnull);
-    WAIT_VMCNT(SLICE_OPS);                                 // groups 0 and 1 have landed: slices 0 and 1
+#pragma unroll
+    for (int g = 0; g + 1 < L; g += 2) {                   // groups 0 .. L - 1, those that there are
+        const bool there = g < k_cnt;
+        issue_group(even_t{}, there ? ra : rnull, there ? rb : rnull);
+        issue_group(odd_t{}, there ? ra : rnull, there ? rb : rnull);
+        if (there) group_fixups();
+    }
+    issue_group(even_t{}, L - 1 < k_cnt ? ra : rnull, L - 1 < k_cnt ? rb : rnull);
+    WAIT_VMCNT((L - 2) * SLICE_OPS);                       // groups 0 and 1 have landed: slices 0 and 1
     BLOCK_BARRIER();
     if (GEO::TWO_PHASE && wm == 1) BLOCK_BARRIER();
     int cur = 0, pair0 = 0;                                // ring slots of the slice's own group, of the even group of its pair
@@ -454,7 +446,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         group_offsets(other_t{}, oa, ob);
         load_frags(stA, stB, PAR, [&](int n) { if (goes_out(n) >= 0) { __builtin_amdgcn_sched_barrier(0); request_piece(goes_out(n), to, a, b, oa, ob); __builtin_amdgcn_sched_barrier(0); } });
         group_done(other_t{});
-        WAIT_VMCNT(par ? SLICE_OPS : 2 * SLICE_OPS);
+        WAIT_VMCNT((par ? L - 2 : L - 1) * SLICE_OPS);     // next: a pair's two groups, or the second one of a pair that has landed
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);                 // no product moves above the wait
@@ -467,11 +459,11 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         cur = (cur + 1 == STAGES) ? 0 : cur + 1;
         if (par) pair0 = (pair0 + 2 >= STAGES) ? pair0 + 2 - STAGES : pair0 + 2;
     };
-    if (k_cnt > 2) { slice(even_t{}, std::true_type{}, ra, rb); group_fixups(); }
+    if (L < k_cnt) { slice(even_t{}, std::true_type{}, ra, rb); group_fixups(); }
     else slice(even_t{}, std::true_type{}, rnull, rnull);
     int s = 1;
     while (s < k_cnt - 1) {
-        const bool more = s + L < k_cnt;                   // the pair of slices s + 3, s + 4 exists
+        const bool more = s + L < k_cnt;                   // the pair of slices s + L, s + L + 1 exists
         const int n = more ? min((k_cnt - L - s + 1) / 2, (k_per_seg - iss_in_seg) / 2) : (k_cnt - 1 - s) / 2;
         const rsrc_t a = more ? ra : rnull, b = more ? rb : rnull;
         for (int i = 0; i < n; ++i) {
@@ -496,7 +488,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         return __builtin_amdgcn_make_buffer_rsrc((void*)(p.part_ws + ((size_t)unit * parts + i) * UNIT_FLOATS), 0, UNIT_FLOATS * 4, 0x00020000);
     };
     const int part_ofs = (wave * (FM * FN) * 64 + lane) * 16;
-    if (parts > 1) {
+    if (CUT && parts > 1) {
         auto tell = [&](int v) {                           // what thread 0 knows, to all
             int* word = reinterpret_cast<int*>(smem);
             if (tid == 0) *word = v;
@@ -524,10 +516,16 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
 
     // ---- epilogue: 64 x 64 results at a time through a patch of LDS of the wave's own, so that memory sees whole lines along the rows
     // and, where the result is wanted the other way round too, along the columns.
-    constexpr int PITCH = WN * 4 + 16, PATCH = 64 * PITCH;
+    // Its rows are 16 slots of 4 numbers, permuted by the row so that neither the writes (16 rows of a slot), nor the reads along a row, nor
+    // those along a column (8 columns of rows 8 apart) meet in a bank.
+    // Slot c4 of row r lies at r * 256 + 16 (c4 ^ (r & 15) ^ ((r >> 3) & 6)); below, as a part of the lane's own, combined with a constant.
+    constexpr int PATCH = 64 * 256;
     static_assert(WN == 64 && WM % 64 == 0 && NWAVES * PATCH <= (int)GEO::LDS_BYTES, "patches inside the ring");
     unsigned char* patch = smem + wave * PATCH;
-    const int lrow = lane & 15, lcol = (lane >> 4) * 4;
+    const int r8 = lane >> 3, c8 = (lane & 7) * 8;         // row of eight that a pass takes, first of its eight columns
+    const int put_at = (lane & 15) * 256, put_slot = (lane >> 4) ^ (lane & 15);                                // row i 16 + lane % 16, slot j 4 + lane / 16
+    const int row_at = r8 * 256, row_slot = (c8 / 4) ^ r8;                                                     // row pass 8 + r8, from column c8
+    const int col_at = c8 * 256 + (r8 & 3) * 4, col_slot = (r8 >> 2) ^ (c8 & 8) ^ ((c8 >> 3) & 6);             // column pass 8 + r8, from row c8
     const int col0 = n0 + wn * WN;
     const int tensor = OUT == UPDATE ? matrix / p.count : 0;
     const bool tall = OUT == UPDATE && p.transposed[tensor] != 0;
@@ -549,6 +547,15 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
 #pragma unroll
         for (int i0 = 0; i0 < 4; i0 += ROWS_AT_ONCE) {
             f32x4 val[ROWS_AT_ONCE][FN];
+            if constexpr (!CUT) {
+#pragma unroll
+                for (int i = 0; i < ROWS_AT_ONCE; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) {
+                        asm volatile("" : "+a"(acc[block * 4 + i0 + i][j]));
+                        val[i][j] = acc[block * 4 + i0 + i][j];
+                    }
+            } else {
 #pragma unroll
             for (int i = 0; i < ROWS_AT_ONCE; ++i)
 #pragma unroll
@@ -579,78 +586,122 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                     val[i][j] += acc[block * 4 + i0 + i][j];
                 }
             add_parts(part + 1, parts);
+            }
 #pragma unroll
             for (int i = 0; i < ROWS_AT_ONCE; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
-                    *reinterpret_cast<float4*>(patch + ((i0 + i) * 16 + lrow) * PITCH + (j * 16 + lcol) * 4) = make_float4(val[i][j][0], val[i][j][1], val[i][j][2], val[i][j][3]);
+                    *reinterpret_cast<float4*>(patch + put_at + (i0 + i) * 4096 + ((put_slot ^ (j * 4) ^ ((i0 + i) * 2)) << 4)) = make_float4(val[i][j][0], val[i][j][1], val[i][j][2], val[i][j][3]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
         if (row0 >= p.M || col0 >= p.N) continue;          // sides are multiples of 64: all of it or none
-        const bool mirror = OUT == UPDATE ? tall : (p.symmetric && rt != ct);
+        auto row_of = [&](int pass, float* v) {            // eight columns of a row of the block
+            const int k = ((pass & 1) << 3) ^ (pass & 6);
+            *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(patch + row_at + pass * 2048 + ((row_slot ^ k) << 4));
+            *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(patch + row_at + pass * 2048 + ((row_slot ^ k ^ 1) << 4));
+        };
+        auto column_of = [&](int pass, float* v) {         // eight rows of a column
 #pragma unroll
-        for (int pass = 0; pass < 8; ++pass) {
-            const int r = pass * 8 + (lane >> 3), c = (lane & 7) * 8;
-            float* at = reinterpret_cast<float*>(patch + r * PITCH + c * 4);
-            float v[8];
-            *reinterpret_cast<float4*>(v) = *reinterpret_cast<float4*>(at);
-            *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<float4*>(at + 4);
-            const size_t o = (size_t)matrix * p.o_stride + (size_t)(row0 + r) * p.ldo + col0 + c;
+            for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float*>(patch + col_at + e * 256 + ((col_slot ^ (pass * 2) ^ e) << 4));
+        };
+        if constexpr (OUT == STORE) {
+            // Along the rows, and off the diagonal of a symmetric product along the columns too: the addend is symmetric as well and
+            // is read where the result goes.  What memory and LDS give is requested for several passes before the first is used.
+            constexpr int BATCH = GEO::NWAVES == 8 ? 2 : 8;
+            const bool diagonal = row0 == col0;
+            auto put = [&](auto COLUMNS) {
+                constexpr bool columns = decltype(COLUMNS)::value;
+                const size_t o = (size_t)matrix * p.o_stride + (size_t)((columns ? col0 : row0) + r8) * p.ldo + (columns ? row0 : col0) + c8;
+                const size_t pass_step = (size_t)8 * p.ldo;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
-            if (p.D) {
-                float d[8];
-                unpack_f16x8(*reinterpret_cast<const u32x4*>(p.D + o), d);
+                for (int b = 0; b < 8; b += BATCH) {
+                    if (BATCH < 8) __builtin_amdgcn_sched_barrier(0);      // no more than a batch in the registers beside the accumulators
+                    u32x4 d[ADD ? PLANES : 1][BATCH];
+                    float v[BATCH][8];
+                    if constexpr (ADD)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, d[e], v[e]);
-                if (p.D_rest) {
-                    unpack_f16x8(*reinterpret_cast<const u32x4*>(p.D_rest + o), d);
+                        for (int i = 0; i < BATCH; ++i) {
+                            d[0][i] = *reinterpret_cast<const u32x4*>(p.D + o + (b + i) * pass_step);
+                            if constexpr (PLANES == 2) d[1][i] = *reinterpret_cast<const u32x4*>(p.D_rest + o + (b + i) * pass_step);
+                        }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, d[e], v[e]);
+                    for (int i = 0; i < BATCH; ++i) {
+                        if constexpr (columns) column_of(b + i, v[i]);
+                        else row_of(b + i, v[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[i][e] *= p.alpha;
+                        if constexpr (ADD) {
+#pragma unroll
+                            for (int k = 0; k < PLANES; ++k) {
+                                float x[8];
+                                unpack_f16x8(d[k][i], x);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[i][e] = fmaf(p.beta, x[e], v[i][e]);
+                            }
+                            if (!columns && diagonal) {
+                                const float here = (lane & 7) == b + i ? p.diag : 0.0f;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[i][e] += r8 == e ? here : 0.0f;
+                            }
+                        }
+                        const u32x4 first = pack_f16x8(v[i]);
+                        *reinterpret_cast<u32x4*>(p.O + o + (b + i) * pass_step) = first;
+                        if constexpr (PLANES == 2) *reinterpret_cast<u32x4*>(p.O_rest + o + (b + i) * pass_step) = pack_rest(v[i], first);
+                    }
                 }
-            }
-            if constexpr (OUT == STORE) {
-                if (p.symmetric && rt == ct)
+            };
+            put(std::false_type{});
+            if (p.symmetric && rt != ct) put(std::true_type{});
+        } else {
+            // along the rows of the weights, which are columns of the block where they lie on their short side
+            typedef WeightOps<WT> Ops;
+            const int wr = (tall ? col0 : row0) + r8, wc = (tall ? row0 : col0) + c8, w_rows = tall ? p.n : p.m, w_cols = tall ? p.m : p.n;
+            const int there = w_cols - wc;
+            typename Ops::raw_t raw[8];
+            if (there >= 8)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += row0 + r == col0 + c + e ? p.diag : 0.0f;
-                const u32x4 first = pack_f16x8(v);
-                *reinterpret_cast<u32x4*>(p.O + o) = first;
-                if (p.O_rest) *reinterpret_cast<u32x4*>(p.O_rest + o) = pack_rest(v, first);
-            } else if (!tall) {
-                if (row0 + r < p.m && col0 + c < p.n) update8(W, copy, (size_t)(row0 + r) * p.n + col0 + c, p.n - col0 - c, v, p.keep, p.rate);
-            }
-            if (mirror) {
-                *reinterpret_cast<float4*>(at) = *reinterpret_cast<float4*>(v);
-                *reinterpret_cast<float4*>(at + 4) = *reinterpret_cast<float4*>(v + 4);
-            }
-        }
-        if (!mirror) continue;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
+                for (int pass = 0; pass < 8; ++pass)
+                    if (wr + 8 * pass < w_rows) raw[pass] = Ops::load8(W + (size_t)(wr + 8 * pass) * w_cols + wc);
 #pragma unroll
-        for (int pass = 0; pass < 8; ++pass) {
-            const int c = pass * 8 + (lane >> 3), r = (lane & 7) * 8;      // column of the tile, its rows r .. r + 7
-            float v[8];
+            for (int pass = 0; pass < 8; ++pass) {
+                float x[8], w[8];
+                if (tall) column_of(pass, x); else row_of(pass, x);
+                if (wr + 8 * pass >= w_rows) continue;
+                const size_t at = (size_t)(wr + 8 * pass) * w_cols + wc;
+                if (there >= 8) {
+                    Ops::numbers(raw[pass], w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<float*>(patch + (r + e) * PITCH + c * 4);
-            if constexpr (OUT == STORE) {
-                const size_t o = (size_t)matrix * p.o_stride + (size_t)(col0 + c) * p.ldo + row0 + r;
-                const u32x4 first = pack_f16x8(v);
-                *reinterpret_cast<u32x4*>(p.O + o) = first;
-                if (p.O_rest) *reinterpret_cast<u32x4*>(p.O_rest + o) = pack_rest(v, first);
-            } else {
-                if (col0 + c < p.n && row0 + r < p.m) update8(W, copy, (size_t)(col0 + c) * p.m + row0 + r, p.m - row0 - r, v, p.keep, p.rate);
+                    for (int e = 0; e < 8; ++e) w[e] = fmaf(-p.rate, x[e] * p.alpha, p.keep * w[e]);
+                    Ops::store8(W + at, w);
+                    if constexpr (PLANES == 2)
+                        if (copy) WeightOps<bf16_t>::store8(copy + at, w);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < there) {
+                            const float one = fmaf(-p.rate, x[e] * p.alpha, p.keep * Ops::load(W + at + e));
+                            Ops::store(W + at + e, one);
+                            if constexpr (PLANES == 2)
+                                if (copy) WeightOps<bf16_t>::store(copy + at + e, one);
+                        }
+                }
             }
         }
     }
 }
 
 // How a product is laid out: the geometry, and into how many parts the tiles after the last full round of the chip's places are cut.
-// Times in us of a slice with one block of 4 waves on a CU and with two (8 waves: one fits), of what a tile costs beside its slices, and of
-// joining parts, as measured where they are the same for all tiles: COSTS
-struct GeometryTime { float alone, slice, over, join; int least; };    // least: slices of a part
-constexpr GeometryTime LARGE_TIME{0.70f, 0.70f, 11.0f, 12.0f, 24}, SMALL_TIME{0.28f, 0.55f, 7.0f, 4.0f, 8};
+// us of a slice (of all the blocks a CU holds), of what a tile costs beside its slices, and of joining two parts (a quarter more for each
+// further one).  128 x 128 tiles are bound by what L2 delivers to a CU, 29 bytes a clock, whether one or two share it: what more parts
+// gain is CUs, not overlap.  Measured, us: squares of m = 4096 (six; 816 tiles of 256, 128 slices) 413 whole, 370 with the last 48 in five parts; X X^T
+// of 4 x 1024 x 4096 (144 tiles of 128, 128 slices) 38 whole, 33 in three parts, of 6 x 500 x 1333 in two numbers (60 tiles, 126 slices) 42 and 25
+// in four; its squares (48 slices) 17.8 whole, 18.8 in three.
+struct GeometryTime { float slice, over, join; int least; };           // least: slices of a part
+constexpr GeometryTime LARGE_TIME{0.70f, 11.0f, 12.0f, 24}, SMALL_TIME{0.50f, 6.0f, 5.0f, 16}, DEEP_TIME{0.245f, 6.0f, 8.0f, 16};
 constexpr int MAX_PARTS = 8;
 struct Layout { float us; int whole, cut, parts; };
 template <class GEO> Layout layout_of(const GeometryTime& g, int tiles, int slices, int cus)
@@ -658,15 +709,15 @@ template <class GEO> Layout layout_of(const GeometryTime& g, int tiles, int slic
     const int places = cus * GEO::BLOCKS;
     const int whole = tiles / places * places, rem = tiles - whole;
     const float rounds = (float)(whole / places) * (slices * g.slice + g.over);
-    Layout best{rounds + (rem ? slices * (rem <= cus ? g.alone : g.slice) + g.over : 0.0f), tiles, 0, 1};
+    Layout best{rounds + (rem ? slices * g.slice + g.over : 0.0f), tiles, 0, 1};
     for (int n = 2; n <= MAX_PARTS && rem > 0 && rem * n <= places && rem < MAX_CUT && slices / n >= g.least; ++n) {
-        const float us = rounds + (float)((slices + n - 1) / n) * (rem * n <= cus ? g.alone : g.slice) + g.over + g.join * (1.0f + 0.25f * (n - 2));
+        const float us = rounds + (float)((slices + n - 1) / n) * g.slice + g.over + g.join * (1.0f + 0.25f * (n - 2));
         if (us < best.us) best = Layout{us, whole, rem, n};
     }
     return best;
 }
 
-template <int KIND, int OUT, typename WT, class GEO>
+template <int KIND, int OUT, bool ADD, int PLANES, typename WT, class GEO>
 hipError_t launch_tiles(Product p, const Layout& l, hipStream_t st)
 {
     p.row_tiles = (p.M + GEO::BM - 1) / GEO::BM;
@@ -679,13 +730,17 @@ hipError_t launch_tiles(Product p, const Layout& l, hipStream_t st)
     p.part_per_xcd = (l.cut * l.parts + 7) / 8;
     static PerDeviceOnce once;
     const int dev = current_device();
-    auto kern = product_kernel<KIND, OUT, WT, GEO>;
+    // (256 x 256 always with the code for parts: one of the kernels without it spills 17 registers)
+    auto kern = product_kernel<KIND, OUT, ADD, PLANES, WT, GEO, GEO::NWAVES == 8>;
+    auto kern_cut = product_kernel<KIND, OUT, ADD, PLANES, WT, GEO, true>;
     if (!once.is_done(dev)) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)GEO::LDS_BYTES);
-        if (e != hipSuccess) return e;
+        for (auto k : {kern, kern_cut}) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)GEO::LDS_BYTES);
+            if (e != hipSuccess) return e;
+        }
         once.mark(dev);
     }
-    hipLaunchKernelGGL(kern, dim3(8 * (p.whole_per_xcd + p.part_per_xcd)), dim3(GEO::THREADS), GEO::LDS_BYTES, st, p);
+    hipLaunchKernelGGL(l.cut ? kern_cut : kern, dim3(8 * (p.whole_per_xcd + p.part_per_xcd)), dim3(GEO::THREADS), GEO::LDS_BYTES, st, p);
     return hipGetLastError();
 }
 
@@ -695,11 +750,15 @@ template <class GEO> int tiles_of(const Product& p, int matrices)
     return (p.symmetric ? rt * (rt + 1) / 2 : rt * ct) * matrices;
 }
 
-template <int KIND, int OUT, typename WT> hipError_t launch_product(const Product& p, int matrices, int cus, hipStream_t st)
+template <int KIND, int OUT, bool ADD, int PLANES, typename WT> hipError_t launch_product(const Product& p, int matrices, int cus, hipStream_t st)
 {
-    const int slices = p.n_seg * (p.K / BK);
-    const Layout l = layout_of<Large>(LARGE_TIME, tiles_of<Large>(p, matrices), slices, cus), m = layout_of<Small>(SMALL_TIME, tiles_of<Small>(p, matrices), slices, cus);
-    return l.us < m.us ? launch_tiles<KIND, OUT, WT, Large>(p, l, st) : launch_tiles<KIND, OUT, WT, Small>(p, m, st);
+    const int slices = p.n_seg * (p.K / BK), tiles = tiles_of<Small>(p, matrices);
+    const Layout l = layout_of<Large>(LARGE_TIME, tiles_of<Large>(p, matrices), slices, cus), m = layout_of<Small>(SMALL_TIME, tiles, slices, cus);
+    if (tiles <= cus) {
+        const Layout d = layout_of<Deep>(DEEP_TIME, tiles, slices, cus);
+        if (d.us < l.us && d.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Deep>(p, d, st);
+    }
+    return l.us < m.us ? launch_tiles<KIND, OUT, ADD, PLANES, WT, Large>(p, l, st) : launch_tiles<KIND, OUT, ADD, PLANES, WT, Small>(p, m, st);
 }
 
 // Compute units of the current device, a multiple of 8 (blocks are dealt to 8 XCDs); 256 at most, which the workspace for parts is sized for.
@@ -758,7 +817,7 @@ MuonPlan plan_of(const moe_muon_t& c)
 // A batch of matrices in the workspace: its numbers and, with two planes, what they leave off.
 struct Stored { f16 *first, *rest; };
 
-template <typename WT>
+template <int PLANES, typename WT>
 hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
                      int32_t* version, void* ws, hipStream_t st)
 {
@@ -806,7 +865,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         p.alpha = alpha; p.beta = beta; p.diag = diag;
         if (add) { p.D = add->first; p.D_rest = add->rest; }
         p.O = out.first; p.O_rest = out.rest;
-        e = launch_product<ROWS, STORE, float>(p, P.matrices, cus, st);
+        e = add ? launch_product<ROWS, STORE, true, PLANES, float>(p, P.matrices, cus, st) : launch_product<ROWS, STORE, false, PLANES, float>(p, P.matrices, cus, st);
     };
     const Stored A = stored(P.off_a[0], P.a_numbers);
     for (int left = c.steps, of = 0; left > 0 && e == hipSuccess; left -= of) {
@@ -834,7 +893,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         q.alpha = 1.0f / q_scale;
         if (of < left) {
             q.O = X2.first; q.O_rest = X2.rest;
-            e = launch_product<COLS, STORE, float>(q, P.matrices, cus, st);
+            e = launch_product<COLS, STORE, false, PLANES, float>(q, P.matrices, cus, st);
             const Stored x = X; X = X2; X2 = x;
         } else {
             q.count = c.count; q.m = P.m; q.n = P.n;
@@ -842,7 +901,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
             q.keep = (float)(1.0 - (double)c.lr * c.weight_decay);
             q.rate = (float)((double)c.lr * c.scale / S);
             q.version = version;
-            e = launch_product<COLS, UPDATE, WT>(q, P.matrices, cus, st);
+            e = launch_product<COLS, UPDATE, false, PLANES, WT>(q, P.matrices, cus, st);
         }
     }
     return e;
@@ -855,6 +914,6 @@ size_t muon_workspace_bytes(const moe_muon_t& c) { return plan_of(c).bytes; }
 hipError_t launch_muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
                             int32_t* version, void* ws, hipStream_t st)
 {
-    return c.dtype == MOE_F32 ? muon_step<float>(c, grads, momenta, weights, copies, version, ws, st)
-                              : muon_step<bf16_t>(c, grads, momenta, weights, copies, version, ws, st);
+    return c.dtype == MOE_F32 ? muon_step<2, float>(c, grads, momenta, weights, copies, version, ws, st)
+                              : muon_step<1, bf16_t>(c, grads, momenta, weights, copies, version, ws, st);
 }

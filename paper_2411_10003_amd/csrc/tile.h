@@ -26,7 +26,7 @@ template <int WGM_, int WGN_, int TM_, int TN_, int STAGES_, int BLOCKS_> struct
     static constexpr int EP_ROWS = 32;                     // rows a wave stages at a time: two rows of fragments
     static constexpr int EP_WAVE = EP_ROWS * EP_PITCH;
     static constexpr size_t LDS_BYTES = (size_t)STAGES * STAGE_BYTES;
-    static constexpr bool TWO_PHASE = BLOCKS == 1;         // the rows of waves of a block alternate; else the blocks of a CU do
+    static constexpr bool TWO_PHASE = BLOCKS == 1 && NWAVES == 8;      // the rows of waves of a block alternate; else the blocks of a CU do
     static constexpr int UNIT_BYTES = BM * BN * 4;         // a partial tile of a K-split round
     static_assert(LDS_BYTES >= (size_t)NWAVES * EP_WAVE && BLOCKS * LDS_BYTES <= 160 * 1024, "patches inside the ring, rings inside LDS");
     static_assert(WGM == 2 && WGN % 2 == 0, "the two halves of a K-contiguous operand's rows belong to one row of waves or half the columns");
