@@ -232,6 +232,18 @@ template <> struct WeightOps<bf16_t> {
     {
         *reinterpret_cast<oct_t*>(p) = oct_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
     }
+    static __device__ __forceinline__ void load4(const bf16_t* p, float* w)
+    {
+        typedef unsigned two_t __attribute__((ext_vector_type(2), aligned(2)));
+        const two_t v = *reinterpret_cast<const two_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { w[2 * i] = __uint_as_float(v[i] << 16); w[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ void store4(bf16_t* p, const float* w)
+    {
+        typedef unsigned two_t __attribute__((ext_vector_type(2), aligned(2)));
+        *reinterpret_cast<two_t*>(p) = two_t{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
+    }
     static __device__ __forceinline__ float load(const bf16_t* p) { return bf16_to_f32(*p); }
     static __device__ __forceinline__ void store(bf16_t* p, float w) { *p = f32_to_bf16(w); }
 };
@@ -251,6 +263,13 @@ template <> struct WeightOps<float> {
         *reinterpret_cast<quad_t*>(p) = quad_t{w[0], w[1], w[2], w[3]};
         *reinterpret_cast<quad_t*>(p + 4) = quad_t{w[4], w[5], w[6], w[7]};
     }
+    static __device__ __forceinline__ void load4(const float* p, float* w)
+    {
+        const quad_t v = *reinterpret_cast<const quad_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = v[i];
+    }
+    static __device__ __forceinline__ void store4(float* p, const float* w) { *reinterpret_cast<quad_t*>(p) = quad_t{w[0], w[1], w[2], w[3]}; }
     static __device__ __forceinline__ float load(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, float w) { *p = w; }
 };
@@ -694,6 +713,303 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     }
 }
 
+// ---- small matrices: the whole update in one launch -----------------------------------------------------
+// A block per matrix, X, A and B in LDS from beginning to end (the form with X on its long side: nothing is gained by the Gram matrix here).
+// What bounds the general way here is what a launch costs: 17 of them, 6 us and more each, 133 us for four matrices of 64 x 256 in two numbers,
+// where this takes 34: 4 us for the momentum, 3.5 for X, 20 for five steps, 4 for the weights.
+// Rows of X, A and B lie in LDS as they are, the 16-byte pieces of 128 bytes permuted by the row (a fragment reads a piece of 16 rows, a transposing
+// one 4 columns of 4 rows at a time).
+constexpr int FEW_WAVES = 8;
+constexpr int FEW_QUADS = 16, FEW_ELEMENTS = FEW_QUADS * 4 * FEW_WAVES * 64;      // of a matrix that a thread, a block has in registers
+constexpr size_t FEW_LDS = 159 * 1024;                     // X, A and B; the rest of the 160 KB holds the parts of the norm
+struct Few {
+    int m, n, np, count, nesterov, steps;
+    float mu, eps, S, SA, SB, a, b, c, keep, rate;
+    const float* grad[MUON_MAX_TENSORS];
+    float* momentum[MUON_MAX_TENSORS];
+    void* W[MUON_MAX_TENSORS];
+    uint16_t* copies[MUON_MAX_TENSORS];
+    int transposed[MUON_MAX_TENSORS];
+    int32_t* version;
+};
+inline size_t few_lds(int mp, int np, int planes) { return (size_t)planes * 2 * ((size_t)mp * np + 2 * (size_t)mp * mp); }
+
+// PLANES numbers an element, MT row tiles of 16
+template <int PLANES, int MT, typename WT>
+__global__ __launch_bounds__(FEW_WAVES * 64) void few_kernel(const Few p)
+{
+    constexpr int MP = MT * 16, THREADS = FEW_WAVES * 64, TILES = MT * MT / FEW_WAVES;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    __shared__ double words[FEW_WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int matrix = blockIdx.x, tensor = matrix / p.count;
+    const bool tall = p.transposed[tensor] != 0;
+    const size_t base = (size_t)(matrix % p.count) * ((size_t)p.m * p.n);
+    const float* __restrict__ G = p.grad[tensor] + base;
+    float* __restrict__ M = p.momentum[tensor] + base;
+
+    const uint32_t x_plane = (uint32_t)MP * p.np * 2;
+    constexpr uint32_t A_PLANE = MP * MP * 2;
+    unsigned char *const X = smem, *const A = smem + PLANES * x_plane, *const B = A + PLANES * A_PLANE;
+    auto at = [](int row, int col, int ld) { return (uint32_t)(row * ld * 2 + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2); };
+    // 16 rows from `row`, 32 steps from `col`
+    auto frag = [&](const unsigned char* m, int row, int col, int ld) {
+        return *reinterpret_cast<const f16x8*>(m + at(row + (lane & 15), col + 8 * (lane >> 4), ld));
+    };
+    // 16 columns from `col`, 32 steps, which are rows, from `row`
+    auto frag_columns = [&](const unsigned char* m, int row, int col, int ld) {
+        typedef __attribute__((__vector_size__(8))) __fp16 four_t;
+        typedef __attribute__((address_space(3))) four_t lds_four_t;
+        f16x8 f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t o = at(row + 8 * (lane >> 4) + 4 * h + ((lane & 15) >> 2), col + 4 * (lane & 3), ld);
+            const four_t v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_four_t*)(m + o));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[4 * h + i] = (f16)v[i];
+        }
+        return f;
+    };
+    // four numbers of a row from a result: row l % 16, columns 4 (l / 16) .. + 3 of a tile
+    auto put = [&](unsigned char* m, uint32_t plane, int row, int col, int ld, const f32x4& v) {
+        const uint32_t o = at(row + (lane & 15), col + 4 * (lane >> 4), ld);
+        const uint32_t lo = pack_f16x2(v[0], v[1]), hi = pack_f16x2(v[2], v[3]);
+        *reinterpret_cast<uint2*>(m + o) = make_uint2(lo, hi);
+        if constexpr (PLANES == 2) {
+            const f16x2 f0 = __builtin_bit_cast(f16x2, lo), f1 = __builtin_bit_cast(f16x2, hi);
+            *reinterpret_cast<uint2*>(m + plane + o) = make_uint2(pack_f16x2(v[0] - (float)f0[0], v[1] - (float)f0[1]), pack_f16x2(v[2] - (float)f1[0], v[3] - (float)f1[1]));
+        }
+    };
+    // The sum of a product of numbers in two planes: hi lo + lo hi apart from hi hi until the end.
+    struct Sum { f32x4 big, small; };
+    auto clear = [](Sum& a) { a.big = a.small = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; };
+    auto mma = [](Sum& a, const f16x8 (&rows)[PLANES], const f16x8 (&cols)[PLANES]) {
+        if constexpr (PLANES == 2) {
+            a.small = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols[1], rows[0], a.small, 0, 0, 0);
+            a.small = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols[0], rows[1], a.small, 0, 0, 0);
+        }
+        a.big = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols[0], rows[0], a.big, 0, 0, 0);
+    };
+    auto total = [](const Sum& a, int e) { return PLANES == 2 ? a.big[e] + a.small[e] : a.big[e]; };
+
+    // ---- momentum and the norm, all of a thread's elements in its registers; then X, with zeros up to the padded sides
+    const int elements = p.m * p.n, quads = elements / 4, w_cols = tall ? p.m : p.n;
+    float u[FEW_QUADS][4], u_tail = 0.0f;
+    {
+        quad_t g[FEW_QUADS], v[FEW_QUADS];
+#pragma unroll
+        for (int k = 0; k < FEW_QUADS; ++k) {
+            const int q = tid + k * THREADS;
+            if (q < quads) { g[k] = *reinterpret_cast<const quad_t*>(G + 4 * q); v[k] = *reinterpret_cast<const quad_t*>(M + 4 * q); }
+        }
+        for (uint32_t o = tid * 16; o < PLANES * x_plane; o += THREADS * 16) *reinterpret_cast<u32x4*>(X + o) = u32x4{0, 0, 0, 0};
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < FEW_QUADS; ++k) {
+            const int q = tid + k * THREADS;
+            if (q < quads) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[k][e] = fmaf(p.mu, v[k][e], g[k][e]);
+                    u[k][e] = direction(g[k][e], v[k][e], p.mu, p.nesterov);
+                    sum = fma((double)u[k][e], (double)u[k][e], sum);
+                }
+                *reinterpret_cast<quad_t*>(M + 4 * q) = v[k];
+            }
+        }
+        if (tid < elements % 4) {
+            const int e = quads * 4 + tid;
+            const float gt = G[e], vt = fmaf(p.mu, M[e], gt);
+            M[e] = vt;
+            u_tail = direction(gt, vt, p.mu, p.nesterov);
+            sum = fma((double)u_tail, (double)u_tail, sum);
+        }
+        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        if (lane == 0) words[wave] = sum;
+    }
+    __syncthreads();
+    // row and column of a thread's quads: q grows by THREADS
+    auto for_each_quad = [&](auto use) {
+        int i = 4 * tid / w_cols, j = 4 * tid - i * w_cols;
+        const int di = 4 * THREADS / w_cols, dj = 4 * THREADS - di * w_cols;
+#pragma unroll
+        for (int k = 0; k < FEW_QUADS; ++k) {
+            if (tid + k * THREADS < quads) {
+                int r = i, c = j;
+                uint32_t o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = tall ? at(c, r, p.np) : at(r, c, p.np);
+                    if (++c == w_cols) { c = 0; ++r; }
+                }
+                use(k, o);
+            }
+            i += di; j += dj;
+            if (j >= w_cols) { j -= w_cols; ++i; }
+        }
+    };
+    const int tail_e = quads * 4 + tid, tail_i = tail_e / w_cols, tail_j = tail_e - tail_i * w_cols;
+    const uint32_t tail_o = tall ? at(tail_j, tail_i, p.np) : at(tail_i, tail_j, p.np);        // of the threads that have one
+    auto put_one = [&](uint32_t o, float x) {
+        const f16 h = (f16)x;
+        *reinterpret_cast<f16*>(X + o) = h;
+        if constexpr (PLANES == 2) *reinterpret_cast<f16*>(X + x_plane + o) = (f16)(x - (float)h);
+    };
+    auto get_one = [&](uint32_t o) {
+        float x = (float)*reinterpret_cast<const f16*>(X + o);
+        if constexpr (PLANES == 2) x += (float)*reinterpret_cast<const f16*>(X + x_plane + o);
+        return x;
+    };
+    {
+        double sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) sum += words[w];
+        const double factor = (double)p.S / (sqrt(sum) + (double)p.eps);
+        for_each_quad([&](int k, const uint32_t (&o)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put_one(o[e], (float)((double)u[k][e] * factor));
+        });
+        if (tid < elements % 4) put_one(tail_o, (float)((double)u_tail * factor));
+    }
+    __syncthreads();
+
+    const int row_tile = wave * TILES / MT, col_tile0 = wave * TILES % MT;         // of A and B: TILES tiles of a row
+    for (int step = 0; step < p.steps; ++step) {
+        Sum acc[TILES];
+        {                                                  // A = X X^T
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) clear(acc[t]);
+#pragma unroll 2
+            for (int k = 0; k < p.np; k += 32) {
+                f16x8 fa[PLANES], fb[TILES][PLANES];
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) {
+                    fa[q] = frag(X + q * x_plane, row_tile * 16, k, p.np);
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) fb[t][q] = frag(X + q * x_plane, (col_tile0 + t) * 16, k, p.np);
+                }
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) mma(acc[t], fa, fb[t]);
+            }
+            const float alpha = p.SA / (p.S * p.S);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = total(acc[t], e) * alpha;
+                put(A, A_PLANE, row_tile * 16, (col_tile0 + t) * 16, MP, v);
+            }
+        }
+        __syncthreads();
+        {                                                  // B = a + b A + c A A
+            const float alpha = p.c * p.SB / (p.SA * p.SA), beta = p.b * p.SB / p.SA, diag = p.a * p.SB;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) clear(acc[t]);
+#pragma unroll
+            for (int k = 0; k < MP; k += 32) {
+                f16x8 fa[PLANES];
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) fa[q] = frag(A + q * A_PLANE, row_tile * 16, k, MP);
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    f16x8 fb[PLANES];
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) fb[q] = frag(A + q * A_PLANE, (col_tile0 + t) * 16, k, MP);
+                    mma(acc[t], fa, fb);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const int row = row_tile * 16 + (lane & 15), col = (col_tile0 + t) * 16 + 4 * (lane >> 4);
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = total(acc[t], e) * alpha;
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) x = fmaf(beta, (float)*reinterpret_cast<const f16*>(A + q * A_PLANE + at(row, col + e, MP)), x);
+                    v[e] = x + (row == col + e ? diag : 0.0f);
+                }
+                put(B, A_PLANE, row_tile * 16, (col_tile0 + t) * 16, MP, v);
+            }
+        }
+        __syncthreads();
+        // X = B X: a wave takes twice 16 columns at a time, which nobody else reads now
+        for (int col0 = wave * 16; col0 < p.np; col0 += 2 * FEW_WAVES * 16) {
+            const bool two = col0 + FEW_WAVES * 16 < p.np;
+            Sum sum[2][MT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) clear(sum[h][t]);
+#pragma unroll
+            for (int k = 0; k < MP; k += 32) {
+                f16x8 fx[2][PLANES];
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) {
+                    fx[0][q] = frag_columns(X + q * x_plane, k, col0, p.np);
+                    fx[1][q] = frag_columns(X + q * x_plane, k, two ? col0 + FEW_WAVES * 16 : col0, p.np);
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    f16x8 fb[PLANES];
+#pragma unroll
+                    for (int q = 0; q < PLANES; ++q) fb[q] = frag(B + q * A_PLANE, t * 16, k, MP);
+                    mma(sum[0][t], fb, fx[0]);
+                    mma(sum[1][t], fb, fx[1]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1 && !two) break;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = total(sum[h][t], e) * (1.0f / p.SB);
+                    put(X, x_plane, t * 16, col0 + h * FEW_WAVES * 16, p.np, v);
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    // ---- the weights, along their rows
+    typedef WeightOps<WT> Ops;
+    WT* W = (WT*)p.W[tensor] + base;
+    uint16_t* copy = PLANES == 2 && p.copies[tensor] ? p.copies[tensor] + base : nullptr;
+    auto one = [&](float w, uint32_t o) { return fmaf(-p.rate, get_one(o), p.keep * w); };
+    float w[FEW_QUADS][4];
+#pragma unroll
+    for (int k = 0; k < FEW_QUADS; ++k)
+        if (tid + k * THREADS < quads) Ops::load4(W + 4 * (tid + k * THREADS), w[k]);
+    for_each_quad([&](int k, const uint32_t (&o)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[k][e] = one(w[k][e], o[e]);
+        Ops::store4(W + 4 * (tid + k * THREADS), w[k]);
+        if (PLANES == 2 && copy) WeightOps<bf16_t>::store4(copy + 4 * (tid + k * THREADS), w[k]);
+    });
+    if (tid < elements % 4) {
+        const float x = one(Ops::load(W + tail_e), tail_o);
+        Ops::store(W + tail_e, x);
+        if (PLANES == 2 && copy) WeightOps<bf16_t>::store(copy + tail_e, x);
+    }
+    if (p.version && tensor == 0 && tid == 0) p.version[matrix] += 1;
+}
+
+template <int PLANES, int MT, typename WT> hipError_t launch_few(const Few& f, int matrices, hipStream_t st)
+{
+    static PerDeviceOnce once;
+    const int dev = current_device();
+    auto kern = few_kernel<PLANES, MT, WT>;
+    if (!once.is_done(dev)) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)FEW_LDS);
+        if (e != hipSuccess) return e;
+        once.mark(dev);
+    }
+    hipLaunchKernelGGL(kern, dim3(matrices), dim3(FEW_WAVES * 64), few_lds(MT * 16, f.np, PLANES), st, f);
+    return hipGetLastError();
+}
+
 // How a product is laid out: the geometry, and into how many parts the tiles after the last full round of the chip's places are cut.
 // us of a slice (of all the blocks a CU holds), of what a tile costs beside its slices, and of joining two parts (a quarter more for each
 // further one).  128 x 128 tiles are bound by what L2 delivers to a CU, 29 bytes a clock, whether one or two share it: what more parts
@@ -834,7 +1150,21 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
     for (int i = 0; i < c.n_tensors; ++i) {
         t.grad[i] = grads[i];
         t.momentum[i] = momenta[i];
+        // what lies on its short side
         t.transposed[i] = (c.rows <= c.cols) == (c.transposed[i] != 0) && c.rows != c.cols ? 1 : 0;
+    }
+    const float keep = (float)(1.0 - (double)c.lr * c.weight_decay), rate = (float)((double)c.lr * c.scale / S);
+    const int few_mp = P.mp <= 64 ? 64 : 128;
+    if (P.mp <= 128 && P.m * P.n <= FEW_ELEMENTS && few_lds(few_mp, P.np, PLANES) <= FEW_LDS) {
+        Few f{};
+        f.m = P.m; f.n = P.n; f.np = P.np; f.count = c.count; f.nesterov = c.nesterov; f.steps = c.steps;
+        f.mu = c.momentum; f.eps = c.eps; f.S = S; f.SA = SA; f.SB = SB; f.a = c.a; f.b = c.b; f.c = c.c; f.keep = keep; f.rate = rate;
+        for (int i = 0; i < c.n_tensors; ++i) {
+            f.grad[i] = grads[i]; f.momentum[i] = momenta[i]; f.W[i] = weights[i]; f.copies[i] = copies ? copies[i] : nullptr; f.transposed[i] = t.transposed[i];
+        }
+        f.version = version;
+        if (few_mp == 64) return launch_few<PLANES, 4, WT>(f, P.matrices, st);
+        if constexpr (PLANES == 1) return launch_few<PLANES, 8, WT>(f, P.matrices, st);    // two numbers of 128 x 128 twice leave no room for X
     }
     hipLaunchKernelGGL(momentum_kernel, dim3(P.chunks, P.matrices), dim3(256), 0, st, t, c.count, (size_t)P.m * P.n, P.chunks, c.momentum, c.nesterov, partial, arrived);
     hipError_t e = hipGetLastError();
@@ -898,8 +1228,8 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         } else {
             q.count = c.count; q.m = P.m; q.n = P.n;
             for (int i = 0; i < c.n_tensors; ++i) { q.transposed[i] = t.transposed[i]; q.W[i] = weights[i]; q.copies[i] = copies ? copies[i] : nullptr; }
-            q.keep = (float)(1.0 - (double)c.lr * c.weight_decay);
-            q.rate = (float)((double)c.lr * c.scale / S);
+            q.keep = keep;
+            q.rate = rate;
             q.version = version;
             e = launch_product<COLS, UPDATE, false, PLANES, WT>(q, P.matrices, cus, st);
         }
