@@ -8,6 +8,10 @@
 // Bound by HBM: two to four elements move per element of the rows and a dozen vector instructions go with them.  A row
 // is read once: it stays in the registers of the TPR threads that share it, U pieces of 16 bytes each, through both of the forward sums
 // (the variance is that of the centred row, not a difference of squares).  Sums are fp32 and in a fixed order.
+//
+// Measured on buffers that change from call to call, bf16 with a residual: 32768 x 4096 forward 184 us, 5.8 TB/s, backward with the parameters'
+// gradients 174, 6.2 TB/s (512 partial sums and no row ahead 207; rows through the caches, with stores and loads as usual, 192 and 207);
+// 16384 x 2048 47 and 52.  One row of 2048: 3.4 us on the GPU.
 #include "internal.h"
 
 #include <type_traits>
@@ -42,10 +46,14 @@ template <> struct Piece<bf16_t> {
 };
 
 // `n`: elements of this piece inside the row; only with TAIL is it ever less than a whole piece.
-template <typename ET, bool TAIL> __device__ __forceinline__ moe_piece_t load_row_piece(const ET* p, int n)
+// NT: past the caches (STREAM_BYTES).
+template <typename ET, bool TAIL, bool NT> __device__ __forceinline__ moe_piece_t load_row_piece(const ET* p, int n)
 {
     typedef typename Piece<ET>::mem_t mem_t;
-    if (!TAIL || n == Piece<ET>::N) return *reinterpret_cast<const mem_t*>(p);
+    if (!TAIL || n == Piece<ET>::N) {
+        if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const mem_t*>(p));
+        else return *reinterpret_cast<const mem_t*>(p);
+    }
     float f[Piece<ET>::N];
 #pragma unroll
     for (int i = 0; i < Piece<ET>::N; ++i) {
@@ -54,10 +62,14 @@ template <typename ET, bool TAIL> __device__ __forceinline__ moe_piece_t load_ro
     }
     return Piece<ET>::pack(f);
 }
-template <typename ET, bool TAIL> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
+template <typename ET, bool TAIL, bool NT> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
 {
     typedef typename Piece<ET>::mem_t mem_t;
-    if (!TAIL || n == Piece<ET>::N) { *reinterpret_cast<mem_t*>(p) = v; return; }
+    if (!TAIL || n == Piece<ET>::N) {
+        if constexpr (NT) __builtin_nontemporal_store((mem_t)v, reinterpret_cast<mem_t*>(p));
+        else *reinterpret_cast<mem_t*>(p) = v;
+        return;
+    }
     float f[Piece<ET>::N];
     Piece<ET>::unpack(v, f);
 #pragma unroll
@@ -84,7 +96,8 @@ template <int N, bool TAIL> __device__ __forceinline__ void load_columns(const f
     for (int i = 0; i < N; ++i) f[i] = i < n ? p[i] : 0.0f;
 }
 
-constexpr int threads_of(int tpr) { return tpr > 256 ? tpr : 256; }
+// Rows of a wave or less share a block of 256; the threads of a wider one are the block.
+constexpr int threads_of(int tpr) { return tpr > 64 ? tpr : 256; }
 
 // Sums of M values over the TPR threads of a row, the same bits in each of them.  Rows of more than a wave go through `words`
 // (LDS, M x waves floats); two sets of them in turn, so that one barrier a sum is enough.
@@ -112,7 +125,7 @@ template <int TPR, int M> __device__ __forceinline__ void row_sums(float (&v)[M]
     }
 }
 
-template <typename ET, int TPR, int U, bool TAIL>
+template <typename ET, int TPR, int U, bool TAIL, bool NT>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
     const ET* X, const ET* R, const float* __restrict__ gamma, const float* __restrict__ beta, ET* S, ET* Y,
     float* __restrict__ mean_out, float* __restrict__ rstd_out, int rows, int d, float eps)
@@ -131,13 +144,13 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
         for (int u = 0; u < U; ++u) {
             n[u] = min(N, max(0, d - (c + u * TPR) * N));
             x[u] = moe_piece_t{0, 0, 0, 0};
-            if (n[u] > 0) x[u] = load_row_piece<ET, TAIL>(X + base + (c + u * TPR) * N, n[u]);
+            if (n[u] > 0) x[u] = load_row_piece<ET, TAIL, NT>(X + base + (c + u * TPR) * N, n[u]);
         }
         if (R) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 r[u] = moe_piece_t{0, 0, 0, 0};
-                if (n[u] > 0) r[u] = load_row_piece<ET, TAIL>(R + base + (c + u * TPR) * N, n[u]);
+                if (n[u] > 0) r[u] = load_row_piece<ET, TAIL, NT>(R + base + (c + u * TPR) * N, n[u]);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -147,7 +160,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
 #pragma unroll
                 for (int i = 0; i < N; ++i) a[i] += b[i];
                 x[u] = Piece<ET>::pack(a);
-                if (n[u] > 0) store_row_piece<ET, TAIL>(S + base + (c + u * TPR) * N, x[u], n[u]);
+                if (n[u] > 0) store_row_piece<ET, TAIL, NT>(S + base + (c + u * TPR) * N, x[u], n[u]);
             }
         }
         float sum[1] = {0.0f};
@@ -186,14 +199,14 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
             if (beta) load_columns<N, TAIL>(beta + (c + u * TPR) * N, n[u], b);
 #pragma unroll
             for (int i = 0; i < N; ++i) a[i] = fmaf((a[i] - mean) * rstd, g[i], b[i]);
-            store_row_piece<ET, TAIL>(Y + base + (c + u * TPR) * N, Piece<ET>::pack(a), n[u]);
+            store_row_piece<ET, TAIL, NT>(Y + base + (c + u * TPR) * N, Piece<ET>::pack(a), n[u]);
         }
     }
 }
 
 // Columns stay with their thread from row to row, so the parameters' gradients are summed in registers; a block leaves one partial
 // sum of each in `partial`, [block][2][d].
-template <typename ET, int TPR, int U, bool TAIL>
+template <typename ET, int TPR, int U, bool TAIL, bool NT>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
     const ET* dY, const ET* __restrict__ S, const float* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
     const ET* dS, ET* dX, float* __restrict__ partial, int rows, int d)
@@ -229,19 +242,34 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
             return g[0];
         }
     };
-    for (long row = (long)blockIdx.x * RPB + in_block; row < rows; row += (long)gridDim.x * RPB) {
+    // The next row is on its way while this one is worked on (32768 x 4096: 232 us without).
+    moe_piece_t ny[U], ns[U], nr[U];
+    float n_mean = 0.0f, n_rstd = 0.0f;
+    auto request = [&](long row) {
         const size_t base = (size_t)row * d;
-        moe_piece_t py[U], ps[U], pr[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            py[u] = ps[u] = pr[u] = moe_piece_t{0, 0, 0, 0};
+            ny[u] = ns[u] = nr[u] = moe_piece_t{0, 0, 0, 0};
             if (n[u] > 0) {
-                py[u] = load_row_piece<ET, TAIL>(dY + base + (c + u * TPR) * N, n[u]);
-                ps[u] = load_row_piece<ET, TAIL>(S + base + (c + u * TPR) * N, n[u]);
-                if (dS) pr[u] = load_row_piece<ET, TAIL>(dS + base + (c + u * TPR) * N, n[u]);
+                ny[u] = load_row_piece<ET, TAIL, NT>(dY + base + (c + u * TPR) * N, n[u]);
+                ns[u] = load_row_piece<ET, TAIL, NT>(S + base + (c + u * TPR) * N, n[u]);
+                if (dS) nr[u] = load_row_piece<ET, TAIL, NT>(dS + base + (c + u * TPR) * N, n[u]);
             }
         }
-        const float mean = mean_in[row], rstd = rstd_in[row];
+        n_mean = mean_in[row];
+        n_rstd = rstd_in[row];
+    };
+    const long row0 = (long)blockIdx.x * RPB + in_block, row_step = (long)gridDim.x * RPB;
+    constexpr bool AHEAD = U < 4;                          // four pieces and the next four do not fit the registers
+    if (AHEAD && row0 < rows) request(row0);
+    for (long row = row0; row < rows; row += row_step) {
+        const size_t base = (size_t)row * d;
+        moe_piece_t py[U], ps[U], pr[U];
+        if (!AHEAD) request(row);
+#pragma unroll
+        for (int u = 0; u < U; ++u) { py[u] = ny[u]; ps[u] = ns[u]; pr[u] = nr[u]; }
+        const float mean = n_mean, rstd = n_rstd;
+        if (AHEAD && row + row_step < rows) request(row + row_step);
         float c12[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -273,7 +301,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
                 const float xh = (s[i] - mean) * rstd;
                 r[i] = fmaf(rstd, fmaf(-xh, c2, fmaf(y[i], gm[i], -c1)), r[i]);
             }
-            store_row_piece<ET, TAIL>(dX + base + (c + u * TPR) * N, Piece<ET>::pack(r), n[u]);
+            store_row_piece<ET, TAIL, NT>(dX + base + (c + u * TPR) * N, Piece<ET>::pack(r), n[u]);
         }
     }
     float* out = partial + (size_t)blockIdx.x * 2 * d;
@@ -312,6 +340,7 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_LINES) void norm_join_kernel(const
     const int col = blockIdx.x * JOIN_COLS + threadIdx.x % JOIN_COLS, line = threadIdx.x / JOIN_COLS;
     float s = 0.0f;
     if (col < 2 * d)
+#pragma unroll 8
         for (int b = line; b < blocks; b += JOIN_LINES) s += partial[(size_t)b * 2 * d + col];
     words[line][threadIdx.x % JOIN_COLS] = s;
     __syncthreads();
@@ -324,13 +353,17 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_LINES) void norm_join_kernel(const
 }
 
 // Threads of a row and pieces of each, by the width.  Forward: the fewest threads that hold it in four pieces, so that most rows need no
-// barrier and every thread has several requests on their way.  Backward, with the parameters' gradients in registers beside the row:
+// barrier and every thread has several requests on their way (32768 x 4096, 8192 x 4096, us, in 8 pieces of 64 threads 182, 48.6,
+// 4 of 128 192, 49.5, 2 of 256 184, 47.9, 1 of 512 182, 48.1).  Backward, with the parameters' gradients in registers beside the row:
 // two pieces where the threads are there.
-template <typename ET, bool BWD, typename F> hipError_t by_width(int d, F f)
+template <typename ET, bool BWD, typename F> hipError_t by_width(int d, bool nt, F f)
 {
     const int nv = (d + Piece<ET>::N - 1) / Piece<ET>::N;
     const bool tail = d % Piece<ET>::N != 0;
-    auto with = [&](auto TPR, auto U) { return tail ? f(TPR, U, std::true_type{}) : f(TPR, U, std::false_type{}); };
+    auto with = [&](auto TPR, auto U) {
+        if (nt) return tail ? f(TPR, U, std::true_type{}, std::true_type{}) : f(TPR, U, std::false_type{}, std::true_type{});
+        return tail ? f(TPR, U, std::true_type{}, std::false_type{}) : f(TPR, U, std::false_type{}, std::false_type{});
+    };
 #define MOE_NORM_CASE(T, UU) if (nv <= T * UU) return with(std::integral_constant<int, T>{}, std::integral_constant<int, UU>{});
     MOE_NORM_CASE(16, 1)
     MOE_NORM_CASE(16, 2)
@@ -352,6 +385,11 @@ template <typename ET, bool BWD, typename F> hipError_t by_width(int d, F f)
     return hipErrorInvalidValue;                           // wider than NORM_MAX_D: the entry points refuse it
 }
 
+// Blocks of the backward pass.  Each leaves a partial sum of the parameters' gradients, 8 d bytes written and read again, and needs rows
+// enough to be worth it: four at least for each group of threads (rows x d bf16, us with 1 | 4 | 8: 4096 x 1024 13.9 | 12.0 | 14.6, 512 x 4096
+// 16.1 | 15.0 | 17.8).  Rows of two pieces a thread and more keep enough on their way with one block of 256 on a CU (32768 x 4096: 512 blocks 187, 256
+// 175), others do not (16384 x 2048: 52, 64).
+constexpr int MIN_ROWS = 4;
 inline int blocks_for(int rows, int tpr, int most)
 {
     const int rpb = threads_of(tpr) / tpr, n = (rows - 1) / rpb + 1;
@@ -362,9 +400,9 @@ template <typename ET>
 hipError_t norm_fwd(const moe_norm_t& c, const void* X, const void* R, const float* gamma, const float* beta, void* S, void* Y,
                     float* mean, float* rstd, hipStream_t st)
 {
-    return by_width<ET, false>(c.d, [&](auto TPR, auto U, auto TAIL) {
+    return by_width<ET, false>(c.d, streams((size_t)c.rows * c.d * sizeof(ET)), [&](auto TPR, auto U, auto TAIL, auto NT) {
         constexpr int tpr = decltype(TPR)::value;
-        hipLaunchKernelGGL((norm_fwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value>), dim3(blocks_for(c.rows, tpr, 1 << 20)), dim3(threads_of(tpr)), 0, st,
+        hipLaunchKernelGGL((norm_fwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value, decltype(NT)::value>), dim3(blocks_for(c.rows, tpr, 1 << 20)), dim3(threads_of(tpr)), 0, st,
                            (const ET*)X, (const ET*)R, gamma, beta, (ET*)S, (ET*)Y, mean, rstd, c.rows, c.d, c.eps);
         return hipGetLastError();
     });
@@ -375,10 +413,11 @@ hipError_t norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const fl
                     void* dX, float* dgamma, float* dbeta, float* partial, hipStream_t st)
 {
     int blocks = 0;
-    hipError_t e = c.rows == 0 ? hipSuccess : by_width<ET, true>(c.d, [&](auto TPR, auto U, auto TAIL) {
+    hipError_t e = c.rows == 0 ? hipSuccess : by_width<ET, true>(c.d, streams((size_t)c.rows * c.d * sizeof(ET)), [&](auto TPR, auto U, auto TAIL, auto NT) {
         constexpr int tpr = decltype(TPR)::value;
-        blocks = blocks_for(c.rows, tpr, NORM_PARTIALS);
-        hipLaunchKernelGGL((norm_bwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value>), dim3(blocks), dim3(threads_of(tpr)), 0, st,
+        constexpr int wide = tpr >= 256 && decltype(U)::value >= 2;
+        blocks = blocks_for((c.rows + MIN_ROWS - 1) / MIN_ROWS, tpr, wide ? NORM_PARTIALS / 2 : NORM_PARTIALS);
+        hipLaunchKernelGGL((norm_bwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value, decltype(NT)::value>), dim3(blocks), dim3(threads_of(tpr)), 0, st,
                            (const ET*)dY, (const ET*)S, gamma, mean, rstd, (const ET*)dS, (ET*)dX, partial, c.rows, c.d);
         return hipGetLastError();
     });
