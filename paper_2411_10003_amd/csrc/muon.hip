@@ -298,6 +298,9 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WGN, wn = wave % WGN;
 
+    // what the first requests need, asked for at once: left to where it is used, it is read from memory in two steps, one after the other
+    asm volatile("" :: "s"(p.A[0]), "s"(p.B[0]), "s"(p.a_stride), "s"(p.b_stride), "s"(p.lda), "s"(p.ldb), "s"(p.n_seg), "s"(p.K), "s"(p.M), "s"(p.N),
+                 "s"(p.tiles), "s"(p.whole), "s"(p.whole_per_xcd), "s"(p.symmetric));
     // ---- which tile, and which part of it
     const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
     int item = xcd * p.whole_per_xcd + turn, part = 0, unit = 0;
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     auto part_begin = [&](int i) { return (int)((long)i * (p.n_seg * k_per_seg) / parts) & ~1; };     // parts begin at even slices
     const int k_lo = part_begin(part), k_cnt = (part + 1 == parts ? p.n_seg * k_per_seg : part_begin(part + 1)) - k_lo;    // an even number, at least two
     rsrc_t ra, rb;
-    int seg = k_lo / k_per_seg;
+    int seg = CUT ? k_lo / k_per_seg : 0;
     auto open_segment = [&]() {
         const f16* a = p.A[seg] + (size_t)matrix * p.a_stride;
         const f16* b = p.B[seg] + (size_t)matrix * p.b_stride;
@@ -396,10 +399,15 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         fpb[v] = A_BYTES + (halfpair_off((wn % (WGN / 2)) * WN + (lane & 15), lane >> 4) ^ (uint32_t)(v << 6));
     }
     f32x4 acc[FM][FN];
-    f16x8 fa[FM], fb[FN];
+    // AHEAD: four waves have the CU to themselves, and nobody's products to fill the time of a slice's fragment reads: they read those of the next
+    // slice into a second set of registers while they multiply.
+    constexpr bool AHEAD = GEO::BLOCKS == 1 && !GEO::TWO_PHASE;
+    f16x8 fa2[AHEAD ? 2 : 1][FM], fb2[AHEAD ? 2 : 1][FN];
     auto goes_out = [](int n) { return (n + 1) % ((FM + FN) / SLICE_OPS) == 0 ? (n + 1) / ((FM + FN) / SLICE_OPS) - 1 : -1; };
     auto load_frags = [&](uint32_t stA, uint32_t stB, auto PAR, auto after) {
         constexpr int par = decltype(PAR)::value;
+        f16x8 (&fa)[FM] = fa2[AHEAD ? par : 0];
+        f16x8 (&fb)[FN] = fb2[AHEAD ? par : 0];
         const uint32_t a = stA + fpa[par];
         auto frag_a = [&](auto I) { lds_frag_kcontig_at<decltype(I)::value * 2048>(fa[decltype(I)::value], a); after(decltype(I)::value); };
         frag_a(std::integral_constant<int, 0>{}); frag_a(std::integral_constant<int, 1>{});
@@ -418,7 +426,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
             frag_b(std::integral_constant<int, 2>{}); frag_b(std::integral_constant<int, 3>{});
         }
     };
-    auto mma_first = [&]() {                               // the first products take zero as their addend
+    auto mma_first = [&](const f16x8 (&fa)[FM], const f16x8 (&fb)[FN]) {       // the first products take zero as their addend
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -427,7 +435,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                 asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(fb[j]), "v"(fa[i]));
             }
     };
-    auto mma = [&]() {
+    auto mma = [&](const f16x8 (&fa)[FM], const f16x8 (&fb)[FN]) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -456,43 +464,65 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     int cur = 0, pair0 = 0;                                // ring slots of the slice's own group, of the even group of its pair
     const int hA = wm, hB = wn / (WGN / 2);                // which group of a pair holds this wave's rows of A and of B
     auto slot_base = [&](int slot) { return lds0 + (uint32_t)(slot >= STAGES ? slot - STAGES : slot) * STAGE_BYTES; };
-    auto slice = [&](auto PAR, auto FIRST, const rsrc_t a, const rsrc_t b) {
-        constexpr int par = decltype(PAR)::value;
-        typedef std::integral_constant<int, 1 - par> other_t;
-        const uint32_t stA = slot_base(pair0 + hA), stB = B_COLS ? slot_base(cur) : slot_base(pair0 + hB);
-        const uint32_t to = lds0 + (uint32_t)iss_stage * STAGE_BYTES;
-        uint32_t oa, ob;
-        group_offsets(other_t{}, oa, ob);
-        load_frags(stA, stB, PAR, [&](int n) { if (goes_out(n) >= 0) { __builtin_amdgcn_sched_barrier(0); request_piece(goes_out(n), to, a, b, oa, ob); __builtin_amdgcn_sched_barrier(0); } });
-        group_done(other_t{});
-        WAIT_VMCNT((par ? L - 2 : L - 1) * SLICE_OPS);     // next: a pair's two groups, or the second one of a pair that has landed
+    auto wait_frags = [&]() {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);                 // no product moves above the wait
-        BLOCK_BARRIER();
-        __builtin_amdgcn_s_setprio(1);
-        if constexpr (decltype(FIRST)::value) mma_first(); else mma();
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (GEO::TWO_PHASE) BLOCK_BARRIER();
-        cur = (cur + 1 == STAGES) ? 0 : cur + 1;
-        if (par) pair0 = (pair0 + 2 >= STAGES) ? pair0 + 2 - STAGES : pair0 + 2;
     };
-    if (L < k_cnt) { slice(even_t{}, std::true_type{}, ra, rb); group_fixups(); }
-    else slice(even_t{}, std::true_type{}, rnull, rnull);
+    auto slice = [&](auto PAR, auto FIRST, auto LAST, const rsrc_t a, const rsrc_t b) {
+        constexpr int par = decltype(PAR)::value;
+        typedef std::integral_constant<int, 1 - par> other_t;
+        const uint32_t to = lds0 + (uint32_t)iss_stage * STAGE_BYTES;
+        uint32_t oa, ob;
+        group_offsets(other_t{}, oa, ob);
+        auto request_between = [&](int n) { if (goes_out(n) >= 0) { __builtin_amdgcn_sched_barrier(0); request_piece(goes_out(n), to, a, b, oa, ob); __builtin_amdgcn_sched_barrier(0); } };
+        if constexpr (AHEAD) {
+            // the next slice's groups, of the L - 1 + t that are on their way
+            WAIT_VMCNT((par ? L - 3 : L - 2) * SLICE_OPS);
+            BLOCK_BARRIER();
+            cur = (cur + 1 == STAGES) ? 0 : cur + 1;
+            if (par) pair0 = (pair0 + 2 >= STAGES) ? pair0 + 2 - STAGES : pair0 + 2;
+            if constexpr (!decltype(LAST)::value) load_frags(slot_base(pair0 + hA), B_COLS ? slot_base(cur) : slot_base(pair0 + hB), other_t{}, request_between);
+            group_done(other_t{});
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(FIRST)::value) mma_first(fa2[par], fb2[par]); else mma(fa2[par], fb2[par]);
+            wait_frags();
+        } else {
+            load_frags(slot_base(pair0 + hA), B_COLS ? slot_base(cur) : slot_base(pair0 + hB), PAR, request_between);
+            group_done(other_t{});
+            WAIT_VMCNT((par ? L - 2 : L - 1) * SLICE_OPS);                 // next: a pair's two groups, or the second one of a pair that has landed
+            wait_frags();
+            BLOCK_BARRIER();
+            __builtin_amdgcn_s_setprio(1);
+            if constexpr (decltype(FIRST)::value) mma_first(fa2[0], fb2[0]); else mma(fa2[0], fb2[0]);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (GEO::TWO_PHASE) BLOCK_BARRIER();
+            cur = (cur + 1 == STAGES) ? 0 : cur + 1;
+            if (par) pair0 = (pair0 + 2 >= STAGES) ? pair0 + 2 - STAGES : pair0 + 2;
+        }
+    };
+    if constexpr (AHEAD) {                                 // the first slice's fragments
+        load_frags(slot_base(hA), B_COLS ? slot_base(0) : slot_base(hB), even_t{}, [](int) {});
+        wait_frags();
+    }
+    typedef std::true_type yes_t;
+    typedef std::false_type no_t;
+    if (L < k_cnt) { slice(even_t{}, yes_t{}, no_t{}, ra, rb); group_fixups(); }
+    else slice(even_t{}, yes_t{}, no_t{}, rnull, rnull);
     int s = 1;
     while (s < k_cnt - 1) {
         const bool more = s + L < k_cnt;                   // the pair of slices s + L, s + L + 1 exists
         const int n = more ? min((k_cnt - L - s + 1) / 2, (k_per_seg - iss_in_seg) / 2) : (k_cnt - 1 - s) / 2;
         const rsrc_t a = more ? ra : rnull, b = more ? rb : rnull;
         for (int i = 0; i < n; ++i) {
-            slice(odd_t{}, std::false_type{}, a, b);
-            slice(even_t{}, std::false_type{}, a, b);
+            slice(odd_t{}, no_t{}, no_t{}, a, b);
+            slice(even_t{}, no_t{}, no_t{}, a, b);
         }
         s += 2 * n;
         if (more) group_fixups();
     }
-    slice(odd_t{}, std::false_type{}, rnull, rnull);       // the last one
+    slice(odd_t{}, no_t{}, yes_t{}, rnull, rnull);         // the last one
     WAIT_VMCNT(0);                                         // the empty requests too: the epilogue reuses the ring
     if (GEO::TWO_PHASE && wm == 0) BLOCK_BARRIER();        // both rows have passed the same number of barriers
     BLOCK_BARRIER();
