@@ -101,6 +101,55 @@ def test_number_of_steps(steps, dtype):
         _check(dtype, grads[i], M0[i], W0[i], momenta[i], weights[i], steps=steps, lr=0.1, wd=0.0, scale=2.0)
 
 
+@pytest.mark.parametrize("rows,cols,count,transposed,dtype", [
+    (1024, 1088, 20, (False,), "bf16"),                    # squares in 256 x 256 tiles, with tiles left over after a full round
+    (1100, 2112, 9, (False, True), "bf16"),                # the same, sides off the tiles, both orientations
+    (1100, 1500, 10, (True,), "f32"),                      # in two numbers
+    (576, 4032, 3, (False, True), "bf16"),                 # few tiles, a long contraction in parts
+    (320, 3840, 2, (True,), "f32"),                        # parts that begin in the middle of a segment
+    (640, 704, 40, (False,), "bf16"),                      # 128 x 128 tiles, two to a CU
+    (640, 704, 20, (False, True), "f32"),
+    (2048, 2560, 4, (False,), "bf16"),
+    (128, 256, 300, (False,), "bf16"),                     # more small matrices than the chip has places
+    (64, 448, 3, (True,), "f32"), (64, 512, 3, (False,), "bf16"), (64, 449, 3, (False,), "f32"), (64, 513, 3, (True,), "bf16"), (65, 256, 2, (False,), "bf16"),
+    (128, 257, 2, (True,), "bf16"),                        # what a block takes whole, and one more
+    (512, 65536, 1, (False,), "bf16"), (1, 65536, 2, (True,), "f32"), (2, 40000, 1, (False,), "bf16"),
+])
+def test_layouts(rows, cols, count, transposed, dtype):
+    """The ways a product is laid out: every tile size, tiles cut along the contraction, whole matrices in a block; sums of a step that do not depend
+    on which part of a tile is done last."""
+    grads, momenta, weights = _case(rows, cols, count, dtype, transposed)
+    M0, W0 = [m.clone() for m in momenta], [w.clone() for w in weights]
+    mu = binding.Muon(count=count, rows=rows, cols=cols, dtype=dtype, transposed=transposed, device=G.DEV)
+    mu.ws.fill_(0xff)
+    lr, wd, scale = 0.02, 0.1, math.sqrt(max(rows, cols)) * 0.2
+    mu.step(grads, momenta, weights, lr=lr, weight_decay=wd, scale=scale)
+    for i in range(len(transposed)):
+        _check(dtype, grads[i], M0[i], W0[i], momenta[i], weights[i], lr=lr, wd=wd, scale=scale)
+    for _ in range(2):
+        m, w = [x.clone() for x in M0], [x.clone() for x in W0]
+        mu.step(grads, m, w, lr=lr, weight_decay=wd, scale=scale)
+        assert all(torch.equal(x, y) for x, y in zip(m + w, momenta + weights))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_matrices_do_not_meet(dtype):
+    """A batch gives each matrix what it gets alone, in the same layout of tiles or another: within the tolerance of the type, and none is left out."""
+    rows, cols, count = 200, 712, 23
+    grads, momenta, weights = _case(rows, cols, count, dtype, (False, True))
+    M0, W0 = [m.clone() for m in momenta], [w.clone() for w in weights]
+    mu = binding.Muon(count=count, rows=rows, cols=cols, dtype=dtype, transposed=(False, True), device=G.DEV)
+    mu.step(grads, momenta, weights, lr=0.1, scale=2.0)
+    alone = binding.Muon(count=1, rows=rows, cols=cols, dtype=dtype, transposed=(False,), device=G.DEV)
+    for i in (0, 11, 22):
+        m, w = [M0[0][i].clone()], [W0[0][i].clone()]
+        alone.step([grads[0][i]], m, w, lr=0.1, scale=2.0)
+        assert torch.equal(m[0], momenta[0][i])
+        d = (w[0].double() - weights[0][i].double()).norm() / (W0[0][i].double() - weights[0][i].double()).norm()
+        # two results of the same inputs: twice the tolerance, and twice the rounding of the weights against the size of the update
+        assert d <= 2 * TOL[dtype] + 2 * torch.finfo(TYPES[dtype]).eps * float(W0[0][i].double().norm() / (W0[0][i].double() - weights[0][i].double()).norm())
+
+
 def test_other_coefficients():
     """A cubic that converges (c = 0), and the momentum off."""
     coef = (1.5, -0.5, 0.0)
