@@ -289,6 +289,8 @@ template <> struct WeightOps<float> {
 // Where a CU gets one tile of 128 x 128 at most it has all of LDS for it, and what the loop waits for is the way of a request: seven slices
 // ahead instead of three.
 typedef Geometry<2, 2, 2, 2, 9, 1> Deep;
+// 64 x 64, four waves of 32 x 32, two blocks on a CU: twice the bytes a product, where there are not tiles enough for the chip.
+typedef Geometry<2, 2, 1, 1, 9, 2> Fine;
 
 // ADD: there is an addend (and a diagonal); PLANES: numbers an operand is kept in; CUT: some of the tiles are.  Everything past the loop runs once per tile, from code that is
 // not in the instruction cache: what a product does not need is not in its kernel.
@@ -402,9 +404,9 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
     };
 
     // ---- fragment addresses inside a ring buffer
-    uint32_t fk_addr[4], fpa[2], fpb[2];
+    uint32_t fk_addr[FN], fpa[2], fpb[2];                  // chunks of 16 columns: the wave's own of a line of 64
 #pragma unroll
-    for (int c = 0; c < 4; ++c) fk_addr[c] = kmajor_off<BN>(8 * (lane >> 4) + ((lane & 15) >> 2), c * 16 + 4 * (lane & 3));
+    for (int c = 0; c < FN; ++c) fk_addr[c] = kmajor_off<BN>(8 * (lane >> 4) + ((lane & 15) >> 2), wn * WN + c * 16 + 4 * (lane & 3));
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
         fpa[v] = halfpair_off(lane & 15, lane >> 4) ^ (uint32_t)(v << 6);
@@ -423,19 +425,19 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         const uint32_t a = stA + fpa[par];
         auto frag_a = [&](auto I) { lds_frag_kcontig_at<decltype(I)::value * 2048>(fa[decltype(I)::value], a); after(decltype(I)::value); };
         frag_a(std::integral_constant<int, 0>{}); frag_a(std::integral_constant<int, 1>{});
-        frag_a(std::integral_constant<int, 2>{}); frag_a(std::integral_constant<int, 3>{});
+        if constexpr (FM >= 4) { frag_a(std::integral_constant<int, 2>{}); frag_a(std::integral_constant<int, 3>{}); }
         if constexpr (FM == 8) {
             frag_a(std::integral_constant<int, 4>{}); frag_a(std::integral_constant<int, 5>{});
             frag_a(std::integral_constant<int, 6>{}); frag_a(std::integral_constant<int, 7>{});
         }
         if constexpr (B_COLS) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) { lds_frag_kmajor_at<BN * 8, 0>(fb[j], stB + A_BYTES + wn * 256 + fk_addr[j]); after(FM + j); }
+            for (int j = 0; j < FN; ++j) { lds_frag_kmajor_at<BN * 8, 0>(fb[j], stB + A_BYTES + fk_addr[j]); after(FM + j); }
         } else {
             const uint32_t b = stB + fpb[par];
             auto frag_b = [&](auto J) { lds_frag_kcontig_at<decltype(J)::value * 2048>(fb[decltype(J)::value], b); after(FM + decltype(J)::value); };
             frag_b(std::integral_constant<int, 0>{}); frag_b(std::integral_constant<int, 1>{});
-            frag_b(std::integral_constant<int, 2>{}); frag_b(std::integral_constant<int, 3>{});
+            if constexpr (FN == 4) { frag_b(std::integral_constant<int, 2>{}); frag_b(std::integral_constant<int, 3>{}); }
         }
     };
     auto mma_first = [&](const f16x8 (&fa)[FM], const f16x8 (&fb)[FN]) {       // the first products take zero as their addend
@@ -575,19 +577,23 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         if (tid == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
 
-    // ---- epilogue: 64 x 64 results at a time through a patch of LDS of the wave's own, so that memory sees whole lines along the rows
+    // ---- epilogue: 64 x 64 results at a time through a patch of LDS, the wave's own or, of four waves of 32 x 32, the block's, so that memory sees whole lines along the rows
     // and, where the result is wanted the other way round too, along the columns.
     // Its rows are 16 slots of 4 numbers, permuted by the row so that neither the writes (16 rows of a slot), nor the reads along a row, nor
     // those along a column (8 columns of rows 8 apart) meet in a bank.
     // Slot c4 of row r lies at r * 256 + 16 (c4 ^ (r & 15) ^ ((r >> 3) & 6)); below, as a part of the lane's own, combined with a constant.
     constexpr int PATCH = 64 * 256;
-    static_assert(WN == 64 && WM % 64 == 0 && NWAVES * PATCH <= (int)GEO::LDS_BYTES, "patches inside the ring");
-    unsigned char* patch = smem + wave * PATCH;
+    constexpr bool SHARED = WN == 32;
+    constexpr int OF64 = SHARED ? 1 : WM / 64, FRAG_ROWS = SHARED ? 2 : 4, PASSES = SHARED ? 2 : 8;    // blocks of 64, rows of fragments in one, passes of the wave
+    static_assert((SHARED ? WM == 32 && NWAVES == 4 : WN == 64 && WM % 64 == 0) && NWAVES * PATCH <= (int)GEO::LDS_BYTES, "patches inside the ring");
+    unsigned char* patch = smem + (SHARED ? 0 : wave * PATCH);
+    const int pass0 = SHARED ? 2 * wave : 0;
     const int r8 = lane >> 3, c8 = (lane & 7) * 8;         // row of eight that a pass takes, first of its eight columns
-    const int put_at = (lane & 15) * 256, put_slot = (lane >> 4) ^ (lane & 15);                                // row i 16 + lane % 16, slot j 4 + lane / 16
+    const int put_at = (lane & 15) * 256 + (SHARED ? wm * 32 * 256 : 0);
+    const int put_slot = (lane >> 4) ^ (lane & 15) ^ (SHARED ? wn * 8 ^ wm * 4 : 0);                                // row i 16 + lane % 16, slot j 4 + lane / 16
     const int row_at = r8 * 256, row_slot = (c8 / 4) ^ r8;                                                     // row pass 8 + r8, from column c8
     const int col_at = c8 * 256 + (r8 & 3) * 4, col_slot = (r8 >> 2) ^ (c8 & 8) ^ ((c8 >> 3) & 6);             // column pass 8 + r8, from row c8
-    const int col0 = n0 + wn * WN;
+    const int col0 = n0 + (SHARED ? 0 : wn * WN);
     const int tensor = OUT == UPDATE ? matrix / p.count : 0;
     const bool tall = OUT == UPDATE && p.transposed[tensor] != 0;
     WT* W = nullptr;
@@ -599,22 +605,22 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         if (p.version && t == 0 && tensor == 0 && tid == 0) p.version[matrix] += 1;
     }
 #pragma unroll
-    for (int block = 0; block < WM / 64; ++block) {
-        const int row0 = m0 + wm * WM + block * 64;
+    for (int block = 0; block < OF64; ++block) {
+        const int row0 = m0 + (SHARED ? 0 : wm * WM + block * 64);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_wave_barrier();
         // rows of fragments at a time: all loads of a part are on their way before the first is added, as far as there are registers for them
-        constexpr int ROWS_AT_ONCE = GEO::BLOCKS == 1 ? 2 : 4;
+        constexpr int ROWS_AT_ONCE = GEO::NWAVES == 8 || SHARED ? 2 : 4;
 #pragma unroll
-        for (int i0 = 0; i0 < 4; i0 += ROWS_AT_ONCE) {
+        for (int i0 = 0; i0 < FRAG_ROWS; i0 += ROWS_AT_ONCE) {
             f32x4 val[ROWS_AT_ONCE][FN];
             if constexpr (!CUT) {
 #pragma unroll
                 for (int i = 0; i < ROWS_AT_ONCE; ++i)
 #pragma unroll
                     for (int j = 0; j < FN; ++j) {
-                        asm volatile("" : "+a"(acc[block * 4 + i0 + i][j]));
-                        val[i][j] = acc[block * 4 + i0 + i][j];
+                        asm volatile("" : "+a"(acc[block * FRAG_ROWS + i0 + i][j]));
+                        val[i][j] = acc[block * FRAG_ROWS + i0 + i][j];
                     }
             } else {
 #pragma unroll
@@ -630,7 +636,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                     for (int i = 0; i < ROWS_AT_ONCE; ++i)
 #pragma unroll
                         for (int j = 0; j < FN; ++j)
-                            x[i][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, part_ofs + ((block * 4 + i0 + i) * FN + j) * 1024, 0, AT_DEVICE));
+                            x[i][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, part_ofs + ((block * FRAG_ROWS + i0 + i) * FN + j) * 1024, 0, AT_DEVICE));
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < ROWS_AT_ONCE; ++i)
@@ -643,8 +649,8 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
             for (int i = 0; i < ROWS_AT_ONCE; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
-                    asm volatile("" : "+a"(acc[block * 4 + i0 + i][j]));   // they stay where they are until here: read earlier, all at once, they would not fit
-                    val[i][j] += acc[block * 4 + i0 + i][j];
+                    asm volatile("" : "+a"(acc[block * FRAG_ROWS + i0 + i][j]));   // they stay where they are until here: read earlier, all at once, they would not fit
+                    val[i][j] += acc[block * FRAG_ROWS + i0 + i][j];
                 }
             add_parts(part + 1, parts);
             }
@@ -655,7 +661,8 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                     *reinterpret_cast<float4*>(patch + put_at + (i0 + i) * 4096 + ((put_slot ^ (j * 4) ^ ((i0 + i) * 2)) << 4)) = make_float4(val[i][j][0], val[i][j][1], val[i][j][2], val[i][j][3]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
+        if constexpr (SHARED) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
         if (row0 >= p.M || col0 >= p.N) continue;          // sides are multiples of 64: all of it or none
         auto row_of = [&](int pass, float* v) {            // eight columns of a row of the block
             const int k = ((pass & 1) << 3) ^ (pass & 6);
@@ -669,15 +676,15 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         if constexpr (OUT == STORE) {
             // Along the rows, and off the diagonal of a symmetric product along the columns too: the addend is symmetric as well and
             // is read where the result goes.  What memory and LDS give is requested for several passes before the first is used.
-            constexpr int BATCH = GEO::NWAVES == 8 ? 2 : 8;
+            constexpr int BATCH = GEO::NWAVES == 8 || SHARED ? 2 : 8;
             const bool diagonal = row0 == col0;
             auto put = [&](auto COLUMNS) {
                 constexpr bool columns = decltype(COLUMNS)::value;
-                const size_t o = (size_t)matrix * p.o_stride + (size_t)((columns ? col0 : row0) + r8) * p.ldo + (columns ? row0 : col0) + c8;
+                const size_t o = (size_t)matrix * p.o_stride + (size_t)((columns ? col0 : row0) + r8) * p.ldo + (columns ? row0 : col0) + c8 + (size_t)pass0 * 8 * p.ldo;
                 const size_t pass_step = (size_t)8 * p.ldo;
 #pragma unroll
-                for (int b = 0; b < 8; b += BATCH) {
-                    if (BATCH < 8) __builtin_amdgcn_sched_barrier(0);      // no more than a batch in the registers beside the accumulators
+                for (int b = 0; b < PASSES; b += BATCH) {
+                    if (BATCH < PASSES) __builtin_amdgcn_sched_barrier(0);      // no more than a batch in the registers beside the accumulators
                     u32x4 d[ADD ? PLANES : 1][BATCH];
                     float v[BATCH][8];
                     if constexpr (ADD)
@@ -688,8 +695,8 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                         }
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        if constexpr (columns) column_of(b + i, v[i]);
-                        else row_of(b + i, v[i]);
+                        if constexpr (columns) column_of(pass0 + b + i, v[i]);
+                        else row_of(pass0 + b + i, v[i]);
                     }
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
@@ -704,7 +711,7 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
                                 for (int e = 0; e < 8; ++e) v[i][e] = fmaf(p.beta, x[e], v[i][e]);
                             }
                             if (!columns && diagonal) {
-                                const float here = (lane & 7) == b + i ? p.diag : 0.0f;
+                                const float here = (lane & 7) == pass0 + b + i ? p.diag : 0.0f;
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) v[i][e] += r8 == e ? here : 0.0f;
                             }
@@ -720,17 +727,17 @@ __global__ __launch_bounds__(GEO::THREADS, GEO::BLOCKS * GEO::NWAVES / 4) void p
         } else {
             // along the rows of the weights, which are columns of the block where they lie on their short side
             typedef WeightOps<WT> Ops;
-            const int wr = (tall ? col0 : row0) + r8, wc = (tall ? row0 : col0) + c8, w_rows = tall ? p.n : p.m, w_cols = tall ? p.m : p.n;
+            const int wr = (tall ? col0 : row0) + r8 + pass0 * 8, wc = (tall ? row0 : col0) + c8, w_rows = tall ? p.n : p.m, w_cols = tall ? p.m : p.n;
             const int there = w_cols - wc;
-            typename Ops::raw_t raw[8];
+            typename Ops::raw_t raw[PASSES];
             if (there >= 8)
 #pragma unroll
-                for (int pass = 0; pass < 8; ++pass)
+                for (int pass = 0; pass < PASSES; ++pass)
                     if (wr + 8 * pass < w_rows) raw[pass] = Ops::load8(W + (size_t)(wr + 8 * pass) * w_cols + wc);
 #pragma unroll
-            for (int pass = 0; pass < 8; ++pass) {
+            for (int pass = 0; pass < PASSES; ++pass) {
                 float x[8], w[8];
-                if (tall) column_of(pass, x); else row_of(pass, x);
+                if (tall) column_of(pass0 + pass, x); else row_of(pass0 + pass, x);
                 if (wr + 8 * pass >= w_rows) continue;
                 const size_t at = (size_t)(wr + 8 * pass) * w_cols + wc;
                 if (there >= 8) {
@@ -1057,9 +1064,11 @@ template <int PLANES, int MT, typename WT> hipError_t launch_few(const Few& f, i
 // further one).  128 x 128 tiles are bound by what L2 delivers to a CU, 29 bytes a clock, whether one or two share it: what more parts
 // gain is CUs, not overlap.  Measured, us: squares of m = 4096 (six; 816 tiles of 256, 128 slices) 413 whole, 370 with the last 48 in five parts; X X^T
 // of 4 x 1024 x 4096 (144 tiles of 128, 128 slices) 38 whole, 33 in three parts, of 6 x 500 x 1333 in two numbers (60 tiles, 126 slices) 42 and 25
-// in four; its squares (48 slices) 17.8 whole, 18.8 in three.
+// in four; its squares (48 slices) 17.8 whole, 18.8 in three.  64 x 64 tiles where those of 128 do not fill the CUs, the whole call, us: two numbers, 6 x
+// 1333 x 500 374 -> 272, 16 x 200 x 300 233 -> 153; bf16, 8 x 256 x 1024 149 -> 108, 6 x 384 x 768 167 -> 121; 4 x 1024 x 4096, whose squares are 144
+// tiles of 128, 387 either way.
 struct GeometryTime { float slice, over, join; int least; };           // least: slices of a part
-constexpr GeometryTime LARGE_TIME{0.70f, 11.0f, 12.0f, 24}, SMALL_TIME{0.50f, 6.0f, 5.0f, 16}, DEEP_TIME{0.245f, 6.0f, 8.0f, 16};
+constexpr GeometryTime LARGE_TIME{0.70f, 11.0f, 12.0f, 24}, SMALL_TIME{0.50f, 6.0f, 5.0f, 16}, DEEP_TIME{0.245f, 6.0f, 8.0f, 16}, FINE_TIME{0.20f, 5.0f, 5.0f, 16};
 constexpr int MAX_PARTS = 8;
 struct Layout { float us; int whole, cut, parts; };
 template <class GEO> Layout layout_of(const GeometryTime& g, int tiles, int slices, int cus)
@@ -1112,6 +1121,10 @@ template <int KIND, int OUT, bool ADD, int PLANES, typename WT> hipError_t launc
 {
     const int slices = p.n_seg * (p.K / BK), tiles = tiles_of<Small>(p, matrices);
     const Layout l = layout_of<Large>(LARGE_TIME, tiles_of<Large>(p, matrices), slices, cus), m = layout_of<Small>(SMALL_TIME, tiles, slices, cus);
+    if (tiles <= cus) {
+        const Layout f = layout_of<Fine>(FINE_TIME, tiles_of<Fine>(p, matrices), slices, cus), d = layout_of<Deep>(DEEP_TIME, tiles, slices, cus);
+        if (f.us < d.us && f.us < l.us && f.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Fine>(p, f, st);
+    }
     if (tiles <= cus) {
         const Layout d = layout_of<Deep>(DEEP_TIME, tiles, slices, cus);
         if (d.us < l.us && d.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Deep>(p, d, st);

@@ -205,11 +205,11 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
 }
 
 // Columns stay with their thread from row to row, so the parameters' gradients are summed in registers; a block leaves one partial
-// sum of each in `partial`, [block][2][d].
+// sum of each in `partial`, [block][2][d]; a block that is alone (partial null) the gradients themselves.
 template <typename ET, int TPR, int U, bool TAIL, bool NT>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
     const ET* dY, const ET* __restrict__ S, const float* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-    const ET* dS, ET* dX, float* __restrict__ partial, int rows, int d)
+    const ET* dS, ET* dX, float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, int rows, int d)
 {
     constexpr int N = Piece<ET>::N, RPB = threads_of(TPR) / TPR, COLS = TPR * U * N;
     __shared__ float words[TPR > 64 ? 4 * (TPR / 64) : 1];
@@ -304,9 +304,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
             store_row_piece<ET, TAIL, NT>(dX + base + (c + u * TPR) * N, Piece<ET>::pack(r), n[u]);
         }
     }
-    float* out = partial + (size_t)blockIdx.x * 2 * d;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
+        float* out = partial ? partial + ((size_t)blockIdx.x * 2 + k) * d : (k ? dbeta : dgamma);
+        if (!out) continue;                                // no bias
         if constexpr (RPB > 1) {
             __syncthreads();                               // the rows of a block are joined in LDS
 #pragma unroll
@@ -319,14 +320,14 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
 #pragma unroll
                 for (int b = 0; b < RPB; ++b) s += join[b * COLS + j];
                 const int col = (j % (TPR * U)) * N + j / (TPR * U);
-                if (col < d) out[(size_t)k * d + col] = s;
+                if (col < d) out[col] = s;
             }
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (i < n[u]) out[(size_t)k * d + (c + u * TPR) * N + i] = k ? sb[u][i] : sg[u][i];
+                    if (i < n[u]) out[(c + u * TPR) * N + i] = k ? sb[u][i] : sg[u][i];
         }
     }
 }
@@ -418,10 +419,10 @@ hipError_t norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const fl
         constexpr int wide = tpr >= 256 && decltype(U)::value >= 2;
         blocks = blocks_for((c.rows + MIN_ROWS - 1) / MIN_ROWS, tpr, wide ? NORM_PARTIALS / 2 : NORM_PARTIALS);
         hipLaunchKernelGGL((norm_bwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value, decltype(NT)::value>), dim3(blocks), dim3(threads_of(tpr)), 0, st,
-                           (const ET*)dY, (const ET*)S, gamma, mean, rstd, (const ET*)dS, (ET*)dX, partial, c.rows, c.d);
+                           (const ET*)dY, (const ET*)S, gamma, mean, rstd, (const ET*)dS, (ET*)dX, blocks > 1 ? partial : nullptr, dgamma, dbeta, c.rows, c.d);
         return hipGetLastError();
     });
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || blocks == 1) return e;
     hipLaunchKernelGGL(norm_join_kernel, dim3((2 * c.d + JOIN_COLS - 1) / JOIN_COLS), dim3(JOIN_COLS * JOIN_LINES), 0, st, partial, blocks, c.d, dgamma, dbeta);
     return hipGetLastError();
 }
