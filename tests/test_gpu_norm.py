@@ -232,6 +232,32 @@ def test_no_rows():
     assert not dg.any() and not db.any()
 
 
+@pytest.mark.parametrize("rows,d", [(700, 256), (9, 1021)])
+def test_captured(rows, d):
+    """Forward and backward in one graph, replayed on new inputs among eager calls: each replay what the eager calls give."""
+    i = _inputs(rows, d, "bf16")
+    n = binding.Norm(d=d, dtype="bf16", device=G.DEV)
+    new = lambda: torch.empty(rows, d, dtype=torch.bfloat16, device=G.DEV)  # noqa: E731
+    outs = [dict(S=new(), Y=new(), dX=new(), mean=torch.empty(rows, device=G.DEV), rstd=torch.empty(rows, device=G.DEV), dg=torch.empty(d, device=G.DEV),
+                 db=torch.empty(d, device=G.DEV)) for _ in range(2)]
+
+    def both(o):
+        n.fwd(i["X"], i["gamma"], i["beta"], o["Y"], residual=i["R"], total=o["S"], mean=o["mean"], rstd=o["rstd"])
+        n.bwd(i["dY"], o["S"], i["gamma"], o["mean"], o["rstd"], o["dX"], o["dg"], o["db"], residual_grad=i["dS"])
+
+    both(outs[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(outs[0])
+    for k in range(4):
+        for name, t in _inputs(rows, d, "bf16", seed=k + 1).items():
+            i[name].copy_(t)
+        graph.replay()
+        both(outs[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[0][m], outs[1][m]) for m in outs[0]), k
+
+
 def test_offsets_past_32_bits():
     """More than 2^32 bytes of rows: the last ones against the formulas."""
     d, rows = 4096, 540000
