@@ -45,55 +45,80 @@ template <> struct Piece<bf16_t> {
     }
 };
 
-// `n`: elements of this piece inside the row; only with TAIL is it ever less than a whole piece.
+// TAIL: a row's last piece is short, `n` of its N elements are inside the row (elsewhere n = N, or 0 and less where a thread has no piece).
+//   1  It is requested as the row's last N elements, those of the piece before it among them, and moved down when it is used (settle): nothing is
+//      waited for where the request is made, which is a row ahead in the backward pass (the gradient of 20000 x 2500 in bf16 110 us, of 20000 x 2496 91).
+//   2  Element by element: rows shorter than a piece, and the forward pass, which waits for its row at once (59811 x 2244 230 us, moved down 250;
+//      20000 x 5001 192, 235; the gradient of 20000 x 2500 291).
 // NT: past the caches (STREAM_BYTES).
-template <typename ET, bool TAIL, bool NT> __device__ __forceinline__ moe_piece_t load_row_piece(const ET* p, int n)
+template <typename ET, int TAIL, bool NT> __device__ __forceinline__ moe_piece_t load_row_piece(const ET* row, int col, int n, int d)
 {
     typedef typename Piece<ET>::mem_t mem_t;
-    if (!TAIL || n == Piece<ET>::N) {
-        if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const mem_t*>(p));
-        else return *reinterpret_cast<const mem_t*>(p);
-    }
-    float f[Piece<ET>::N];
+    constexpr int N = Piece<ET>::N;
+    if (TAIL == 2 && n < N) {
+        float f[N];
 #pragma unroll
-    for (int i = 0; i < Piece<ET>::N; ++i) {
-        if constexpr (std::is_same<ET, float>::value) f[i] = i < n ? p[i] : 0.0f;
-        else f[i] = i < n ? bf16_to_f32(p[i]) : 0.0f;
+        for (int i = 0; i < N; ++i) {
+            if constexpr (std::is_same<ET, float>::value) f[i] = i < n ? row[col + i] : 0.0f;
+            else f[i] = i < n ? bf16_to_f32(row[col + i]) : 0.0f;
+        }
+        return Piece<ET>::pack(f);
     }
-    return Piece<ET>::pack(f);
+    const mem_t* p = reinterpret_cast<const mem_t*>(row + (TAIL == 1 && n < N ? d - N : col));
+    if constexpr (NT) return __builtin_nontemporal_load(p);
+    else return *p;
 }
-template <typename ET, bool TAIL, bool NT> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
+template <typename ET, int TAIL> __device__ __forceinline__ void settle(moe_piece_t& v, int n, int d)
+{
+    constexpr int N = Piece<ET>::N;
+    if (TAIL != 1 || n >= N || n <= 0) return;
+    int bits = (N - n) * (int)sizeof(ET) * 8;              // zeros come in at the end
+    uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    if (bits >= 64) { lo = hi; hi = 0; bits -= 64; }
+    if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+    v = moe_piece_t{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+template <typename ET, int TAIL, bool NT> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
 {
     typedef typename Piece<ET>::mem_t mem_t;
-    if (!TAIL || n == Piece<ET>::N) {
+    constexpr int N = Piece<ET>::N;
+    if (!TAIL || n == N) {
         if constexpr (NT) __builtin_nontemporal_store((mem_t)v, reinterpret_cast<mem_t*>(p));
         else *reinterpret_cast<mem_t*>(p) = v;
         return;
     }
-    float f[Piece<ET>::N];
-    Piece<ET>::unpack(v, f);
-#pragma unroll
-    for (int i = 0; i < Piece<ET>::N; ++i)
-        if (i < n) {
-            if constexpr (std::is_same<ET, float>::value) p[i] = f[i];
-            else p[i] = (bf16_t)(__float_as_uint(f[i]) >> 16);             // it is one already
-        }
+    typedef unsigned two_t __attribute__((ext_vector_type(2), aligned(2)));
+    typedef unsigned one_t __attribute__((aligned(2)));
+    const int words = n * (int)sizeof(ET) / 4;             // whole 32-bit words
+    if (words & 2) *reinterpret_cast<two_t*>(p) = two_t{v[0], v[1]};
+    if (words & 1) *reinterpret_cast<one_t*>(p + (words & 2) * 4 / sizeof(ET)) = words & 2 ? v[2] : v[0];
+    if constexpr (N == 8)
+        if (n & 1) p[n - 1] = (bf16_t)(words == 0 ? v[0] : words == 1 ? v[1] : words == 2 ? v[2] : v[3]);
 }
-// The parameters of a piece's columns.
-template <int N, bool TAIL> __device__ __forceinline__ void load_columns(const float* p, int n, float* f)
+// The parameters of a piece's columns; zeros past the row's end.
+template <int N, int TAIL> __device__ __forceinline__ void load_columns(const float* all, int col, int n, int d, float* f)
 {
     typedef float quad_t __attribute__((ext_vector_type(4), aligned(4)));
-    if (!TAIL || n == N) {
+    if (TAIL == 2 && n < N) {
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const quad_t q = *reinterpret_cast<const quad_t*>(p + 4 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f[4 * i + k] = q[k];
-        }
+        for (int i = 0; i < N; ++i) f[i] = i < n ? all[col + i] : 0.0f;
         return;
     }
+    const float* p = all + (TAIL == 1 && n < N ? d - N : col);
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = i < n ? p[i] : 0.0f;
+    for (int i = 0; i < N / 4; ++i) {
+        const quad_t q = *reinterpret_cast<const quad_t*>(p + 4 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[4 * i + k] = q[k];
+    }
+    if (TAIL == 1 && n < N) {
+        const int k = N - n;
+#pragma unroll
+        for (int step = N / 2; step >= 1; step /= 2)
+            if (k & step)
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[i] = i + step < N ? f[i + step] : 0.0f;
+    }
 }
 
 // Rows of a wave or less share a block of 256; the threads of a wider one are the block.
@@ -125,7 +150,7 @@ template <int TPR, int M> __device__ __forceinline__ void row_sums(float (&v)[M]
     }
 }
 
-template <typename ET, int TPR, int U, bool TAIL, bool NT>
+template <typename ET, int TPR, int U, int TAIL, bool NT>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
     const ET* X, const ET* R, const float* __restrict__ gamma, const float* __restrict__ beta, ET* S, ET* Y,
     float* __restrict__ mean_out, float* __restrict__ rstd_out, int rows, int d, float eps)
@@ -135,26 +160,29 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
     int turn = 0;
     const int c = threadIdx.x % TPR;
     const float inv_d = 1.0f / (float)d;
+    int n[U];                                              // elements of a piece inside the row
+#pragma unroll
+    for (int u = 0; u < U; ++u) n[u] = min(N, max(0, d - (c + u * TPR) * N));
     // rows of a block are a block apart from the next block's; the threads of a row leave the loop together
     for (long row = (long)blockIdx.x * RPB + threadIdx.x / TPR; row < rows; row += (long)gridDim.x * RPB) {
         const size_t base = (size_t)row * d;
         moe_piece_t x[U], r[U];
-        int n[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            n[u] = min(N, max(0, d - (c + u * TPR) * N));
             x[u] = moe_piece_t{0, 0, 0, 0};
-            if (n[u] > 0) x[u] = load_row_piece<ET, TAIL, NT>(X + base + (c + u * TPR) * N, n[u]);
+            if (n[u] > 0) x[u] = load_row_piece<ET, TAIL, NT>(X + base, (c + u * TPR) * N, n[u], d);
         }
         if (R) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 r[u] = moe_piece_t{0, 0, 0, 0};
-                if (n[u] > 0) r[u] = load_row_piece<ET, TAIL, NT>(R + base + (c + u * TPR) * N, n[u]);
+                if (n[u] > 0) r[u] = load_row_piece<ET, TAIL, NT>(R + base, (c + u * TPR) * N, n[u], d);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float a[N], b[N];
+                settle<ET, TAIL>(x[u], n[u], d);
+                settle<ET, TAIL>(r[u], n[u], d);
                 Piece<ET>::unpack(x[u], a);
                 Piece<ET>::unpack(r[u], b);
 #pragma unroll
@@ -163,6 +191,9 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
                 if (n[u] > 0) store_row_piece<ET, TAIL, NT>(S + base + (c + u * TPR) * N, x[u], n[u]);
             }
         }
+        if (!R)
+#pragma unroll
+            for (int u = 0; u < U; ++u) settle<ET, TAIL>(x[u], n[u], d);
         float sum[1] = {0.0f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -193,10 +224,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
             if (n[u] <= 0) continue;
             float a[N], g[N], b[N];
             Piece<ET>::unpack(x[u], a);
-            load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g);
+            load_columns<N, TAIL>(gamma, (c + u * TPR) * N, n[u], d, g);
 #pragma unroll
             for (int i = 0; i < N; ++i) b[i] = 0.0f;
-            if (beta) load_columns<N, TAIL>(beta + (c + u * TPR) * N, n[u], b);
+            if (beta) load_columns<N, TAIL>(beta, (c + u * TPR) * N, n[u], d, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) a[i] = fmaf((a[i] - mean) * rstd, g[i], b[i]);
             store_row_piece<ET, TAIL, NT>(Y + base + (c + u * TPR) * N, Piece<ET>::pack(a), n[u]);
@@ -206,7 +237,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_fwd_kernel(
 
 // Columns stay with their thread from row to row, so the parameters' gradients are summed in registers; a block leaves one partial
 // sum of each in `partial`, [block][2][d]; a block that is alone (partial null) the gradients themselves.
-template <typename ET, int TPR, int U, bool TAIL, bool NT>
+template <typename ET, int TPR, int U, int TAIL, bool NT>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
     const ET* dY, const ET* __restrict__ S, const float* __restrict__ gamma, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
     const ET* dS, ET* dX, float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta, int rows, int d)
@@ -222,14 +253,15 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
     float g[KEEP_GAMMA ? U : 1][N], sg[U][N], sb[U][N];
     int n[U];
 #pragma unroll
+    for (int u = 0; u < U; ++u) n[u] = min(N, max(0, d - (c + u * TPR) * N));
+#pragma unroll
     for (int u = 0; u < U; ++u) {
-        n[u] = min(N, max(0, d - (c + u * TPR) * N));
 #pragma unroll
         for (int i = 0; i < N; ++i) sg[u][i] = sb[u][i] = 0.0f;
         if constexpr (KEEP_GAMMA) {
 #pragma unroll
             for (int i = 0; i < N; ++i) g[u][i] = 0.0f;
-            if (n[u] > 0) load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g[u]);
+            if (n[u] > 0) load_columns<N, TAIL>(gamma, (c + u * TPR) * N, n[u], d, g[u]);
         }
     }
     auto columns = [&](int u) -> float (&)[N] {
@@ -238,7 +270,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) g[0][i] = 0.0f;
-            if (n[u] > 0) load_columns<N, TAIL>(gamma + (c + u * TPR) * N, n[u], g[0]);
+            if (n[u] > 0) load_columns<N, TAIL>(gamma, (c + u * TPR) * N, n[u], d, g[0]);
             return g[0];
         }
     };
@@ -251,9 +283,9 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
         for (int u = 0; u < U; ++u) {
             ny[u] = ns[u] = nr[u] = moe_piece_t{0, 0, 0, 0};
             if (n[u] > 0) {
-                ny[u] = load_row_piece<ET, TAIL, NT>(dY + base + (c + u * TPR) * N, n[u]);
-                ns[u] = load_row_piece<ET, TAIL, NT>(S + base + (c + u * TPR) * N, n[u]);
-                if (dS) nr[u] = load_row_piece<ET, TAIL, NT>(dS + base + (c + u * TPR) * N, n[u]);
+                ny[u] = load_row_piece<ET, TAIL, NT>(dY + base, (c + u * TPR) * N, n[u], d);
+                ns[u] = load_row_piece<ET, TAIL, NT>(S + base, (c + u * TPR) * N, n[u], d);
+                if (dS) nr[u] = load_row_piece<ET, TAIL, NT>(dS + base, (c + u * TPR) * N, n[u], d);
             }
         }
         n_mean = mean_in[row];
@@ -267,7 +299,12 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_bwd_kernel(
         moe_piece_t py[U], ps[U], pr[U];
         if (!AHEAD) request(row);
 #pragma unroll
-        for (int u = 0; u < U; ++u) { py[u] = ny[u]; ps[u] = ns[u]; pr[u] = nr[u]; }
+        for (int u = 0; u < U; ++u) {
+            py[u] = ny[u]; ps[u] = ns[u]; pr[u] = nr[u];
+            settle<ET, TAIL>(py[u], n[u], d);
+            settle<ET, TAIL>(ps[u], n[u], d);
+            settle<ET, TAIL>(pr[u], n[u], d);
+        }
         const float mean = n_mean, rstd = n_rstd;
         if (AHEAD && row + row_step < rows) request(row + row_step);
         float c12[2] = {0.0f, 0.0f};
@@ -353,31 +390,41 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_LINES) void norm_join_kernel(const
     else if (dbeta) dbeta[col - d] = t;
 }
 
-// Threads of a row and pieces of each, by the width.  Forward: the fewest threads that hold it in four pieces, so that most rows need no
-// barrier and every thread has several requests on their way (32768 x 4096, 8192 x 4096, us, in 8 pieces of 64 threads 182, 48.6,
-// 4 of 128 192, 49.5, 2 of 256 184, 47.9, 1 of 512 182, 48.1).  Backward, with the parameters' gradients in registers beside the row:
-// two pieces where the threads are there.
+// Threads of a row and pieces of each, by the width.  Forward: a wave up to eight pieces a thread, so that most rows need no barrier and every
+// thread has several requests on their way (59811 x 2240 in 5 pieces of 64 threads 178 us, 2 of 256 207; 32768 x 4096 in 8 of 64 184, 4 of 128 192, 2 of
+// 256 184).  Backward, with the parameters' gradients in registers beside the row: two pieces where the threads are there (a wave of one piece instead
+// of 16 threads of four: 16184 x 467 28 -> 18).
 template <typename ET, bool BWD, typename F> hipError_t by_width(int d, bool nt, F f)
 {
     const int nv = (d + Piece<ET>::N - 1) / Piece<ET>::N;
     const bool tail = d % Piece<ET>::N != 0;
+    typedef std::integral_constant<int, 0> whole_t;
+    typedef std::integral_constant<int, 2> short_t;
+    typedef std::integral_constant<int, BWD ? 1 : 2> tail_t;
+    if (d < Piece<ET>::N) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}, short_t{}, std::false_type{});
     auto with = [&](auto TPR, auto U) {
-        if (nt) return tail ? f(TPR, U, std::true_type{}, std::true_type{}) : f(TPR, U, std::false_type{}, std::true_type{});
-        return tail ? f(TPR, U, std::true_type{}, std::false_type{}) : f(TPR, U, std::false_type{}, std::false_type{});
+        if (nt) return tail ? f(TPR, U, tail_t{}, std::true_type{}) : f(TPR, U, whole_t{}, std::true_type{});
+        return tail ? f(TPR, U, tail_t{}, std::false_type{}) : f(TPR, U, whole_t{}, std::false_type{});
     };
 #define MOE_NORM_CASE(T, UU) if (nv <= T * UU) return with(std::integral_constant<int, T>{}, std::integral_constant<int, UU>{});
     MOE_NORM_CASE(16, 1)
     MOE_NORM_CASE(16, 2)
-    MOE_NORM_CASE(16, 4)
+    if constexpr (BWD) { MOE_NORM_CASE(64, 1) } else { MOE_NORM_CASE(16, 4) }
     MOE_NORM_CASE(64, 2)
     if constexpr (BWD) {
         MOE_NORM_CASE(256, 1)
         MOE_NORM_CASE(256, 2)
+        MOE_NORM_CASE(256, 3)
         MOE_NORM_CASE(512, 2)
+        MOE_NORM_CASE(512, 3)
         MOE_NORM_CASE(512, 4)
     } else {
+        MOE_NORM_CASE(64, 3)
         MOE_NORM_CASE(64, 4)
-        MOE_NORM_CASE(256, 2)
+        MOE_NORM_CASE(64, 5)
+        MOE_NORM_CASE(64, 6)
+        MOE_NORM_CASE(64, 8)
+        MOE_NORM_CASE(256, 3)
         MOE_NORM_CASE(256, 4)
         MOE_NORM_CASE(1024, 2)
     }

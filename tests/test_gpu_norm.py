@@ -104,6 +104,34 @@ def test_forward_and_backward_by_width(d, dtype):
                 assert ((db.double() - wb).abs() <= (rows + 4) * 2.0 ** -24 * sb).all(), (rows, "dbeta")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [5, 15, 17, 130, 260, 300, 515, 770, 1283, 1540, 1795, 2055, 2570, 2571, 3079, 3585, 4099, 5001, 6145, 6986, 8195, 12281, 12290])
+def test_short_last_pieces(d, dtype):
+    """Widths that leave a short piece at every place it can have among a row's threads and pieces."""
+    for rows in (1, 3, 70):
+        i = _inputs(rows, d, dtype, seed=1)
+        n = binding.Norm(d=d, dtype=dtype, eps=1e-5, device=G.DEV)
+        # rows end to end with guards around them: nothing outside is read into the result or written
+        guard = lambda: torch.full((rows * d + 64,), 7.0, dtype=TYPES[dtype], device=G.DEV)  # noqa: E731
+        inside = lambda t: t[32:32 + rows * d].view(rows, d)  # noqa: E731
+        bS, bY, bX = guard(), guard(), guard()
+        S, Y, dX = inside(bS), inside(bY), inside(bX)
+        mean, rstd = torch.empty(rows, device=G.DEV), torch.empty(rows, device=G.DEV)
+        n.fwd(i["X"], i["gamma"], i["beta"], Y, residual=i["R"], total=S, mean=mean, rstd=rstd)
+        assert torch.equal(S, (i["X"].float() + i["R"].float()).to(S.dtype))
+        wm, wr, wy = _forward(S, i["gamma"], i["beta"], 1e-5)
+        em, er, ey = _forward_bounds(S, i["gamma"], i["beta"], wm, wr, wy)
+        assert ((mean.double() - wm).abs() <= em).all() and ((rstd.double() / wr - 1).abs() <= er).all() and ((Y.double() - wy).abs() <= ey).all()
+        dg, db = torch.full((d + 8,), 7.0, device=G.DEV), torch.full((d + 8,), 7.0, device=G.DEV)
+        n.bwd(i["dY"], S, i["gamma"], mean, rstd, dX, dg[:d], db[:d], residual_grad=i["dS"])
+        wx, ex, wg, sg, wb, sb = _backward(i["dY"], S, i["gamma"], mean, rstd, i["dS"])
+        assert ((dX.double() - wx).abs() <= ex).all()
+        assert ((dg[:d].double() - wg).abs() <= (rows + 8) * 2.0 ** -24 * sg).all() and ((db[:d].double() - wb).abs() <= (rows + 4) * 2.0 ** -24 * sb).all()
+        for t in (bS, bY, bX):
+            assert (t[:32] == 7.0).all() and (t[32 + rows * d:] == 7.0).all()
+        assert (dg[d:] == 7.0).all() and (db[d:] == 7.0).all()
+
+
 @pytest.mark.parametrize("rows,d,dtype", [(100000, 64, "bf16"), (70001, 24, "f32"), (9000, 1000, "bf16"), (5000, 4096, "bf16"), (3001, 6001, "f32")])
 def test_many_rows(rows, d, dtype):
     """More rows than a launch of the gradient has places for: every block walks several."""
