@@ -435,9 +435,10 @@ template <typename ET, bool BWD, typename F> hipError_t by_width(int d, bool nt,
 
 // Blocks of the backward pass.  Each leaves a partial sum of the parameters' gradients, 8 d bytes written and read again, and needs rows
 // enough to be worth it: four at least for each group of threads (rows x d bf16, us with 1 | 4 | 8: 4096 x 1024 13.9 | 12.0 | 14.6, 512 x 4096
-// 16.1 | 15.0 | 17.8).  Rows of two pieces a thread and more keep enough on their way with one block of 256 on a CU (32768 x 4096: 512 blocks 187, 256
+// 16.1 | 15.0 | 17.8), but for the first 64 blocks, which cost next to nothing (512 x 64 in fp32, the kernel: 32 blocks 3.3, 8 blocks 4.8), unless a block
+// alone, which needs no second launch, has them all.  Rows of two pieces a thread and more keep enough on their way with one block of 256 on a CU (32768 x 4096: 512 blocks 187, 256
 // 175), others do not (16384 x 2048: 52, 64).
-constexpr int MIN_ROWS = 4;
+constexpr int MIN_ROWS = 4, FREE_BLOCKS = 64;
 inline int blocks_for(int rows, int tpr, int most)
 {
     const int rpb = threads_of(tpr) / tpr, n = (rows - 1) / rpb + 1;
@@ -465,6 +466,7 @@ hipError_t norm_bwd(const moe_norm_t& c, const void* dY, const void* S, const fl
         constexpr int tpr = decltype(TPR)::value;
         constexpr int wide = tpr >= 256 && decltype(U)::value >= 2;
         blocks = blocks_for((c.rows + MIN_ROWS - 1) / MIN_ROWS, tpr, wide ? NORM_PARTIALS / 2 : NORM_PARTIALS);
+        if (blocks > 1 && blocks < FREE_BLOCKS) blocks = blocks_for(c.rows, tpr, FREE_BLOCKS);
         hipLaunchKernelGGL((norm_bwd_kernel<ET, tpr, decltype(U)::value, decltype(TAIL)::value, decltype(NT)::value>), dim3(blocks), dim3(threads_of(tpr)), 0, st,
                            (const ET*)dY, (const ET*)S, gamma, mean, rstd, (const ET*)dS, (ET*)dX, blocks > 1 ? partial : nullptr, dgamma, dbeta, c.rows, c.d);
         return hipGetLastError();
