@@ -291,6 +291,15 @@ def _checked(rc: int, where: str) -> None:
         raise MoeError(rc, where, detail)
 
 
+class _Address(int):
+    """The address of a structure, which it keeps: a call object keeps what it was made from, also when nothing else does."""
+
+    def __new__(cls, struct):
+        self = super().__new__(cls, ctypes.addressof(struct))
+        self.struct = struct
+        return self
+
+
 class Norm:
     """The layer norm of one width and type, with the workspace of its backward pass.  The rows of a call are those of its first tensor."""
 
@@ -315,13 +324,12 @@ class Norm:
         if calls is None:
             if len(self._calls) >= self.MAX_CALLS:
                 self._calls.clear()
-            c = _Norm(rows, self.d, self._dtype, self.eps)
-            e, f, all_, cfg = self.elt, torch.float32, rows * self.d, ctypes.addressof(c)
+            e, f, all_, cfg = self.elt, torch.float32, rows * self.d, _Address(_Norm(rows, self.d, self._dtype, self.eps))
             fwd = (cfg, (e, all_, "X"), (e, all_, "residual"), (f, self.d, "gamma"), (f, self.d, "beta"), (e, all_, "total"), (e, all_, "Y"),
                    (f, rows, "mean"), (f, rows, "rstd"), "int")
             bwd = (cfg, (e, all_, "dY"), (e, all_, "S"), (f, self.d, "gamma"), (f, rows, "mean"), (f, rows, "rstd"), (e, all_, "residual_grad"),
                    (e, all_, "dX"), (f, self.d, "dgamma"), (f, self.d, "dbeta"), "int", "int")
-            calls = self._calls[rows] = (_call_type()(_entry("moe_norm_fwd"), fwd, _ptr), _call_type()(_entry("moe_norm_bwd"), bwd, _ptr), c)
+            calls = self._calls[rows] = (_call_type()(_entry("moe_norm_fwd"), fwd, _ptr), _call_type()(_entry("moe_norm_bwd"), bwd, _ptr))
         return calls
 
     def fwd(self, X, gamma, beta, Y, *, residual=None, total=None, mean=None, rstd=None):

@@ -5,7 +5,8 @@
 // A Call is made from the entry's address and, for each of its arguments (all of them pointers), what stands there: an int, passed
 // on as it is; "int", an int given at the call; or (dtype, numel, name), a tensor given at the call, None for a null pointer.  A
 // tensor that is not plainly fine (of the dtype, contiguous, on the device, large enough) goes to the Python check instead, which
-// raises the error or returns its address.
+// raises the error or returns its address.  The call keeps what it was made from: an int that is an object of its own (an address that
+// keeps the structure it is the address of) lives as long as the call.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Dtype.h>
@@ -16,12 +17,13 @@
 namespace {
 
 constexpr int MAX_ARGS = 16;
-struct Arg { enum Kind { FIXED, INT, TENSOR } kind; void* fixed; PyObject *dtype, *numel, *name; at::ScalarType type; int64_t least; };
+struct Arg { enum Kind { FIXED, INT, TENSOR } kind; void* fixed; PyObject *dtype, *numel, *name; at::ScalarType type; int64_t least; };   // objects of the spec, which keeps them
 struct Call {
     PyObject_HEAD
     vectorcallfunc vectorcall;
     void* entry;
     PyObject* check;                                       // the Python check: (tensor, dtype, numel, name) -> address
+    PyObject* spec;
     int n, n_given;
     Arg args[MAX_ARGS];
 };
@@ -85,14 +87,11 @@ PyObject* call_vector(PyObject* self, PyObject* const* given, size_t nargsf, PyO
     return PyLong_FromLong(rc);
 }
 
-void drop(Call* c)
-{
-    for (int i = 0; i < c->n; ++i) { Py_XDECREF(c->args[i].dtype); Py_XDECREF(c->args[i].numel); Py_XDECREF(c->args[i].name); }
-    Py_XDECREF(c->check);
-}
 void call_dealloc(PyObject* self)
 {
-    drop(reinterpret_cast<Call*>(self));
+    Call* c = reinterpret_cast<Call*>(self);
+    Py_XDECREF(c->spec);
+    Py_XDECREF(c->check);
     Py_TYPE(self)->tp_free(self);
 }
 
@@ -108,6 +107,8 @@ PyObject* call_new(PyTypeObject* type, PyObject* args, PyObject*)
     c->entry = PyLong_AsVoidPtr(entry);
     Py_INCREF(check);
     c->check = check;
+    Py_INCREF(spec);
+    c->spec = spec;
     for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(spec) && !PyErr_Occurred(); ++i) {
         PyObject* o = PyTuple_GET_ITEM(spec, i);
         Arg& a = c->args[c->n++];
@@ -115,8 +116,7 @@ PyObject* call_new(PyTypeObject* type, PyObject* args, PyObject*)
         ++c->n_given;
         if (PyUnicode_Check(o)) { a.kind = Arg::INT; continue; }
         a.kind = Arg::TENSOR;
-        if (!PyArg_ParseTuple(o, "OOO", &a.dtype, &a.numel, &a.name)) { a.dtype = a.numel = a.name = nullptr; break; }
-        Py_INCREF(a.dtype); Py_INCREF(a.numel); Py_INCREF(a.name);
+        if (!PyArg_ParseTuple(o, "OOO", &a.dtype, &a.numel, &a.name)) break;
         if (!THPDtype_Check(a.dtype)) { PyErr_SetString(PyExc_TypeError, "a torch.dtype expected"); break; }
         a.type = reinterpret_cast<THPDtype*>(a.dtype)->scalar_type;
         a.least = PyLong_AsLongLong(a.numel);
