@@ -299,7 +299,8 @@ typedef struct {
 int moe_norm_fwd(const moe_norm_t* cfg, const void* X, const void* R, const float* gamma, const float* beta,
                  void* S, void* Y, float* mean, float* rstd, void* stream);
 
-/* Bytes of workspace (256-byte aligned device memory) moe_norm_bwd may use for any number of rows of this width and type. */
+/* Bytes of workspace (256-byte aligned device memory) moe_norm_bwd may use for any number of rows of this width and type.  Nothing is kept
+ * in it between calls; calls that may run beside each other (two streams) need one each. */
 int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes);
 
 /* Gradient of moe_norm_fwd.  With xh = (S - mean) rstd and g = dY gamma:
@@ -332,7 +333,8 @@ typedef struct {
     float lr, weight_decay, scale;
 } moe_muon_t;
 
-/* Bytes of workspace (256-byte aligned device memory) a step of these sizes uses. */
+/* Bytes of workspace (256-byte aligned device memory) a step of these sizes uses.  Nothing is kept in it between calls; steps that may run
+ * beside each other (two streams) need one each. */
 int moe_muon_workspace_bytes(const moe_muon_t* cfg, size_t* bytes);
 
 /*   in    : on the HOST, arrays of n_tensors device pointers: grads[i] float

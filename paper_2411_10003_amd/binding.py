@@ -301,7 +301,10 @@ class _Address(int):
 
 
 class Norm:
-    """The layer norm of one width and type, with the workspace of its backward pass.  The rows of a call are those of its first tensor."""
+    """The layer norm of one width and type, with the workspace of its backward pass.  The rows of a call are those of its first tensor.
+
+    bwd() calls of one object share that workspace: they belong on one stream, or behind each other by events; what runs beside each other takes an object
+    each.  fwd() uses none."""
 
     MAX_CALLS = 64                                         # row counts whose call objects are kept
 
@@ -347,7 +350,10 @@ class Norm:
 
 class Muon:
     """The update of a set of expert parameters (moe_muon_step), with its workspace: as many tensors as `transposed` has entries, `count` matrices
-    each, rows x cols or, where transposed, cols x rows."""
+    each, rows x cols or, where transposed, cols x rows.
+
+    Steps of one object share the workspace: they belong on one stream, or behind each other by events; what runs beside each other takes an object
+    each."""
 
     def __init__(self, *, count: int, rows: int, cols: int, dtype: str, transposed=(False,), momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
                  coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, device="cuda:0", alloc_workspace: bool = True):
@@ -373,7 +379,7 @@ class Muon:
         """One update of momenta and weights in place, and of copies and version where they are given."""
         if self.ws is None:
             raise ValueError("no workspace attached")
-        cfg = self._cfg
+        cfg = _Muon.from_buffer_copy(self._cfg)            # this call's own: the library reads it without the interpreter's lock
         cfg.lr, cfg.weight_decay, cfg.scale = lr, weight_decay, scale
         rc = self.lib.moe_muon_step(
             ctypes.byref(cfg), self._pointers(grads, torch.float32, "grads"), self._pointers(momenta, torch.float32, "momenta"),

@@ -35,3 +35,26 @@ def test_sizes_of_a_norm_outlive_its_memory_of_row_counts(monkeypatch, kind):
     del call
     gc.collect()
     assert sizes() is None
+
+
+def test_a_step_of_the_update_has_its_own_rates(monkeypatch):
+    """The library reads a step's constants without the interpreter's lock: a step that begins meanwhile with other rates leaves them alone."""
+    mu = binding.Muon(count=1, rows=8, cols=8, dtype="f32", alloc_workspace=False)
+    mu.ws = torch.empty(1)
+    monkeypatch.setattr(binding, "_ptr", lambda *a: 0x1000)
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    seen = []
+
+    class Library:
+        def moe_muon_step(self, cfg, *rest):
+            c = cfg._obj
+            before = (c.lr, c.weight_decay, c.scale)
+            if not seen:
+                seen.append(None)
+                mu.step([0], [0], [0], lr=0.5, weight_decay=0.25, scale=4.0)           # another thread's
+            seen.append((before, (c.lr, c.weight_decay, c.scale), (c.rows, c.cols, c.steps, c.momentum)))
+            return 0
+    monkeypatch.setattr(mu, "lib", Library())
+    mu.step([0], [0], [0], lr=0.125)
+    constants = (8, 8, 5, seen[1][2][3])
+    assert seen[1:] == [((0.5, 0.25, 4.0), (0.5, 0.25, 4.0), constants), ((0.125, 0.0, 1.0), (0.125, 0.0, 1.0), constants)]
