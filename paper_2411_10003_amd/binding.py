@@ -362,6 +362,8 @@ class Muon:
         if not 1 <= self.n <= 8:
             raise ValueError(f"{self.n} tensors: 1 to 8 are taken")
         self.numel = count * rows * cols
+        self.matrix = rows * cols
+        self._row = [rows if t else cols for t in transposed]              # numbers in a row of each tensor
         self.elt = TORCH_DTYPE[DTYPES[dtype]]
         self._cfg = _Muon(self.n, count, rows, cols, (ctypes.c_int * 8)(*(int(bool(t)) for t in transposed)), DTYPES[dtype], int(bool(nesterov)), steps,
                           momentum, eps, *coefficients, 0.0, 0.0, 1.0)
@@ -373,7 +375,22 @@ class Muon:
     def _pointers(self, tensors, dtype, name: str):
         if len(tensors) != self.n:
             raise ValueError(f"{name}: {len(tensors)} tensors, expected {self.n}")
+        for i, (t, row) in enumerate(zip(tensors, self._row)):
+            if t is not None and not self._in_rows(t.shape, row):
+                raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, expected rows of {row}")
         return (ctypes.c_void_p * self.n)(*(_ptr(t, dtype, self.numel, name) for t in tensors))
+
+    def _in_rows(self, shape, row: int) -> bool:
+        """Whether a tensor of this shape may hold matrices whose rows have `row` numbers: the last dimensions make up a row, or it is flat (or flat a
+        matrix).  One that lies the other way round would be updated as other matrices."""
+        if len(shape) <= 1 or shape[-1] == row or shape[-1] % self.matrix == 0:
+            return True
+        n = 1
+        for s in reversed(shape):
+            n *= s
+            if n >= row:
+                return n == row
+        return False
 
     def step(self, grads, momenta, weights, *, lr: float, weight_decay: float = 0.0, scale: float = 1.0, copies=None, version=None):
         """One update of momenta and weights in place, and of copies and version where they are given."""
