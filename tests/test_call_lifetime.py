@@ -43,7 +43,7 @@ def test_a_step_of_the_update_has_its_own_rates(monkeypatch):
     mu.ws = torch.empty(1)
     monkeypatch.setattr(binding, "_ptr", lambda *a: 0x1000)
     monkeypatch.setattr(binding, "_stream", lambda: 0)
-    seen = []
+    seen, one = [], [torch.empty(1, 8, 8, device="meta")]
 
     class Library:
         def moe_muon_step(self, cfg, *rest):
@@ -51,10 +51,10 @@ def test_a_step_of_the_update_has_its_own_rates(monkeypatch):
             before = (c.lr, c.weight_decay, c.scale)
             if not seen:
                 seen.append(None)
-                mu.step([0], [0], [0], lr=0.5, weight_decay=0.25, scale=4.0)           # another thread's
+                mu.step(one, one, one, lr=0.5, weight_decay=0.25, scale=4.0)           # another thread's
             seen.append((before, (c.lr, c.weight_decay, c.scale), (c.rows, c.cols, c.steps, c.momentum)))
             return 0
     monkeypatch.setattr(mu, "lib", Library())
-    mu.step([0], [0], [0], lr=0.125)
+    mu.step(one, one, one, lr=0.125)
     constants = (8, 8, 5, seen[1][2][3])
     assert seen[1:] == [((0.5, 0.25, 4.0), (0.5, 0.25, 4.0), constants), ((0.125, 0.0, 1.0), (0.125, 0.0, 1.0), constants)]
