@@ -291,6 +291,14 @@ def _checked(rc: int, where: str) -> None:
         raise MoeError(rc, where, detail)
 
 
+def _int32(value, name: str) -> int:
+    """A size for a 32-bit field of a structure, which would take any number and keep its low bits."""
+    value = operator.index(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name}: {value} does not fit 32 bits")
+    return value
+
+
 class _Address(int):
     """The address of a structure, which it keeps: a call object keeps what it was made from, also when nothing else does."""
 
@@ -307,10 +315,11 @@ class Norm:
     each.  fwd() uses none."""
 
     MAX_CALLS = 64                                         # row counts whose call objects are kept
+    MAX_ROWS = 2 ** 30 - 1                                 # of a call of moe_norm_fwd, moe_norm_bwd
 
     def __init__(self, *, d: int, dtype: str, eps: float = 1e-5, device="cuda:0", alloc_workspace: bool = True):
         self.lib = load()
-        self.d, self.eps = d, eps
+        self.d, self.eps = _int32(d, "d"), eps
         self.elt = TORCH_DTYPE[DTYPES[dtype]]
         self._dtype = DTYPES[dtype]
         n = ctypes.c_size_t()
@@ -324,6 +333,8 @@ class Norm:
         calls = self._calls.get(rows)
         if rest:
             raise ValueError(f"{first.numel()} elements are no rows of {self.d}")
+        if rows > self.MAX_ROWS:
+            raise ValueError(f"{rows} rows: {self.MAX_ROWS} at most")
         if calls is None:
             if len(self._calls) >= self.MAX_CALLS:
                 self._calls.clear()
@@ -361,6 +372,7 @@ class Muon:
         self.n = len(transposed)
         if not 1 <= self.n <= 8:
             raise ValueError(f"{self.n} tensors: 1 to 8 are taken")
+        count, rows, cols, steps = (_int32(v, name) for v, name in ((count, "count"), (rows, "rows"), (cols, "cols"), (steps, "steps")))
         self.numel = count * rows * cols
         self.matrix = rows * cols
         self._row = [rows if t else cols for t in transposed]              # numbers in a row of each tensor
