@@ -47,7 +47,7 @@ template <> struct Piece<bf16_t> {
 
 // TAIL: a row's last piece is short, `n` of its N elements are inside the row (elsewhere n = N, or 0 and less where a thread has no piece).
 //   1  It is requested as the row's last N elements, those of the piece before it among them, and moved down when it is used (settle): nothing is
-//      waited for where the request is made, which is a row ahead in the backward pass (the gradient of 20000 x 2500 in bf16 110 us, of 20000 x 2496 91).
+//      waited for where the request is made, which is a row ahead in the backward pass (the gradient of 20000 x 2500 in bf16 117 us, of 20000 x 2496 91).
 //   2  Element by element: rows shorter than a piece, and the forward pass, which waits for its row at once (59811 x 2244 230 us, moved down 250;
 //      20000 x 5001 192, 235; the gradient of 20000 x 2500 291).
 // NT: past the caches (STREAM_BYTES).
@@ -77,6 +77,10 @@ template <typename ET, int TAIL> __device__ __forceinline__ void settle(moe_piec
     if (bits >= 64) { lo = hi; hi = 0; bits -= 64; }
     if (bits > 0) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
     v = moe_piece_t{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+    // The gradient may be written over dY or dS.  A short piece's request reads columns of the piece before it, which a thread of another wave stores once
+    // it is past the barrier of the row's sums: what was requested has arrived here, and this stays ahead of that barrier, also for dS, which
+    // nothing uses until after it (20000 x 2500 in bf16 109 -> 117 us, 4000 x 16383 in fp32 417 -> 402, most widths as before).
+    asm volatile("" : "+v"(v));
 }
 template <typename ET, int TAIL, bool NT> __device__ __forceinline__ void store_row_piece(ET* p, const moe_piece_t& v, int n)
 {
