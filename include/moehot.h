@@ -320,8 +320,10 @@ int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const flo
  *   `steps` times, with X on its long side:  A = X X^T,  X <- a X + (b A + c A A) X
  *   W <- (1 - lr weight_decay) W - lr scale X
  * The steps have to keep the singular values of X below 3 (the usual coefficients, 3.4445, -4.7750, 2.0315, below 1.3): the iterates are scaled for that.
- * M, |U| and the sums are fp32 or more.  For MOE_BF16 weights the iterates are kept in 11 bits, fp16 with a scale (X is then within some
- * 1e-3 of what 64 bits give, W within its own rounding); for MOE_F32 weights in 22.
+ * M, |U| and the sums are fp32 or more.  For MOE_BF16 weights the iterates are kept in 11 bits, fp16 with a scale, for MOE_F32 weights in 22.
+ * What a rounding leaves outside the range of U grows by a in each step: of a rank r (an expert that received r rows) X is off what 64 bits give by
+ * up to 0.15 / sqrt(r) of its norm in 11 bits and 3e-5 / sqrt(r) in 22, of full rank with a falling spectrum by 5e-3 and 4e-6.  bf16 parameters that
+ * are to have the second are kept as MOE_F32 weights with `copies`.
  * Limits: rows, cols >= 1, rows * cols < 2^30, each <= 65536; n_tensors * count <= 65535; 1 <= steps <= 16; 0 <= momentum < 1; eps > 0;
  * |a|, |b|, |c| <= 16; lr, weight_decay, scale finite. */
 typedef struct {

@@ -18,10 +18,13 @@
 // bf16 with 8; its range is made up for by powers of two: |X|_F <= 1.3 or so is stored times the root mean square of its elements' size
 // (S = 2^floor(log2 sqrt(mn)), at most 2^14), A, whose eigenvalues are at most 1.5, times 2^10, B, at most a, times 2^6,
 // Q, at most a^3, times 2^3.
-// What a rounding to 11 bits leaves off the orthogonal factor is 1.5e-3 of it for a dense spectrum and 3.5e-3 for one of a quarter of the
-// rank with a tail (bf16: eight times that), and the factor changes a weight by a few per cent of it: nothing that a bf16 weight resolves.
+// What a rounding leaves outside the range of U, some 2^-12 of |X| in 11 bits, grows by a a step, 485 times in five.  Off the orthogonal factor it is
+// 1.5e-3 of it for a dense spectrum, 5e-3 for one of a quarter of the rank with noise below it, and up to 0.15 / sqrt(r) for a rank r without: 0.15,
+// 6e-2, 3e-2, 1.5e-2 at ranks 1, 4, 16, 64 (bf16: up to eight times that).  The factor changes a weight by a few per cent of it: short of the lowest
+// ranks that is nothing that a bf16 weight resolves, and there it is a step of its rounding.
 // fp32 weights do resolve it: for them every operand is two fp16 numbers, the second the rounding error of the first (22 bits), and a
-// product is three, hi lo + lo hi + hi hi, segments of one contraction (2e-6 to 4e-6 off the factor, as fp32 throughout is).
+// product is three, hi lo + lo hi + hi hi, segments of one contraction (2e-6 to 4e-6 off the factor, as fp32 throughout is; 3e-5 / sqrt(r) at rank r,
+// where fp32 throughout leaves 1e-4).
 #include "tile.h"
 
 #include <cmath>
