@@ -295,6 +295,7 @@ typedef struct {
  *   in : X[rows,d] elt, R[rows,d] elt (the residual stream; NULL: S is X itself), gamma[d], beta[d] (NULL: none) float
  *   out: S[rows,d] elt (given with R, NULL without), Y[rows,d] elt, mean[rows], rstd[rows] float (both or neither: a backward call
  *        needs them, a forward-only pass does not)
+ * A row whose sum of squares leaves fp32 (elements of 1e19 / sqrt(d) and more off its mean) has rstd = 0.
  * S may be X or R, and without R Y may be X; other overlaps are not allowed. */
 int moe_norm_fwd(const moe_norm_t* cfg, const void* X, const void* R, const float* gamma, const float* beta,
                  void* S, void* Y, float* mean, float* rstd, void* stream);
@@ -305,7 +306,7 @@ int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes);
 
 /* Gradient of moe_norm_fwd.  With xh = (S - mean) rstd and g = dY gamma:
  *   dX = dS + rstd (g - sum_c g / d - xh sum_c (g xh) / d), rounded once;  dgamma = sum_rows dY xh,  dbeta = sum_rows dY
- * fp32 sums in a fixed order (same bits every run on a GPU of as many compute units).
+ * fp32 sums in a fixed order (same bits every run).
  *   in : dY[rows,d] elt, S[rows,d] elt (X where there was no R), gamma[d], mean[rows], rstd[rows] as moe_norm_fwd left them;
  *        dS[rows,d] elt (the residual stream's own gradient; NULL: none)
  *   out: dX[rows,d] elt (the gradient of X and of R alike), dgamma[d] float, dbeta[d] float (NULL: not wanted)
@@ -320,6 +321,7 @@ int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const flo
  *   `steps` times, with X on its long side:  A = X X^T,  X <- a X + (b A + c A A) X
  *   W <- (1 - lr weight_decay) W - lr scale X
  * The steps have to keep the singular values of X below 3 (the usual coefficients, 3.4445, -4.7750, 2.0315, below 1.3): the iterates are scaled for that.
+ * Same bits every run on a GPU of as many compute units: how products are cut into tiles goes by their number.
  * M, |U| and the sums are fp32 or more.  For MOE_BF16 weights the iterates are kept in 11 bits, fp16 with a scale, for MOE_F32 weights in 22.
  * What a rounding leaves outside the range of U grows by a in each step: of a rank r (an expert that received r rows) X is off what 64 bits give by
  * up to 0.15 / sqrt(r) of its norm in 11 bits and 3e-5 / sqrt(r) in 22, of full rank with a falling spectrum by 5e-3 and 4e-6.  bf16 parameters that

@@ -9,15 +9,17 @@
 //
 // Every X is Q X0 with Q a polynomial in A0 = X0 X0^T, so the steps can be taken on the short side: B = a + b A + c A A,  Q <- B Q,
 // A <- B A B (all of them polynomials in A0: they commute and are symmetric, half of each product is the other half), and X = Q X0 at
-// the end.  Five steps: 6 m^2 n + 14 m^3 multiply-adds where the form above takes 15 m^2 n + 5 m^3; as many at n = m, 0.58 of it at n = 4 m.  A
-// carries the squares of the singular values, and what a rounding adds to those near zero grows by a^2 = 11.9 a step that goes on
-// with the same A: after three steps (each, where the short side is 64 or less) A is formed again from X.  Off the factor that 64 bits give, 11 bits kept, 256 x 1024 of a falling spectrum:
-// the form above 3.4e-3; all five steps on one A 1.2e-1; two, then three 1.5e-2; three, then two 3.5e-3.
+// the end.  Five steps: 6 m^2 n + 14 m^3 operations, halves of symmetric products, where the form above takes 15 m^2 n + 5 m^3; as many at
+// n = m, 0.58 of it at n = 4 m.  A carries the squares of the singular values, and what a rounding adds to those near zero grows by a^2 = 11.9 a
+// step that goes on with the same A: after three steps (each, where the short side is 64 or less) A is formed again from X.  Off the
+// factor that 64 bits give, 11 bits kept, 256 x 1024 of a falling spectrum: the form above 3.4e-3; all five steps on one A 1.2e-1; two, then
+// three 1.5e-2; three, then two 3.5e-3.
 //
 // What X, A and the polynomial are kept in.  The products take 16-bit operands and add in fp32.  fp16, with its 11 bits, at the rate of
-// bf16 with 8; its range is made up for by powers of two: |X|_F <= 1.3 or so is stored times the root mean square of its elements' size
-// (S = 2^floor(log2 sqrt(mn)), at most 2^14), A, whose eigenvalues are at most 1.5, times 2^10, B, at most a, times 2^6,
-// Q, at most a^3, times 2^3.
+// bf16 with 8; its range is made up for by powers of two.  X is stored times S = 2^floor(log2 sqrt(mn)), at most 2^14, which brings the elements of the
+// first, of Frobenius norm 1, near 1; its singular values stay below 1.3 with the usual coefficients and have to below 3.  A, whose
+// eigenvalues are their squares, times 2^10, B, at most a, times 2^6, Q, at most a^3, times 2^3.  Of the 65504 that fp16 holds an element
+// is then, singular values of 3 and a = 16 given, X 49152, A 9216, B 1024 and Q 32768 at most.
 // What a rounding leaves outside the range of U, some 2^-12 of |X| in 11 bits, grows by a a step, 485 times in five.  Off the orthogonal factor it is
 // 1.5e-3 of it for a dense spectrum, 5e-3 for one of a quarter of the rank with noise below it, and up to 0.15 / sqrt(r) for a rank r without: 0.15,
 // 6e-2, 3e-2, 1.5e-2 at ranks 1, 4, 16, 64 (bf16: up to eight times that).  The factor changes a weight by a few per cent of it: short of the lowest
