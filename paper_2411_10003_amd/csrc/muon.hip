@@ -1090,8 +1090,9 @@ template <class GEO> Layout layout_of(const GeometryTime& g, int tiles, int slic
 }
 
 template <int KIND, int OUT, bool ADD, int PLANES, typename WT, class GEO>
-hipError_t launch_tiles(Product p, const Layout& l, hipStream_t st)
+hipError_t launch_tiles(Product p, const Layout& l, size_t part_bytes, hipStream_t st)
 {
+    if ((size_t)l.cut * l.parts * GEO::UNIT_BYTES > part_bytes) return hipErrorInvalidValue;   // the plan has room for any layout (parts_bytes)
     p.row_tiles = (p.M + GEO::BM - 1) / GEO::BM;
     p.col_tiles = (p.N + GEO::BN - 1) / GEO::BN;
     p.tiles = p.symmetric ? p.row_tiles * (p.row_tiles + 1) / 2 : p.row_tiles * p.col_tiles;
@@ -1122,30 +1123,43 @@ template <class GEO> int tiles_of(const Product& p, int matrices)
     return (p.symmetric ? rt * (rt + 1) / 2 : rt * ct) * matrices;
 }
 
-template <int KIND, int OUT, bool ADD, int PLANES, typename WT> hipError_t launch_product(const Product& p, int matrices, int cus, hipStream_t st)
+template <int KIND, int OUT, bool ADD, int PLANES, typename WT> hipError_t launch_product(const Product& p, int matrices, int cus, size_t part_bytes, hipStream_t st)
 {
     const int slices = p.n_seg * (p.K / BK), tiles = tiles_of<Small>(p, matrices);
     const Layout l = layout_of<Large>(LARGE_TIME, tiles_of<Large>(p, matrices), slices, cus), m = layout_of<Small>(SMALL_TIME, tiles, slices, cus);
     if (tiles <= cus) {
         const Layout f = layout_of<Fine>(FINE_TIME, tiles_of<Fine>(p, matrices), slices, cus), d = layout_of<Deep>(DEEP_TIME, tiles, slices, cus);
-        if (f.us < d.us && f.us < l.us && f.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Fine>(p, f, st);
+        if (f.us < d.us && f.us < l.us && f.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Fine>(p, f, part_bytes, st);
+        if (d.us < l.us && d.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Deep>(p, d, part_bytes, st);
     }
-    if (tiles <= cus) {
-        const Layout d = layout_of<Deep>(DEEP_TIME, tiles, slices, cus);
-        if (d.us < l.us && d.us < m.us) return launch_tiles<KIND, OUT, ADD, PLANES, WT, Deep>(p, d, st);
-    }
-    return l.us < m.us ? launch_tiles<KIND, OUT, ADD, PLANES, WT, Large>(p, l, st) : launch_tiles<KIND, OUT, ADD, PLANES, WT, Small>(p, m, st);
+    return l.us < m.us ? launch_tiles<KIND, OUT, ADD, PLANES, WT, Large>(p, l, part_bytes, st) : launch_tiles<KIND, OUT, ADD, PLANES, WT, Small>(p, m, part_bytes, st);
 }
 
-// Compute units of the current device, a multiple of 8 (blocks are dealt to 8 XCDs); 256 at most, which the workspace for parts is sized for.
+// What the parts of a product's cut tiles take at most: no more than MAX_PARTS of each tile, no more than there are places for blocks.
+constexpr int MAX_CUS = 256;
+template <class GEO> size_t parts_bytes(const GeometryTime& g, const Product& p, int matrices)
+{
+    const long units = (long)tiles_of<GEO>(p, matrices) * MAX_PARTS, places = (long)MAX_CUS * GEO::BLOCKS;
+    return p.n_seg * (p.K / BK) / 2 < g.least ? 0 : (size_t)(units < places ? units : places) * GEO::UNIT_BYTES;
+}
+size_t parts_bytes(const Product& p, int matrices)
+{
+    size_t most = 0;
+    for (size_t b : {parts_bytes<Large>(LARGE_TIME, p, matrices), parts_bytes<Small>(SMALL_TIME, p, matrices), parts_bytes<Deep>(DEEP_TIME, p, matrices),
+                     parts_bytes<Fine>(FINE_TIME, p, matrices)})
+        most = b > most ? b : most;
+    return most;
+}
+
+// Compute units of the current device, a multiple of 8 (blocks are dealt to 8 XCDs); MAX_CUS at most, which the workspace for parts is sized for.
 inline int device_cus()
 {
     static std::atomic<int> of[64];
     const int dev = current_device();
     int n = (dev >= 0 && dev < 64) ? of[dev].load(std::memory_order_acquire) : 0;
     if (n == 0) {
-        if (dev < 0 || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8) n = 256;
-        n = n > 256 ? 256 : n / 8 * 8;
+        if (dev < 0 || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8) n = MAX_CUS;
+        n = n > MAX_CUS ? MAX_CUS : n / 8 * 8;
         if (dev >= 0 && dev < 64) of[dev].store(n, std::memory_order_release);
     }
     return n;
@@ -1164,8 +1178,14 @@ constexpr int MAX_CHUNKS = 256;                            // parts of a matrix'
 struct MuonPlan {
     int matrices, m, n, mp, np, planes, chunks;
     size_t x_numbers, a_numbers;                           // of all matrices
-    size_t off_partial, off_arrived, off_parts, off_x[2], off_a[4], bytes;         // a second plane, where there is one, follows the first
+    size_t part_bytes, off_partial, off_arrived, off_parts, off_x[2], off_a[4], bytes;         // a second plane, where there is one, follows the first
 };
+// Whether a block takes a whole matrix (few_kernel), and the padded short side it is made for.
+inline int few_side(const MuonPlan& p) { return p.mp <= 64 ? 64 : 128; }
+inline bool takes_few(const MuonPlan& p)
+{
+    return p.mp <= (p.planes == 1 ? 128 : 64) && p.m * p.n <= FEW_ELEMENTS && few_lds(few_side(p), p.np, p.planes) <= FEW_LDS;
+}
 MuonPlan plan_of(const moe_muon_t& c)
 {
     MuonPlan p{};
@@ -1183,7 +1203,16 @@ MuonPlan plan_of(const moe_muon_t& c)
     auto take = [&](size_t bytes) { const size_t at = off; off += align_ws(bytes); return at; };
     p.off_partial = take((size_t)p.matrices * p.chunks * sizeof(double));
     p.off_arrived = take(MAX_CUT * sizeof(int));
-    p.off_parts = take((size_t)256 * Large::UNIT_BYTES);                   // a tile of 256 x 256 for each CU, or two of 128 x 128
+    if (!takes_few(p)) {
+        Product square{}, product{};
+        square.n_seg = product.n_seg = p.planes == 1 ? 1 : 3;
+        square.M = square.N = product.M = product.K = p.mp;
+        square.K = product.N = p.np;                       // X X^T; the others' contraction is shorter
+        square.symmetric = 1;
+        const size_t a = parts_bytes(square, p.matrices), b = parts_bytes(product, p.matrices);
+        p.part_bytes = a > b ? a : b;
+    }
+    p.off_parts = take(p.part_bytes);
     for (size_t& x : p.off_x) x = take(p.x_numbers * sizeof(f16) * p.planes);
     for (size_t& a : p.off_a) a = take(p.a_numbers * sizeof(f16) * p.planes);
     p.bytes = off;
@@ -1214,8 +1243,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         t.transposed[i] = (c.rows <= c.cols) == (c.transposed[i] != 0) && c.rows != c.cols ? 1 : 0;
     }
     const float keep = (float)(1.0 - (double)c.lr * c.weight_decay), rate = (float)((double)c.lr * c.scale / S);
-    const int few_mp = P.mp <= 64 ? 64 : 128;
-    if (P.mp <= 128 && P.m * P.n <= FEW_ELEMENTS && few_lds(few_mp, P.np, PLANES) <= FEW_LDS) {
+    if (takes_few(P)) {
         Few f{};
         f.m = P.m; f.n = P.n; f.np = P.np; f.count = c.count; f.nesterov = c.nesterov; f.steps = c.steps;
         f.mu = c.momentum; f.eps = c.eps; f.S = S; f.SA = SA; f.SB = SB; f.a = c.a; f.b = c.b; f.c = c.c; f.keep = keep; f.rate = rate;
@@ -1223,7 +1251,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
             f.grad[i] = grads[i]; f.momentum[i] = momenta[i]; f.W[i] = weights[i]; f.copies[i] = copies ? copies[i] : nullptr; f.transposed[i] = t.transposed[i];
         }
         f.version = version;
-        if (few_mp == 64) return launch_few<PLANES, 4, WT>(f, P.matrices, st);
+        if (few_side(P) == 64) return launch_few<PLANES, 4, WT>(f, P.matrices, st);
         if constexpr (PLANES == 1) return launch_few<PLANES, 8, WT>(f, P.matrices, st);    // two numbers of 128 x 128 twice leave no room for X
     }
     const bool nt = (size_t)P.matrices * P.m * P.n * 8 >= CACHE_BYTES;
@@ -1256,7 +1284,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         p.alpha = alpha; p.beta = beta; p.diag = diag;
         if (add) { p.D = add->first; p.D_rest = add->rest; }
         p.O = out.first; p.O_rest = out.rest;
-        e = add ? launch_product<ROWS, STORE, true, PLANES, float>(p, P.matrices, cus, st) : launch_product<ROWS, STORE, false, PLANES, float>(p, P.matrices, cus, st);
+        e = add ? launch_product<ROWS, STORE, true, PLANES, float>(p, P.matrices, cus, P.part_bytes, st) : launch_product<ROWS, STORE, false, PLANES, float>(p, P.matrices, cus, P.part_bytes, st);
     };
     const Stored A = stored(P.off_a[0], P.a_numbers);
     for (int left = c.steps, of = 0; left > 0 && e == hipSuccess; left -= of) {
@@ -1284,7 +1312,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
         q.alpha = 1.0f / q_scale;
         if (of < left) {
             q.O = X2.first; q.O_rest = X2.rest;
-            e = launch_product<COLS, STORE, false, PLANES, float>(q, P.matrices, cus, st);
+            e = launch_product<COLS, STORE, false, PLANES, float>(q, P.matrices, cus, P.part_bytes, st);
             const Stored x = X; X = X2; X2 = x;
         } else {
             q.count = c.count; q.m = P.m; q.n = P.n;
@@ -1292,7 +1320,7 @@ hipError_t muon_step(const moe_muon_t& c, const float* const* grads, float* cons
             q.keep = keep;
             q.rate = rate;
             q.version = version;
-            e = launch_product<COLS, UPDATE, false, PLANES, WT>(q, P.matrices, cus, st);
+            e = launch_product<COLS, UPDATE, false, PLANES, WT>(q, P.matrices, cus, P.part_bytes, st);
         }
     }
     return e;
