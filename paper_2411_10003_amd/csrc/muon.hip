@@ -1066,8 +1066,9 @@ template <int PLANES, int MT, typename WT> hipError_t launch_few(const Few& f, i
 
 // How a product is laid out: the geometry, and into how many parts the tiles after the last full round of the chip's places are cut.
 // us of a slice (of all the blocks a CU holds), of what a tile costs beside its slices, and of joining two parts (a quarter more for each
-// further one).  128 x 128 tiles are bound by what L2 delivers to a CU, 29 bytes a clock, whether one or two share it: what more parts
-// gain is CUs, not overlap.  Measured, us: squares of m = 4096 (six; 816 tiles of 256, 128 slices) 413 whole, 370 with the last 48 in five parts; X X^T
+// further one).  A slice of 128 x 128 takes as long whether one or two blocks share a CU: what more parts gain is CUs, not overlap.  Of its 560 to 590
+// clocks the matrix pipes have 256 and the fragment reads 177, and it fetches 29 bytes a clock, half of what the path from L2 gives: counted on the
+// squares of 4 x 1024 x 4096, no one of them bounds it, their order between two barriers does.  Measured, us: squares of m = 4096 (six; 816 tiles of 256, 128 slices) 413 whole, 370 with the last 48 in five parts; X X^T
 // of 4 x 1024 x 4096 (144 tiles of 128, 128 slices) 38 whole, 33 in three parts, of 6 x 500 x 1333 in two numbers (60 tiles, 126 slices) 42 and 25
 // in four; its squares (48 slices) 17.8 whole, 18.8 in three.  64 x 64 tiles where those of 128 do not fill the CUs, the whole call, us: two numbers, 6 x
 // 1333 x 500 374 -> 272, 16 x 200 x 300 233 -> 153; bf16, 8 x 256 x 1024 149 -> 108, 6 x 384 x 768 167 -> 121; 4 x 1024 x 4096, whose squares are 144
