@@ -282,7 +282,7 @@ int moe_agg(moe_handle_t h, const int32_t* expert_dest, int n_tensors, const flo
  * The layer is one half of a pre-norm block: what its gate reads is the layer norm of the residual stream, and the
  * stream goes on past it.  These two calls need no handle: a model's norms are as many as its widths.
  *
- * moe_norm_t: rows >= 0 (none: the forward call does nothing, the backward call writes zero parameter gradients), 1 <= d <= 16384, any d
+ * moe_norm_t: 0 <= rows < 2^30 (none: the forward call does nothing, the backward call writes zero parameter gradients), 1 <= d <= 16384, any d
  * (rows lie d elements apart and need no alignment beyond an element's), eps > 0 and finite. */
 typedef struct {
     int rows, d;
