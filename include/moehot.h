@@ -314,6 +314,91 @@ int moe_norm_workspace_bytes(const moe_norm_t* cfg, size_t* bytes);
 int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const float* gamma, const float* mean, const float* rstd,
                  const void* dS, void* dX, float* dgamma, float* dbeta, void* ws, void* stream);
 
+/* Attention, the other half of the block (the paper's non-MoE layer).  Tensors of rows x heads x d: element (r, h, c) lies r * row + h * head + c
+ * elements from p, so a token's heads may lie beside each other, in the middle of a projection's output, or a head's rows together.
+ * p and both strides are multiples of 16 bytes (a stride along a dimension of one is not looked at); row strides at least d and below 2^21 elements, head strides not negative.
+ * What a call writes must not lie on itself: row >= (heads - 1) * head + d with head >= d, or head >= (rows - 1) * row + d with row >= d. */
+typedef struct {
+    void* p;
+    long long row, head;
+} moe_heads_t;
+
+/* moe_rotary_fwd: what comes between the projection of queries and keys and their products.  Per head x of d elements, in fp32, rounded once:
+ *   norm = 1:  x <- x / sqrt(sum_c x^2 / d + eps) * gamma   (gamma_q for queries, gamma_k for keys)
+ *   then its first `rot` columns in pairs (a, b), the others as they are:  pair i by the angle t = positions[row] * frequencies[i], of 64 bits,
+ *   (a, b) <- amplitude * (a cos t - b sin t, b cos t + a sin t);  interleaved = 1: columns (2i, 2i + 1), 0: (i, i + rot / 2).
+ * Limits: 0 <= rows < 2^30, heads, kv_heads >= 1, heads + 2 kv_heads <= 65535, d a multiple of 8 up to 256, rot even, 0 <= rot <= d, eps > 0 (with the norm), amplitude finite. */
+typedef struct {
+    int rows, heads, kv_heads, d;
+    int rot, interleaved, norm;
+    moe_dtype_t dtype;
+    float eps, amplitude;
+    int out_rows;               /* rows of Ko and Vo where slots are given */
+} moe_rotary_t;
+
+/*   in : Q[rows,heads,d], K[rows,kv_heads,d]; gamma_q[d], gamma_k[d] float (with the norm; NULL without); positions[rows] int32;
+ *        frequencies[rot/2] double, radians a position; V[rows,kv_heads,d] (NULL, as Vo: values are not looked at)
+ *        slots[rows] int32 (NULL: none): keys and values of row r go to row slots[r] of Ko and Vo, a cache of out_rows rows; where that is
+ *        outside 0 .. out_rows - 1 (a padded row) they go nowhere.  No slot twice in one call.
+ *   out: Qo[rows,heads,d], Ko[rows,kv_heads,d], Vo (as V)
+ * Without slots Qo may be Q and Ko K (the same strides); other overlaps are not allowed. */
+int moe_rotary_fwd(const moe_rotary_t* cfg, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const float* gamma_q, const float* gamma_k,
+                   const int32_t* positions, const double* frequencies, const int32_t* slots, const moe_heads_t* Qo, const moe_heads_t* Ko,
+                   const moe_heads_t* Vo, void* stream);
+
+/* Bytes of workspace (256-byte aligned device memory) moe_rotary_bwd may use for any number of rows and heads.  Nothing is kept in it between calls;
+ * calls that may run beside each other (two streams) need one each. */
+int moe_rotary_workspace_bytes(const moe_rotary_t* cfg, size_t* bytes);
+
+/* Gradient of moe_rotary_fwd (without slots): the rotation back, then with the norm, xh = x rstd, g = dy gamma:
+ *   dx = rstd (g - xh sum_c (g xh) / d), rounded once;  dgamma = sum over rows and heads of dy xh (fp32, in a fixed order)
+ *   in : dQo[rows,heads,d], dKo[rows,kv_heads,d]; with the norm Q, K as they went into the forward call, gamma_q, gamma_k (NULL without)
+ *   out: dQ, dK; with the norm dgamma_q[d], dgamma_k[d] float (NULL without)
+ * dQ may be dQo or Q and dK may be dKo or K (the same strides).  Uses the workspace. */
+int moe_rotary_bwd(const moe_rotary_t* cfg, const moe_heads_t* dQo, const moe_heads_t* dKo, const moe_heads_t* Q, const moe_heads_t* K,
+                   const float* gamma_q, const float* gamma_k, const int32_t* positions, const double* frequencies, const moe_heads_t* dQ,
+                   const moe_heads_t* dK, float* dgamma_q, float* dgamma_k, void* ws, void* stream);
+
+/* moe_attn_fwd: softmax attention of `seqs` sequences.  Sequence s has the queries offsets[s] .. offsets[s+1] - 1 (n of them) and the keys k_begin[s] ..
+ * k_end[s] - 1 (m of them): those of packed sequences (k_begin and k_end NULL) lie where their
+ * queries do, a cache has each sequence's keys in a place of its own.  heads / kv_heads
+ * neighbouring heads share keys and values.  Query i sees the keys j < m or, with causal = 1, j <= i + m - n: the last query sees the last key.
+ *   a_ij = scale <q_i, k_j>, fp32;  lse_i = log sum_j exp(a_ij);  O_i = sum_j exp(a_ij - lse_i) v_j, exponentials rounded to bf16 for MOE_BF16, sums in fp32
+ * A query that sees nothing has O = 0 and lse = -inf.  Rows that no sequence has are left as they were.  Offsets are held inside 0 .. q_rows and 0 .. k_rows on the
+ * device, whatever they are (offsets that fall, or lie on each other: some of the rows are not right).
+ * A NaN or an infinity in a row of Q stays in that row, one in K in the rows that see the key; one in V reaches the rows that see it and, through
+ * products with the zeros of a mask, may reach queries of its own sequence that causality hides it from by up to 63 keys.  Memory past a sequence's end is
+ * not read into any result.
+ * Limits: 0 <= q_rows, k_rows < 2^30, 0 <= seqs <= 65535, heads a multiple of kv_heads, heads <= 1024, d a multiple of 8 up to 128, scale > 0 and finite,
+ * (q_rows / 32 + seqs) * heads < 2^30. */
+typedef struct {
+    int q_rows, k_rows, seqs;
+    int heads, kv_heads, d;
+    moe_dtype_t dtype;
+    int causal;
+    float scale;
+} moe_attn_t;
+
+/* Bytes of workspace (256-byte aligned device memory) the calls of this or fewer rows and sequences, of the same heads, may use.  Nothing is kept in it between calls;
+ * calls that may run beside each other (two streams) need one each. */
+int moe_attn_workspace_bytes(const moe_attn_t* cfg, size_t* bytes);
+
+/*   in : Q[q_rows,heads,d], K[k_rows,kv_heads,d], V[k_rows,kv_heads,d]; offsets[seqs+1], k_begin[seqs], k_end[seqs] int32, device
+ *   out: O[q_rows,heads,d], lse[heads,q_rows] float (NULL: not wanted; a backward call needs it)
+ * O may be Q (the same strides); other overlaps are not allowed. */
+int moe_attn_fwd(const moe_attn_t* cfg, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const moe_heads_t* O, float* lse,
+                 const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, void* ws, void* stream);
+
+/* Gradient of moe_attn_fwd.  With p_ij = exp(a_ij - lse_i), D_i = <dO_i, O_i>, ds_ij = p_ij (<dO_i, v_j> - D_i):
+ *   dQ_i = scale sum_j ds_ij k_j;  dK_j = scale sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i, the last two over the heads that share the key; sums in fp32 in a fixed
+ *   order, p and ds rounded to bf16 for MOE_BF16
+ *   in : dO[q_rows,heads,d], Q, K, V, O, lse as the forward call had and left them; offsets, k_begin, k_end: k_begin rises, and no key belongs to two sequences
+ *   out: dQ[q_rows,heads,d], dK[k_rows,kv_heads,d], dV[k_rows,kv_heads,d]: rows of sequences only, those of keys that no query sees zero
+ * No output may lie on an input.  Uses the workspace. */
+int moe_attn_bwd(const moe_attn_t* cfg, const moe_heads_t* dO, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const moe_heads_t* O,
+                 const float* lse, const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, const moe_heads_t* dQ, const moe_heads_t* dK,
+                 const moe_heads_t* dV, void* ws, void* stream);
+
 /* moe_muon_step: the update of expert parameters that comes before they are transferred (Section 5.1), by the Muon rule: momentum,
  * orthogonalised by a few Newton-Schulz products.  n_tensors (1..8) tensors of `count` matrices each; tensor i holds matrices of
  * rows x cols, or of cols x rows where transposed[i] is 1 (W1, W3 [G,d,h] and W2 [G,h,d] of the same experts are one call).  Per matrix:

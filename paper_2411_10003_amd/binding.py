@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import math
 import operator
 import os
 from typing import Dict, Optional
@@ -30,6 +31,7 @@ EXPORTS = [
     "moe_plan", "moe_gate_bwd_params", "moe_input_grad", "moe_expert_ffn_bwd_acc", "moe_trans", "moe_recv_layout",
     "moe_dispatch_after_counts", "moe_set_act_saved", "moe_expert_counts_static", "moe_agg", "moe_calib_copy", "moe_calib_mfma",
     "moe_calib_round_bf16", "moe_norm_fwd", "moe_norm_workspace_bytes", "moe_norm_bwd",
+    "moe_rotary_fwd", "moe_rotary_workspace_bytes", "moe_rotary_bwd", "moe_attn_workspace_bytes", "moe_attn_fwd", "moe_attn_bwd",
     "moe_muon_workspace_bytes", "moe_muon_step",
 ]
 
@@ -56,6 +58,19 @@ class _Planner(ctypes.Structure):
 
 class _Norm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_longlong), ("head", ctypes.c_longlong)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "heads", "kv_heads", "d", "rot", "interleaved", "norm", "dtype")] + \
+               [("eps", ctypes.c_float), ("amplitude", ctypes.c_float), ("out_rows", ctypes.c_int)]
+
+
+class _Attn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("q_rows", "k_rows", "seqs", "heads", "kv_heads", "d", "dtype", "causal")] + [("scale", ctypes.c_float)]
 
 
 class _Muon(ctypes.Structure):
@@ -110,6 +125,13 @@ def load() -> ctypes.CDLL:
         lib.moe_norm_fwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 9
         lib.moe_norm_workspace_bytes.argtypes = [ctypes.POINTER(_Norm), ctypes.POINTER(ctypes.c_size_t)]
         lib.moe_norm_bwd.argtypes = [ctypes.POINTER(_Norm)] + [vp] * 11
+        hp = ctypes.POINTER(_Heads)
+        lib.moe_rotary_fwd.argtypes = [ctypes.POINTER(_Rotary), hp, hp, hp] + [vp] * 5 + [hp, hp, hp, vp]
+        lib.moe_rotary_workspace_bytes.argtypes = [ctypes.POINTER(_Rotary), ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_rotary_bwd.argtypes = [ctypes.POINTER(_Rotary), hp, hp, hp, hp] + [vp] * 4 + [hp, hp] + [vp] * 4
+        lib.moe_attn_workspace_bytes.argtypes = [ctypes.POINTER(_Attn), ctypes.POINTER(ctypes.c_size_t)]
+        lib.moe_attn_fwd.argtypes = [ctypes.POINTER(_Attn), hp, hp, hp, hp] + [vp] * 6
+        lib.moe_attn_bwd.argtypes = [ctypes.POINTER(_Attn), hp, hp, hp, hp, hp] + [vp] * 4 + [hp, hp, hp, vp, vp]
         lib.moe_muon_workspace_bytes.argtypes = [ctypes.POINTER(_Muon), ctypes.POINTER(ctypes.c_size_t)]
         lib.moe_muon_step.argtypes = [ctypes.POINTER(_Muon)] + [ctypes.POINTER(vp)] * 4 + [vp] * 3
         lib.moe_plan.argtypes = [ctypes.POINTER(_Planner), vp, ctypes.POINTER(_PlanOut), vp]
@@ -128,7 +150,8 @@ class PythonCall:
         if len(given) != self._n:
             raise TypeError(f"{self._n} positional arguments expected")
         it = iter(given)
-        return self._f(*(a if isinstance(a, int) else self._pointer(next(it), a) for a in self._args))
+        passed = [a if isinstance(a, int) else self._pointer(next(it), a) for a in self._args]       # some keep a structure until the call is over
+        return self._f(*passed)
 
     def _pointer(self, given, arg):
         if arg == "int":
@@ -150,11 +173,13 @@ def _call_type():
     return _call_class
 
 
-def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, name: str) -> Optional[int]:
+def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, name: str, device: int = -1) -> Optional[int]:
     if t is None:
         return None
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: need a contiguous device tensor")
+    if device >= 0 and t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, expected {device}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
     if t.numel() < numel:
@@ -357,6 +382,201 @@ class Norm:
         rc = self._for_rows(dY)[1](dY, S, gamma, mean, rstd, residual_grad, dX, dgamma, dbeta, self.ws.data_ptr(), _stream())
         if rc != 0:
             _checked(rc, "moe_norm_bwd")
+
+
+def _heads(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, heads: int, d: int, name: str, device: int) -> Optional[int]:
+    """The address of a moe_heads_t of a tensor [rows, heads, d] with any strides whose heads are contiguous."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"{name}: need a device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, expected {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != (rows, heads, d):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, heads, d)}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: a head's elements have to lie beside each other")
+    return _Address(_Heads(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def _argument(given, *said) -> Optional[int]:
+    """The check of a call's tensor: what is said of it are _heads' arguments or _ptr's."""
+    return _heads(given, *said) if len(said) == 6 else _ptr(given, *said)
+
+
+def _device_index(device) -> int:
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device {device}: a GPU is needed")
+    return device.index if device.index is not None else 0
+
+
+def _on_device(index: int) -> int:
+    """The current stream, which has to be one of the object's device: kernels are launched on the current one."""
+    if _current_device is not None:
+        current = _current_device()
+    else:
+        current = torch.cuda.current_device()
+    if current != index:
+        raise ValueError(f"the current device is {current}, this object's is {index}")
+    return _stream()
+
+
+class _PerShape:
+    """Call objects kept by the sizes that they pass on."""
+
+    MAX_CALLS = 64
+
+    def __init__(self):
+        self._calls: Dict[tuple, object] = {}
+
+    def get(self, key, entry: str, make):
+        call = self._calls.get(key)
+        if call is None:
+            if len(self._calls) >= self.MAX_CALLS:
+                self._calls.clear()
+            call = self._calls[key] = _call_type()(_entry(entry), make(), _argument)
+        return call
+
+
+def rotary_frequencies(rot: int, base: float = 10000.0, *, factor: float = 1.0, trained: Optional[int] = None, fast: float = 32.0, slow: float = 1.0,
+                       device="cuda:0") -> torch.Tensor:
+    """Radians a position of each of the rot / 2 pairs, base^(-2i / rot), in 64 bits, as Rotary takes them.  For contexts longer than the model was trained on: all of them
+    divided by `factor` (positions as if they lay closer) or, with `trained` positions, those that turn fewer than `slow` times in them divided, those of more
+    than `fast` turns left alone, and between the two by parts."""
+    if rot < 0 or rot % 2:
+        raise ValueError(f"rot: {rot} columns are no pairs")
+    if not (base > 0.0 and factor > 0.0):
+        raise ValueError("base and factor have to be positive")
+    f = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1))
+    if trained is None:
+        f = f / factor
+    else:
+        if not fast > slow:
+            raise ValueError("fast has to be more turns than slow")
+        keep = ((trained * f / (2.0 * math.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
+        f = f * keep + f / factor * (1.0 - keep)
+    return f.to(device)
+
+
+class Rotary:
+    """Norm (with norm=True) and rotation of the heads of queries and keys (moe_rotary_fwd, moe_rotary_bwd), with the workspace of the backward pass.  Tensors are
+    [rows, heads, d] of any strides whose heads are contiguous and lie at multiples of 16 bytes, say views of a projection's output.
+
+    bwd() calls of one object share the workspace: they belong on one stream, or behind each other by events; what runs beside each other takes an object
+    each.  fwd() uses none."""
+
+    def __init__(self, *, heads: int, kv_heads: int, d: int, dtype: str, rot: Optional[int] = None, interleaved: bool = False, norm: bool = False, eps: float = 1e-6,
+                 amplitude: float = 1.0, device="cuda:0", alloc_workspace: bool = True):
+        self.lib = load()
+        self.heads, self.kv_heads, self.d = (_int32(v, name) for v, name in ((heads, "heads"), (kv_heads, "kv_heads"), (d, "d")))
+        self.rot = self.d if rot is None else _int32(rot, "rot")
+        self.elt, self.norm = TORCH_DTYPE[DTYPES[dtype]], bool(norm)
+        self._rest = (self.heads, self.kv_heads, self.d, self.rot, int(bool(interleaved)), int(self.norm), DTYPES[dtype], eps, amplitude)
+        n = ctypes.c_size_t()
+        _checked(self.lib.moe_rotary_workspace_bytes(ctypes.byref(_Rotary(0, *self._rest, 0)), ctypes.byref(n)), "moe_rotary_workspace_bytes")
+        self.workspace_bytes = n.value
+        self._index = _device_index(device)
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+        self._calls = _PerShape()
+
+    def _parts(self, rows: int):
+        i, f = self._index, torch.float32
+        head = lambda n, name, r=rows: (self.elt, r, n, self.d, name, i)  # noqa: E731
+        return head, lambda name: (f, self.d, name, i), (torch.int32, rows, "positions", i), (torch.float64, self.rot // 2, "frequencies", i)
+
+    def _fwd(self, rows: int, out_rows: int):
+        head, vector, positions, frequencies = self._parts(rows)
+        return (_Address(_Rotary(rows, *self._rest, out_rows)), head(self.heads, "Q"), head(self.kv_heads, "K"), head(self.kv_heads, "V"), vector("gamma_q"),
+                vector("gamma_k"), positions, frequencies, (torch.int32, rows, "slots", self._index), head(self.heads, "Qo"), head(self.kv_heads, "Ko", out_rows),
+                head(self.kv_heads, "Vo", out_rows), "int")
+
+    def _bwd(self, rows: int):
+        head, vector, positions, frequencies = self._parts(rows)
+        return (_Address(_Rotary(rows, *self._rest, 0)), head(self.heads, "dQo"), head(self.kv_heads, "dKo"), head(self.heads, "Q"), head(self.kv_heads, "K"),
+                vector("gamma_q"), vector("gamma_k"), positions, frequencies, head(self.heads, "dQ"), head(self.kv_heads, "dK"), vector("dgamma_q"),
+                vector("dgamma_k"), "int", "int")
+
+    def fwd(self, Q, K, positions, frequencies, Qo, Ko, *, gamma_q=None, gamma_k=None, V=None, Vo=None, slots=None):
+        """With slots, Ko and Vo are caches: row r's keys and values go to their row slots[r], or nowhere where it is negative."""
+        rows, out_rows = Q.shape[0], Q.shape[0] if slots is None else Ko.shape[0]
+        call = self._calls.get((rows, out_rows, 0), "moe_rotary_fwd", lambda: self._fwd(_int32(rows, "rows"), _int32(out_rows, "rows of Ko")))
+        rc = call(Q, K, V, gamma_q, gamma_k, positions, frequencies, slots, Qo, Ko, Vo, _on_device(self._index))
+        if rc != 0:
+            _checked(rc, "moe_rotary_fwd")
+
+    def bwd(self, dQo, dKo, positions, frequencies, dQ, dK, *, Q=None, K=None, gamma_q=None, gamma_k=None, dgamma_q=None, dgamma_k=None):
+        if self.ws is None:
+            raise ValueError("no workspace attached")
+        rows = dQo.shape[0]
+        call = self._calls.get((rows, 0, 1), "moe_rotary_bwd", lambda: self._bwd(_int32(rows, "rows")))
+        rc = call(dQo, dKo, Q, K, gamma_q, gamma_k, positions, frequencies, dQ, dK, dgamma_q, dgamma_k, self.ws.data_ptr(), _on_device(self._index))
+        if rc != 0:
+            _checked(rc, "moe_rotary_bwd")
+
+
+class Attention:
+    """Attention of packed sequences (moe_attn_fwd, moe_attn_bwd), with a workspace for calls of up to `rows` query rows, `k_rows` rows of keys and `seqs` sequences.
+    Tensors are [rows, heads, d] of any strides whose heads are contiguous and lie at multiples of 16 bytes.
+
+    Calls of one object share the workspace: they belong on one stream, or behind each other by events; what runs beside each other takes an object
+    each."""
+
+    def __init__(self, *, heads: int, kv_heads: int, d: int, dtype: str, rows: int, seqs: int, k_rows: Optional[int] = None, causal: bool = True,
+                 scale: Optional[float] = None, device="cuda:0", alloc_workspace: bool = True):
+        self.lib = load()
+        self.heads, self.kv_heads, self.d = (_int32(v, name) for v, name in ((heads, "heads"), (kv_heads, "kv_heads"), (d, "d")))
+        self.rows, self.k_rows, self.seqs = _int32(rows, "rows"), _int32(rows if k_rows is None else k_rows, "k_rows"), _int32(seqs, "seqs")
+        self.elt = TORCH_DTYPE[DTYPES[dtype]]
+        if scale is None:
+            scale = max(self.d, 1) ** -0.5
+        self._rest = (self.heads, self.kv_heads, self.d, DTYPES[dtype], int(bool(causal)), scale)
+        n = ctypes.c_size_t()
+        _checked(self.lib.moe_attn_workspace_bytes(ctypes.byref(_Attn(self.rows, self.k_rows, self.seqs, *self._rest)), ctypes.byref(n)), "moe_attn_workspace_bytes")
+        self.workspace_bytes = n.value
+        self._index = _device_index(device)
+        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+        self._calls = _PerShape()
+
+    def _spec(self, rows: int, k_rows: int, seqs: int, back: bool):
+        for name, n, most in (("rows", rows, self.rows), ("k_rows", k_rows, self.k_rows), ("seqs", seqs, self.seqs)):
+            if not 0 <= n <= most:
+                raise ValueError(f"{name}: {n}, this object's workspace is for up to {most}")
+        i = self._index
+        q = lambda name: (self.elt, rows, self.heads, self.d, name, i)  # noqa: E731
+        k = lambda name: (self.elt, k_rows, self.kv_heads, self.d, name, i)  # noqa: E731
+        i32 = lambda n, name: (torch.int32, n, name, i)  # noqa: E731
+        lse, where = (torch.float32, self.heads * rows, "lse", i), (i32(seqs + 1, "offsets"), i32(seqs, "k_begin"), i32(seqs, "k_end"))
+        cfg = _Address(_Attn(rows, k_rows, seqs, *self._rest))
+        if back:
+            return (cfg, q("dO"), q("Q"), k("K"), k("V"), q("O"), lse, *where, q("dQ"), k("dK"), k("dV"), "int", "int")
+        return (cfg, q("Q"), k("K"), k("V"), q("O"), lse, *where, "int", "int")
+
+    def _call(self, entry: str, Q, K, offsets, k_begin, k_end):
+        if self.ws is None:
+            raise ValueError("no workspace attached")
+        if (k_begin is None) != (k_end is None):
+            raise ValueError("k_begin and k_end: both or neither")
+        rows, k_rows, seqs = Q.shape[0], K.shape[0], offsets.shape[0] - 1
+        call = self._calls.get((rows, k_rows, seqs, entry), entry, lambda: self._spec(rows, k_rows, seqs, entry == "moe_attn_bwd"))
+        if k_begin is None and rows != k_rows:
+            raise ValueError(f"{k_rows} rows of keys for {rows} of queries: k_begin and k_end say where they lie")
+        return call
+
+    def fwd(self, Q, K, V, O, offsets, *, k_begin=None, k_end=None, lse=None):
+        """offsets[seqs + 1]: where each sequence's queries begin and the last one's end; its keys lie there too, or at k_begin .. k_end."""
+        call = self._call("moe_attn_fwd", Q, K, offsets, k_begin, k_end)
+        rc = call(Q, K, V, O, lse, offsets, k_begin, k_end, self.ws.data_ptr(), _on_device(self._index))
+        if rc != 0:
+            _checked(rc, "moe_attn_fwd")
+
+    def bwd(self, dO, Q, K, V, O, lse, offsets, dQ, dK, dV, *, k_begin=None, k_end=None):
+        call = self._call("moe_attn_bwd", Q, K, offsets, k_begin, k_end)
+        rc = call(dO, Q, K, V, O, lse, offsets, k_begin, k_end, dQ, dK, dV, self.ws.data_ptr(), _on_device(self._index))
+        if rc != 0:
+            _checked(rc, "moe_attn_bwd")
 
 
 class Muon:

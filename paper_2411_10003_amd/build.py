@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoehot.so")
 PYCALL = os.path.join(HERE, "_pycall.so")
-UNITS = ["api", "gate", "gate_grad", "route", "rows", "norm", "muon", "plan", "ffn_f32", "ffn_bf16", "noalloc", "calib"]
+UNITS = ["api", "gate", "gate_grad", "route", "rows", "norm", "rotary", "attn", "attn_bwd", "muon", "plan", "ffn_f32", "ffn_bf16", "noalloc", "calib"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

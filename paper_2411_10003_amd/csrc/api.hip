@@ -392,6 +392,136 @@ int moe_norm_bwd(const moe_norm_t* cfg, const void* dY, const void* S, const flo
     return hip_status(launch_norm_bwd(*cfg, dY, S, gamma, mean, rstd, dS, dX, dgamma, dbeta, (float*)ws, (hipStream_t)stream));
 }
 
+// A tensor of rows x heads x d as the kernels take it: strides along a dimension of one are not looked at.  `out`: it is written, so no element may be two.
+static int take_heads(const moe_heads_t* t, int rows, int heads, int d, int size, bool out, moe_heads_t& to)
+{
+    if (!t || (rows > 0 && !t->p)) return MOE_ERR_NULL;
+    const int piece = 16 / size;
+    to.p = t->p;
+    to.row = rows > 1 ? t->row : d;
+    to.head = heads > 1 ? t->head : 0;
+    if (((uintptr_t)t->p & 15) || to.row % piece || to.head % piece) return MOE_ERR_SHAPE;
+    if (to.row < d || to.row >= (1ll << 21) || to.head < 0 || to.head >= (1ll << 42)) return MOE_ERR_SHAPE;
+    if (out && rows > 0) {
+        const bool beside = to.row >= (heads - 1ll) * to.head + d && (heads == 1 || to.head >= d);
+        const bool behind = to.head >= (rows - 1ll) * to.row + d;
+        if (!beside && !behind) return MOE_ERR_SHAPE;
+    }
+    return MOE_OK;
+}
+
+static int check_rotary(const moe_rotary_t* c)
+{
+    if (!c) return MOE_ERR_NULL;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    if (c->rows < 0 || c->rows >= (1 << 30) || c->heads < 1 || c->kv_heads < 1 || c->heads > 65535 || c->kv_heads > 65535 || c->heads + 2 * c->kv_heads > 65535) return MOE_ERR_SHAPE;
+    if (c->d < 8 || c->d > ROTARY_MAX_D || c->d % 8 || c->rot < 0 || c->rot > c->d || c->rot % 2) return MOE_ERR_SHAPE;
+    if ((c->interleaved != 0 && c->interleaved != 1) || (c->norm != 0 && c->norm != 1)) return MOE_ERR_SHAPE;
+    if ((c->norm && (!(c->eps > 0.0f) || !std::isfinite(c->eps))) || !std::isfinite(c->amplitude)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+int moe_rotary_fwd(const moe_rotary_t* cfg, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const float* gamma_q, const float* gamma_k,
+                   const int32_t* positions, const double* frequencies, const int32_t* slots, const moe_heads_t* Qo, const moe_heads_t* Ko,
+                   const moe_heads_t* Vo, void* stream)
+{
+    int rc = check_rotary(cfg);
+    if (rc != MOE_OK) return rc;
+    const moe_rotary_t& c = *cfg;
+    if (!V != !Vo || (c.norm ? !gamma_q || !gamma_k : gamma_q || gamma_k)) return MOE_ERR_NULL;
+    if (c.rot > 0 && ((c.rows > 0 && !positions) || !frequencies)) return MOE_ERR_NULL;
+    if (slots && (c.out_rows < 0 || c.out_rows >= (1 << 30))) return MOE_ERR_SHAPE;
+    const int size = c.dtype == MOE_BF16 ? 2 : 4, out_rows = slots ? c.out_rows : c.rows;
+    moe_heads_t q, k, v, qo, ko, vo;
+    if ((rc = take_heads(Q, c.rows, c.heads, c.d, size, false, q)) != MOE_OK || (rc = take_heads(K, c.rows, c.kv_heads, c.d, size, false, k)) != MOE_OK ||
+        (rc = take_heads(Qo, c.rows, c.heads, c.d, size, true, qo)) != MOE_OK || (rc = take_heads(Ko, out_rows, c.kv_heads, c.d, size, true, ko)) != MOE_OK) return rc;
+    if (V && ((rc = take_heads(V, c.rows, c.kv_heads, c.d, size, false, v)) != MOE_OK || (rc = take_heads(Vo, out_rows, c.kv_heads, c.d, size, true, vo)) != MOE_OK)) return rc;
+    return hip_status(launch_rotary_fwd(c, q, k, V ? &v : nullptr, gamma_q, gamma_k, positions, frequencies, slots, qo, ko, V ? &vo : nullptr, (hipStream_t)stream));
+}
+
+int moe_rotary_workspace_bytes(const moe_rotary_t* cfg, size_t* bytes)
+{
+    const int rc = check_rotary(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!bytes) return MOE_ERR_NULL;
+    *bytes = align256((size_t)ROTARY_PARTIALS * 2 * cfg->d * sizeof(float));
+    return MOE_OK;
+}
+
+int moe_rotary_bwd(const moe_rotary_t* cfg, const moe_heads_t* dQo, const moe_heads_t* dKo, const moe_heads_t* Q, const moe_heads_t* K,
+                   const float* gamma_q, const float* gamma_k, const int32_t* positions, const double* frequencies, const moe_heads_t* dQ,
+                   const moe_heads_t* dK, float* dgamma_q, float* dgamma_k, void* ws, void* stream)
+{
+    int rc = check_rotary(cfg);
+    if (rc != MOE_OK) return rc;
+    const moe_rotary_t& c = *cfg;
+    if (c.norm ? !gamma_q || !gamma_k || !dgamma_q || !dgamma_k : gamma_q || gamma_k || dgamma_q || dgamma_k) return MOE_ERR_NULL;
+    if (c.rot > 0 && ((c.rows > 0 && !positions) || !frequencies)) return MOE_ERR_NULL;
+    const int size = c.dtype == MOE_BF16 ? 2 : 4;
+    moe_heads_t gqo, gko, q, k, gq, gk;
+    if ((rc = take_heads(dQo, c.rows, c.heads, c.d, size, false, gqo)) != MOE_OK || (rc = take_heads(dKo, c.rows, c.kv_heads, c.d, size, false, gko)) != MOE_OK ||
+        (rc = take_heads(dQ, c.rows, c.heads, c.d, size, true, gq)) != MOE_OK || (rc = take_heads(dK, c.rows, c.kv_heads, c.d, size, true, gk)) != MOE_OK) return rc;
+    if (c.norm && ((rc = take_heads(Q, c.rows, c.heads, c.d, size, false, q)) != MOE_OK || (rc = take_heads(K, c.rows, c.kv_heads, c.d, size, false, k)) != MOE_OK)) return rc;
+    if (!ws || misaligned(ws)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_rotary_bwd(c, gqo, gko, c.norm ? &q : nullptr, c.norm ? &k : nullptr, gamma_q, gamma_k, positions, frequencies, gq, gk, dgamma_q, dgamma_k,
+                                        (float*)ws, (hipStream_t)stream));
+}
+
+static int check_attn(const moe_attn_t* c)
+{
+    if (!c) return MOE_ERR_NULL;
+    if (c->dtype != MOE_F32 && c->dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    if (c->q_rows < 0 || c->q_rows >= (1 << 30) || c->k_rows < 0 || c->k_rows >= (1 << 30) || c->seqs < 0 || c->seqs > 65535) return MOE_ERR_SHAPE;
+    if (c->kv_heads < 1 || c->heads < 1 || c->heads > 1024 || c->heads % c->kv_heads || c->d < 8 || c->d > ATTN_MAX_D || c->d % 8) return MOE_ERR_SHAPE;
+    if ((c->causal != 0 && c->causal != 1) || !(c->scale > 0.0f) || !std::isfinite(c->scale)) return MOE_ERR_SHAPE;
+    if (((long long)c->q_rows / 32 + c->seqs) * c->heads >= (1 << 30) || ((long long)c->k_rows / 32 + c->seqs) * c->kv_heads >= (1 << 30)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+int moe_attn_workspace_bytes(const moe_attn_t* cfg, size_t* bytes)
+{
+    const int rc = check_attn(cfg);
+    if (rc != MOE_OK) return rc;
+    if (!bytes) return MOE_ERR_NULL;
+    *bytes = attn_workspace_bytes(*cfg);
+    return MOE_OK;
+}
+
+int moe_attn_fwd(const moe_attn_t* cfg, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const moe_heads_t* O, float* lse,
+                 const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, void* ws, void* stream)
+{
+    int rc = check_attn(cfg);
+    if (rc != MOE_OK) return rc;
+    const moe_attn_t& c = *cfg;
+    if ((c.seqs > 0 && !offsets) || !k_begin != !k_end) return MOE_ERR_NULL;
+    if (!k_begin && offsets) k_begin = offsets, k_end = offsets + 1;
+    const int size = c.dtype == MOE_BF16 ? 2 : 4;
+    moe_heads_t q, k, v, o;
+    if ((rc = take_heads(Q, c.q_rows, c.heads, c.d, size, false, q)) != MOE_OK || (rc = take_heads(K, c.k_rows, c.kv_heads, c.d, size, false, k)) != MOE_OK ||
+        (rc = take_heads(V, c.k_rows, c.kv_heads, c.d, size, false, v)) != MOE_OK || (rc = take_heads(O, c.q_rows, c.heads, c.d, size, true, o)) != MOE_OK) return rc;
+    if (!ws || misaligned(ws)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_attn_fwd(c, q, k, v, o, lse, offsets, k_begin, k_end, ws, (hipStream_t)stream));
+}
+
+int moe_attn_bwd(const moe_attn_t* cfg, const moe_heads_t* dO, const moe_heads_t* Q, const moe_heads_t* K, const moe_heads_t* V, const moe_heads_t* O,
+                 const float* lse, const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, const moe_heads_t* dQ, const moe_heads_t* dK,
+                 const moe_heads_t* dV, void* ws, void* stream)
+{
+    int rc = check_attn(cfg);
+    if (rc != MOE_OK) return rc;
+    const moe_attn_t& c = *cfg;
+    if ((c.seqs > 0 && !offsets) || !k_begin != !k_end || (c.q_rows > 0 && !lse)) return MOE_ERR_NULL;
+    if (!k_begin && offsets) k_begin = offsets, k_end = offsets + 1;
+    const int size = c.dtype == MOE_BF16 ? 2 : 4;
+    moe_heads_t go, q, k, v, o, gq, gk, gv;
+    if ((rc = take_heads(dO, c.q_rows, c.heads, c.d, size, false, go)) != MOE_OK || (rc = take_heads(Q, c.q_rows, c.heads, c.d, size, false, q)) != MOE_OK ||
+        (rc = take_heads(K, c.k_rows, c.kv_heads, c.d, size, false, k)) != MOE_OK || (rc = take_heads(V, c.k_rows, c.kv_heads, c.d, size, false, v)) != MOE_OK ||
+        (rc = take_heads(O, c.q_rows, c.heads, c.d, size, false, o)) != MOE_OK || (rc = take_heads(dQ, c.q_rows, c.heads, c.d, size, true, gq)) != MOE_OK ||
+        (rc = take_heads(dK, c.k_rows, c.kv_heads, c.d, size, true, gk)) != MOE_OK || (rc = take_heads(dV, c.k_rows, c.kv_heads, c.d, size, true, gv)) != MOE_OK) return rc;
+    if (!ws || misaligned(ws)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_attn_bwd(c, go, q, k, v, o, lse, offsets, k_begin, k_end, gq, gk, gv, ws, (hipStream_t)stream));
+}
+
 static int check_muon(const moe_muon_t* c)
 {
     if (!c) return MOE_ERR_NULL;

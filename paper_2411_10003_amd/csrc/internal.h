@@ -130,6 +130,22 @@ size_t muon_workspace_bytes(const moe_muon_t& c);
 hipError_t launch_muon_step(const moe_muon_t& c, const float* const* grads, float* const* momenta, void* const* weights, uint16_t* const* copies,
                             int32_t* version, void* ws, hipStream_t st);
 
+constexpr int ATTN_MAX_D = 128, ROTARY_MAX_D = 256;
+constexpr int ATTN_PARTS = 2048;       // parts of keys that a forward call of few rows may cut its sequences into, all together
+constexpr int ROTARY_PARTIALS = 512;   // blocks of the rotation's gradient, each with one partial sum of the norms' parameters
+hipError_t launch_rotary_fwd(const moe_rotary_t& c, const moe_heads_t& Q, const moe_heads_t& K, const moe_heads_t* V, const float* gamma_q, const float* gamma_k,
+                             const int32_t* positions, const double* frequencies, const int32_t* slots, const moe_heads_t& Qo, const moe_heads_t& Ko,
+                             const moe_heads_t* Vo, hipStream_t st);
+hipError_t launch_rotary_bwd(const moe_rotary_t& c, const moe_heads_t& dQo, const moe_heads_t& dKo, const moe_heads_t* Q, const moe_heads_t* K,
+                             const float* gamma_q, const float* gamma_k, const int32_t* positions, const double* frequencies, const moe_heads_t& dQ,
+                             const moe_heads_t& dK, float* dgamma_q, float* dgamma_k, float* partial, hipStream_t st);
+size_t attn_workspace_bytes(const moe_attn_t& c);
+hipError_t launch_attn_fwd(const moe_attn_t& c, const moe_heads_t& Q, const moe_heads_t& K, const moe_heads_t& V, const moe_heads_t& O, float* lse,
+                           const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, void* ws, hipStream_t st);
+hipError_t launch_attn_bwd(const moe_attn_t& c, const moe_heads_t& dO, const moe_heads_t& Q, const moe_heads_t& K, const moe_heads_t& V, const moe_heads_t& O,
+                           const float* lse, const int32_t* offsets, const int32_t* k_begin, const int32_t* k_end, const moe_heads_t& dQ, const moe_heads_t& dK,
+                           const moe_heads_t& dV, void* ws, hipStream_t st);
+
 constexpr int SPLIT_UNITS = 320;       // partial tiles the K-split of a last round may need: at most one per block
 constexpr int UNEVEN_UNITS = 512;      // and an uneven cut: two for each of fewer tiles than there are blocks
 constexpr int SPLIT_COUNTERS = 1024;   // a counter for each of them, in the smaller tiles

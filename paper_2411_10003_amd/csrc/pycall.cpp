@@ -3,9 +3,10 @@
 // the forward layer of a tiny model (five calls, 21 tensors) was bound by them.
 //
 // A Call is made from the entry's address and, for each of its arguments (all of them pointers), what stands there: an int, passed
-// on as it is; "int", an int given at the call; or (dtype, numel, name), a tensor given at the call, None for a null pointer.  A
-// tensor that is not plainly fine (of the dtype, contiguous, on the device, large enough) goes to the Python check instead, which
-// raises the error or returns its address.  The call keeps what it was made from: an int that is an object of its own (an address that
+// on as it is; "int", an int given at the call; (dtype, numel, name) or (dtype, numel, name, device), a tensor given at the call, None for a null pointer; or
+// (dtype, rows, heads, d, name, device), a tensor of that shape with strides of its own, passed on as a moe_heads_t.  A
+// tensor that is not plainly fine (of the dtype, contiguous or of the shape, on a device or on that one, large enough) goes to the Python check instead, which
+// raises the error or returns its address (or that of its moe_heads_t, in an int that is kept until the call is over).  The call keeps what it was made from: an int that is an object of its own (an address that
 // keeps the structure it is the address of) lives as long as the call.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -17,12 +18,13 @@
 namespace {
 
 constexpr int MAX_ARGS = 16;
-struct Arg { enum Kind { FIXED, INT, TENSOR } kind; void* fixed; PyObject *dtype, *numel, *name; at::ScalarType type; int64_t least; };   // objects of the spec, which keeps them
+struct Heads { void* p; long long row, head; };            // moe_heads_t
+struct Arg { enum Kind { FIXED, INT, TENSOR, HEADS } kind; void* fixed; PyObject* said; at::ScalarType type; int64_t least, heads, d; int device; };   // said: what stands in the spec, which keeps it
 struct Call {
     PyObject_HEAD
     vectorcallfunc vectorcall;
     void* entry;
-    PyObject* check;                                       // the Python check: (tensor, dtype, numel, name) -> address
+    PyObject* check;                                       // the Python check: the tensor and what is said of it -> address
     PyObject* spec;
     int n, n_given;
     Arg args[MAX_ARGS];
@@ -42,12 +44,19 @@ template <size_t... I> caller caller_of(int n, std::index_sequence<I...>)
 }
 
 // The address of a tensor that is plainly fine.
-bool plain_address(PyObject* o, const Arg& a, void** p)
+bool plain_address(PyObject* o, const Arg& a, void** p, Heads* heads)
 {
     if (!THPVariable_CheckExact(o)) return false;
     try {
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.defined() || !t.is_cuda() || t.scalar_type() != a.type || t.layout() != at::kStrided || !t.is_contiguous() || t.numel() < a.least) return false;
+        if (!t.defined() || !t.is_cuda() || t.scalar_type() != a.type || t.layout() != at::kStrided || (a.device >= 0 && t.get_device() != a.device)) return false;
+        if (a.kind == Arg::HEADS) {
+            if (t.dim() != 3 || t.size(0) != a.least || t.size(1) != a.heads || t.size(2) != a.d || t.stride(2) != 1) return false;
+            *heads = Heads{t.data_ptr(), (long long)t.stride(0), (long long)t.stride(1)};
+            *p = heads;
+            return true;
+        }
+        if (!t.is_contiguous() || t.numel() < a.least) return false;
         *p = t.data_ptr();
         return true;
     } catch (...) {
@@ -63,27 +72,40 @@ PyObject* call_vector(PyObject* self, PyObject* const* given, size_t nargsf, PyO
         return nullptr;
     }
     void* p[MAX_ARGS];
-    for (int i = 0; i < c->n; ++i) {
+    Heads heads[MAX_ARGS];
+    PyObject* kept[MAX_ARGS];                              // structures that a check made
+    int n_kept = 0;
+    bool failed = false;
+    for (int i = 0; i < c->n && !failed; ++i) {
         const Arg& a = c->args[i];
         if (a.kind == Arg::FIXED) { p[i] = a.fixed; continue; }
         PyObject* o = *given++;
-        if (a.kind == Arg::TENSOR) {
+        if (a.kind == Arg::TENSOR || a.kind == Arg::HEADS) {
             if (o == Py_None) { p[i] = nullptr; continue; }
-            if (plain_address(o, a, &p[i])) continue;
-            PyObject* r = PyObject_CallFunctionObjArgs(c->check, o, a.dtype, a.numel, a.name, nullptr);
-            if (!r) return nullptr;
+            if (plain_address(o, a, &p[i], &heads[i])) continue;
+            PyObject* first = PyTuple_Pack(1, o);
+            PyObject* all = first ? PySequence_Concat(first, a.said) : nullptr;
+            Py_XDECREF(first);
+            PyObject* r = all ? PyObject_CallObject(c->check, all) : nullptr;
+            Py_XDECREF(all);
+            if (!r) { failed = true; break; }
+            kept[n_kept++] = r;
             p[i] = r == Py_None ? nullptr : PyLong_AsVoidPtr(r);
-            Py_DECREF(r);
         } else {
             p[i] = PyLong_AsVoidPtr(o);
         }
-        if (!p[i] && PyErr_Occurred()) return nullptr;
+        failed = !p[i] && PyErr_Occurred();
+    }
+    if (failed) {
+        while (n_kept) Py_DECREF(kept[--n_kept]);
+        return nullptr;
     }
     const caller f = caller_of(c->n, std::make_index_sequence<MAX_ARGS + 1>{});
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = f(c->entry, p);
     Py_END_ALLOW_THREADS
+    while (n_kept) Py_DECREF(kept[--n_kept]);
     return PyLong_FromLong(rc);
 }
 
@@ -115,11 +137,16 @@ PyObject* call_new(PyTypeObject* type, PyObject* args, PyObject*)
         if (PyLong_Check(o)) { a.kind = Arg::FIXED; a.fixed = PyLong_AsVoidPtr(o); continue; }
         ++c->n_given;
         if (PyUnicode_Check(o)) { a.kind = Arg::INT; continue; }
-        a.kind = Arg::TENSOR;
-        if (!PyArg_ParseTuple(o, "OOO", &a.dtype, &a.numel, &a.name)) break;
-        if (!THPDtype_Check(a.dtype)) { PyErr_SetString(PyExc_TypeError, "a torch.dtype expected"); break; }
-        a.type = reinterpret_cast<THPDtype*>(a.dtype)->scalar_type;
-        a.least = PyLong_AsLongLong(a.numel);
+        if (!PyTuple_Check(o)) { PyErr_SetString(PyExc_TypeError, "a tuple expected"); break; }
+        a.said = o;
+        a.kind = PyTuple_GET_SIZE(o) == 6 ? Arg::HEADS : Arg::TENSOR;
+        a.device = -1;
+        PyObject *dtype, *name;
+        long long least, n_heads = 0, d = 0;
+        if (a.kind == Arg::HEADS ? !PyArg_ParseTuple(o, "OLLLOi", &dtype, &least, &n_heads, &d, &name, &a.device) : !PyArg_ParseTuple(o, "OLO|i", &dtype, &least, &name, &a.device)) break;
+        if (!THPDtype_Check(dtype)) { PyErr_SetString(PyExc_TypeError, "a torch.dtype expected"); break; }
+        a.type = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+        a.least = least, a.heads = n_heads, a.d = d;
     }
     if (PyErr_Occurred()) { Py_DECREF(c); return nullptr; }
     return reinterpret_cast<PyObject*>(c);

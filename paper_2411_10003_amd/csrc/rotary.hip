@@ -1,0 +1,414 @@
+// Queries and keys on their way from the projection to their products: RMS norm of each head, rotation by the position, and for an answer's tokens the
+// way into the cache, in one pass; and its gradient.
+//
+// forward, per head x of d elements:  x <- x rstd gamma, rstd = 1 / sqrt(sum x^2 / d + eps);  pairs (a, b) of its first `rot` columns
+//   (a, b) <- amplitude (a cos t - b sin t, b cos t + a sin t),  t = position * frequency
+// backward: dy turned back by the same angle, then with xh = x rstd, g = dy gamma:  dx = rstd (g - xh sum g xh / d),  dgamma = sum dy xh
+//
+// Bound by HBM: an element comes and goes once.  A head is shared by TPH threads with two pieces of eight elements each, which stay in registers; where
+// the halves of a head are pairs and whole pieces, a thread has both pieces of its pairs and no word goes between lanes.  Angles are 64-bit products reduced
+// to a turn before they are rounded (a position of 10^6 leaves fp32 two digits of its angle), once per row for all heads, kept in LDS.
+#include "internal.h"
+
+#include <type_traits>
+
+namespace {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = 256, PIECE = 8, MAX_ROWS = 4;      // rows whose angles a block keeps at a time
+
+struct side_t { const char *in, *x; char* out; const float* gamma; int heads; long long in_row, in_head, x_row, x_head, out_row, out_head; };      // strides in bytes
+struct rotary_args {
+    side_t side[3];                                        // queries, keys, values
+    const int32_t *positions, *slots;
+    const double* frequencies;
+    float* partial;                                        // [blocks][2][d], or the parameters' gradients where there is one block
+    float *dgamma_q, *dgamma_k;
+    int rows, d, rot, sides, out_rows, rows_at_once;
+    float eps, amplitude, inv_d;
+};
+
+enum Pairs { NEIGHBOURS, HALVES, HALVES_CUT };             // CUT: a half is no whole number of pieces
+
+template <typename ET, bool NT> __device__ __forceinline__ void load8(const char* p, float* f)
+{
+    if constexpr (sizeof(ET) == 2) {
+        const u32x4 v = load_piece_of<NT>((const u32x4*)p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x4 v = load_piece_of<NT>((const f32x4*)p + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[4 * i + k] = v[k];
+        }
+    }
+}
+template <typename ET, bool NT> __device__ __forceinline__ void store8(char* p, const float* f)
+{
+    if constexpr (sizeof(ET) == 2) {
+        store_piece_of<NT>((u32x4*)p, u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])});
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) store_piece_of<NT>((f32x4*)p + i, f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]});
+    }
+}
+
+// The two pieces of thread c of a head, by their index; one at or past d / 8 is not there.
+template <Pairs PAIRS> __device__ __forceinline__ void pieces_of(int c, int rot, int (&p)[2])
+{
+    const int pairs = PAIRS == HALVES ? rot / (2 * PIECE) : 0;
+    if (PAIRS == HALVES && c < pairs) { p[0] = c; p[1] = c + pairs; }
+    else { p[0] = 2 * c; p[1] = 2 * c + 1; }               // 2 pairs + 2 (c - pairs)
+}
+
+// Turns the pairs among a thread's two pieces; angles: cosines and sines of the row.  BACK: the other way.
+template <Pairs PAIRS, bool BACK>
+__device__ __forceinline__ void turn(float (&v)[2][PIECE], const int (&p)[2], const float2* angles, int rot, float* mine, int c)
+{
+    auto pair = [](float& a, float& b, float2 t) {
+        const float s = BACK ? -t.y : t.y, x = a * t.x - b * s, y = b * t.x + a * s;
+        a = x;
+        b = y;
+    };
+    if constexpr (PAIRS == NEIGHBOURS) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < PIECE / 2; ++i) {
+                const int at = p[u] * (PIECE / 2) + i;
+                if (2 * at < rot) pair(v[u][2 * i], v[u][2 * i + 1], angles[at]);
+            }
+    } else if constexpr (PAIRS == HALVES) {
+        if (p[0] * PIECE * 2 < rot) {
+#pragma unroll
+            for (int i = 0; i < PIECE; ++i) pair(v[0][i], v[1][i], angles[p[0] * PIECE + i]);
+        }
+    } else {
+        // through LDS: a head's threads are lanes of one wave
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < PIECE; ++i) mine[(2 * c + u) * PIECE + i] = v[u][i];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < PIECE; ++i) {
+                const int at = p[u] * PIECE + i;
+                if (at >= rot) continue;
+                const bool low = at < rot / 2;
+                float a = low ? v[u][i] : mine[at - rot / 2], b = low ? mine[at + rot / 2] : v[u][i];
+                pair(a, b, angles[low ? at : at - rot / 2]);
+                v[u][i] = low ? a : b;
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+template <int TPH, int M> __device__ __forceinline__ void head_sums(float (&v)[M])
+{
+#pragma unroll
+    for (int off = TPH / 2; off >= 1; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] += __shfl_xor(v[i], off, 64);
+}
+
+// Cosines and sines, times the amplitude, of `n` rows from `row` on.
+__device__ __forceinline__ void make_angles(const rotary_args& a, int row, int n, float2* angles)
+{
+    const int half = a.rot / 2;
+    for (int i = threadIdx.x; i < n * half; i += THREADS) {
+        const int r = i / half;
+        double t = (double)a.positions[row + r] * a.frequencies[i - r * half] * 0.15915494309189533577;      // in turns
+        t -= rint(t);
+        float s, c;
+        sincospif((float)(2.0 * t), &s, &c);
+        angles[i] = make_float2(c * a.amplitude, s * a.amplitude);
+    }
+}
+
+template <typename ET, int TPH, Pairs PAIRS, bool NORM, bool NT>
+__global__ __launch_bounds__(THREADS) void rotary_kernel(rotary_args a)
+{
+    constexpr int GROUPS = THREADS / TPH;
+    __shared__ float2 angles[MAX_ROWS * ROTARY_MAX_D / 2];
+    __shared__ float patch[PAIRS == HALVES_CUT ? GROUPS * TPH * 2 * PIECE : 1];
+    const int c = threadIdx.x % TPH, group = threadIdx.x / TPH, first = blockIdx.x * a.rows_at_once, n = min(a.rows_at_once, a.rows - first);
+    int p[2];
+    pieces_of<PAIRS>(c, a.rot, p);
+    const bool there[2] = {p[0] * PIECE < a.d, p[1] * PIECE < a.d};
+    // a block has all sides of its rows, or one of them where there are few rows
+    const int side0 = gridDim.y > 1 ? blockIdx.y : 0, side1 = gridDim.y > 1 ? side0 + 1 : a.sides;
+    if (side0 < 2) {
+        make_angles(a, first, n, angles);
+        __syncthreads();
+    }
+    for (int k = side0; k < side1; ++k) {
+        const side_t& s = a.side[k];
+        float gamma[2][PIECE];
+        if (NORM && k < 2)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < PIECE; ++i) gamma[u][i] = there[u] ? s.gamma[p[u] * PIECE + i] : 0.0f;
+        const int items = n * s.heads;
+        for (int i0 = 0; i0 < items; i0 += GROUPS) {
+            const int item = i0 + group;
+            const bool on = item < items;
+            const int r = on ? item / s.heads : 0, h = on ? item - r * s.heads : 0, row = first + r;
+            const char* in = s.in + row * s.in_row + h * s.in_head;
+            float v[2][PIECE];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (on && there[u]) load8<ET, NT>(in + p[u] * PIECE * (int)sizeof(ET), v[u]);
+                else
+#pragma unroll
+                    for (int i = 0; i < PIECE; ++i) v[u][i] = 0.0f;
+            }
+            const int to = k > 0 && a.slots ? a.slots[row] : row;
+            const bool kept = on && (k == 0 || !a.slots || (unsigned)to < (unsigned)a.out_rows);
+            if (k < 2) {
+                if constexpr (NORM) {
+                    float sq[1] = {0.0f};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i) sq[0] = fmaf(v[u][i], v[u][i], sq[0]);
+                    head_sums<TPH>(sq);
+                    const float rstd = 1.0f / sqrtf(sq[0] * a.inv_d + a.eps);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i) v[u][i] *= rstd * gamma[u][i];
+                }
+                turn<PAIRS, false>(v, p, angles + r * (a.rot / 2), a.rot, patch + group * TPH * 2 * PIECE, c);
+            }
+            char* out = s.out + to * s.out_row + h * s.out_head;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (kept && there[u]) store8<ET, NT>(out + p[u] * PIECE * (int)sizeof(ET), v[u]);
+        }
+    }
+}
+
+// The gradient.  Columns stay with their thread from head to head, so the norms' parameters are summed in registers, then over the block's groups in
+// LDS, then over the blocks by a second launch.
+template <typename ET, int TPH, Pairs PAIRS, bool NORM, bool NT>
+__global__ __launch_bounds__(THREADS) void rotary_bwd_kernel(rotary_args a)
+{
+    constexpr int GROUPS = THREADS / TPH;
+    __shared__ float2 angles[MAX_ROWS * ROTARY_MAX_D / 2];
+    __shared__ float patch[PAIRS == HALVES_CUT || NORM ? GROUPS * TPH * 2 * PIECE : 1];
+    const int c = threadIdx.x % TPH, group = threadIdx.x / TPH;
+    int p[2];
+    pieces_of<PAIRS>(c, a.rot, p);
+    const bool there[2] = {p[0] * PIECE < a.d, p[1] * PIECE < a.d};
+    float dg[2][2][PIECE];
+    if constexpr (NORM)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < PIECE; ++i) dg[k][u][i] = 0.0f;
+    for (long long first = (long long)blockIdx.x * a.rows_at_once; first < a.rows; first += (long long)gridDim.x * a.rows_at_once) {
+        const int n = (int)min((long long)a.rows_at_once, a.rows - first);
+        __syncthreads();                                   // the angles of the rows before are done with
+        make_angles(a, (int)first, n, angles);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const side_t& s = a.side[k];
+            float gamma[2][PIECE];
+            if constexpr (NORM)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < PIECE; ++i) gamma[u][i] = there[u] ? s.gamma[p[u] * PIECE + i] : 0.0f;
+            const int items = n * s.heads;
+            for (int i0 = 0; i0 < items; i0 += GROUPS) {
+                const int item = i0 + group;
+                const bool on = item < items;
+                const int r = on ? item / s.heads : 0, h = on ? item - r * s.heads : 0;
+                const long long row = first + r;
+                float v[2][PIECE], x[2][PIECE];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int at = p[u] * PIECE * (int)sizeof(ET);
+                    if (on && there[u]) {
+                        load8<ET, NT>(s.in + row * s.in_row + h * s.in_head + at, v[u]);
+                        if constexpr (NORM) load8<ET, NT>(s.x + row * s.x_row + h * s.x_head + at, x[u]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i) v[u][i] = x[u][i] = 0.0f;
+                    }
+                }
+                turn<PAIRS, true>(v, p, angles + r * (a.rot / 2), a.rot, patch + group * TPH * 2 * PIECE, c);
+                if constexpr (NORM) {
+                    float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i) {
+                            sums[0] = fmaf(x[u][i], x[u][i], sums[0]);
+                            sums[1] = fmaf(v[u][i] * gamma[u][i], x[u][i], sums[1]);
+                        }
+                    head_sums<TPH>(sums);
+                    const float rstd = 1.0f / sqrtf(sums[0] * a.inv_d + a.eps), mid = sums[1] * rstd * a.inv_d;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i) {
+                            const float xh = x[u][i] * rstd;
+                            dg[k][u][i] = fmaf(v[u][i], xh, dg[k][u][i]);
+                            v[u][i] = rstd * (v[u][i] * gamma[u][i] - xh * mid);
+                        }
+                }
+                char* out = s.out + row * s.out_row + h * s.out_head;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (on && there[u]) store8<ET, NT>(out + p[u] * PIECE * (int)sizeof(ET), v[u]);
+            }
+        }
+    }
+    if constexpr (NORM) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (there[u])
+#pragma unroll
+                    for (int i = 0; i < PIECE; ++i) patch[group * a.d + p[u] * PIECE + i] = dg[k][u][i];
+            __syncthreads();
+            float* to = gridDim.x > 1 ? a.partial + ((size_t)blockIdx.x * 2 + k) * a.d : k ? a.dgamma_k : a.dgamma_q;
+            for (int i = threadIdx.x; i < a.d; i += THREADS) {
+                float sum = 0.0f;
+                for (int g = 0; g < GROUPS; ++g) sum += patch[g * a.d + i];
+                to[i] = sum;
+            }
+        }
+    }
+}
+
+// dgamma_q, dgamma_k: sums over the blocks, 16 lines of them side by side.
+__global__ __launch_bounds__(THREADS) void rotary_join_kernel(const float* __restrict__ partial, int blocks, int d, float* __restrict__ dq, float* __restrict__ dk)
+{
+    __shared__ float lines[16][17];
+    const int c = threadIdx.x & 15, line = threadIdx.x >> 4, at = blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (at < 2 * d)
+        for (int b = line; b < blocks; b += 16) sum += partial[(size_t)b * 2 * d + at];
+    lines[line][c] = sum;
+    __syncthreads();
+    if (line == 0 && at < 2 * d) {
+        sum = 0.0f;
+#pragma unroll
+        for (int l = 0; l < 16; ++l) sum += lines[l][c];
+        (at < d ? dq : dk)[at < d ? at : at - d] = sum;
+    }
+}
+
+template <typename F> hipError_t by_head(int d, int rot, int interleaved, F f)
+{
+    auto with = [&](auto TPH) {
+        if (interleaved || rot == 0) return f(TPH, std::integral_constant<Pairs, NEIGHBOURS>{});
+        if (rot % (2 * PIECE) == 0) return f(TPH, std::integral_constant<Pairs, HALVES>{});
+        return f(TPH, std::integral_constant<Pairs, HALVES_CUT>{});
+    };
+    if (d <= 16) return with(std::integral_constant<int, 1>{});
+    if (d <= 32) return with(std::integral_constant<int, 2>{});
+    if (d <= 64) return with(std::integral_constant<int, 4>{});
+    if (d <= 128) return with(std::integral_constant<int, 8>{});
+    return with(std::integral_constant<int, 16>{});
+}
+
+inline side_t make_side(const moe_heads_t* in, const moe_heads_t* x, const moe_heads_t* out, const float* gamma, int heads, int size)
+{
+    side_t s = {};
+    s.in = (const char*)in->p, s.in_row = in->row * size, s.in_head = in->head * size;
+    if (x) s.x = (const char*)x->p, s.x_row = x->row * size, s.x_head = x->head * size;
+    s.out = (char*)out->p, s.out_row = out->row * size, s.out_head = out->head * size;
+    s.gamma = gamma, s.heads = heads;
+    return s;
+}
+
+inline rotary_args make_args(const moe_rotary_t& c, const int32_t* positions, const double* frequencies)
+{
+    rotary_args a = {};
+    a.positions = positions, a.frequencies = frequencies;
+    a.rows = c.rows, a.d = c.d, a.rot = c.rot, a.out_rows = c.out_rows;
+    a.eps = c.eps, a.amplitude = c.amplitude, a.inv_d = 1.0f / (float)c.d;
+    return a;
+}
+
+inline bool streams_rows(const moe_rotary_t& c, int size) { return streams((size_t)c.rows * (c.heads + c.kv_heads) * c.d * size); }
+
+}  // namespace
+
+hipError_t launch_rotary_fwd(const moe_rotary_t& c, const moe_heads_t& Q, const moe_heads_t& K, const moe_heads_t* V, const float* gamma_q, const float* gamma_k,
+                             const int32_t* positions, const double* frequencies, const int32_t* slots, const moe_heads_t& Qo, const moe_heads_t& Ko,
+                             const moe_heads_t* Vo, hipStream_t st)
+{
+    if (c.rows == 0) return hipSuccess;
+    const int size = c.dtype == MOE_BF16 ? 2 : 4;
+    rotary_args a = make_args(c, positions, frequencies);
+    a.slots = slots;
+    a.side[0] = make_side(&Q, nullptr, &Qo, gamma_q, c.heads, size);
+    a.side[1] = make_side(&K, nullptr, &Ko, gamma_k, c.kv_heads, size);
+    a.sides = 2;
+    if (V) a.side[a.sides++] = make_side(V, nullptr, Vo, nullptr, c.kv_heads, size);
+    const bool few = c.rows <= 1024;
+    a.rows_at_once = few ? 1 : MAX_ROWS;
+    const dim3 grid((unsigned)((c.rows + a.rows_at_once - 1) / a.rows_at_once), few ? a.sides : 1);
+    return by_head(c.d, c.rot, c.interleaved, [&](auto TPH, auto PAIRS) {
+        auto go = [&](auto ET, auto NORM, auto NT) {
+            hipLaunchKernelGGL((rotary_kernel<decltype(ET), decltype(TPH)::value, decltype(PAIRS)::value, decltype(NORM)::value, decltype(NT)::value>), grid, dim3(THREADS), 0, st, a);
+            return hipGetLastError();
+        };
+        const bool nt = streams_rows(c, size);
+        auto typed = [&](auto ET) {
+            if (c.norm) return nt ? go(ET, std::true_type{}, std::true_type{}) : go(ET, std::true_type{}, std::false_type{});
+            return nt ? go(ET, std::false_type{}, std::true_type{}) : go(ET, std::false_type{}, std::false_type{});
+        };
+        return size == 2 ? typed(bf16_t{}) : typed(float{});
+    });
+}
+
+hipError_t launch_rotary_bwd(const moe_rotary_t& c, const moe_heads_t& dQo, const moe_heads_t& dKo, const moe_heads_t* Q, const moe_heads_t* K,
+                             const float* gamma_q, const float* gamma_k, const int32_t* positions, const double* frequencies, const moe_heads_t& dQ,
+                             const moe_heads_t& dK, float* dgamma_q, float* dgamma_k, float* partial, hipStream_t st)
+{
+    const int size = c.dtype == MOE_BF16 ? 2 : 4;
+    rotary_args a = make_args(c, positions, frequencies);
+    a.side[0] = make_side(&dQo, Q, &dQ, gamma_q, c.heads, size);
+    a.side[1] = make_side(&dKo, K, &dK, gamma_k, c.kv_heads, size);
+    a.sides = 2;
+    a.partial = partial, a.dgamma_q = dgamma_q, a.dgamma_k = dgamma_k;
+    int blocks = 0;
+    hipError_t e = hipSuccess;
+    if (c.rows > 0) {
+        a.rows_at_once = c.rows <= 2048 ? 1 : MAX_ROWS;
+        const long long all = (c.rows + a.rows_at_once - 1) / a.rows_at_once;
+        blocks = (int)(all < ROTARY_PARTIALS || !c.norm ? all : ROTARY_PARTIALS);
+        e = by_head(c.d, c.rot, c.interleaved, [&](auto TPH, auto PAIRS) {
+            auto go = [&](auto ET, auto NORM, auto NT) {
+                hipLaunchKernelGGL((rotary_bwd_kernel<decltype(ET), decltype(TPH)::value, decltype(PAIRS)::value, decltype(NORM)::value, decltype(NT)::value>), dim3(blocks), dim3(THREADS), 0, st, a);
+                return hipGetLastError();
+            };
+            const bool nt = streams_rows(c, size);
+            auto typed = [&](auto ET) {
+                if (c.norm) return nt ? go(ET, std::true_type{}, std::true_type{}) : go(ET, std::true_type{}, std::false_type{});
+                return nt ? go(ET, std::false_type{}, std::true_type{}) : go(ET, std::false_type{}, std::false_type{});
+            };
+            return size == 2 ? typed(bf16_t{}) : typed(float{});
+        });
+    }
+    if (e != hipSuccess || !c.norm || blocks == 1) return e;
+    hipLaunchKernelGGL(rotary_join_kernel, dim3((2 * c.d + 15) / 16), dim3(THREADS), 0, st, partial, blocks, c.d, dgamma_q, dgamma_k);
+    return hipGetLastError();
+}

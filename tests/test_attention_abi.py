@@ -1,0 +1,191 @@
+"""moe_rotary_* and moe_attn_* check their arguments on the host before anything is launched, and their call objects what they are given (no GPU needed here)."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2411_10003_amd import binding
+
+vp = ctypes.c_void_p
+P = vp(0x10000)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return binding.load()
+
+
+def _heads(p=0x10000, row=4 * 64, head=64):
+    return ctypes.byref(binding._Heads(p, row, head))
+
+
+def _rotary(rows=8, heads=4, kv=2, d=64, rot=64, interleaved=0, norm=0, dtype=1, eps=1e-6, amplitude=1.0, out=0):
+    return binding._Rotary(rows, heads, kv, d, rot, interleaved, norm, dtype, eps, amplitude, out)
+
+
+def _attn(q=8, k=8, seqs=2, heads=4, kv=2, d=64, dtype=1, causal=1, scale=0.125):
+    return binding._Attn(q, k, seqs, heads, kv, d, dtype, causal, scale)
+
+
+BAD_HEADS = [dict(p=0x10008), dict(row=4 * 64 + 4), dict(row=32), dict(row=0), dict(row=-256), dict(row=1 << 21), dict(head=68), dict(head=-64), dict(head=1 << 42)]
+TWICE = [dict(head=0), dict(head=32), dict(row=3 * 64), dict(row=64, head=64)]         # outputs some of whose elements would be two
+
+
+def test_rotary_forward(lib):
+    def call(c, Q=_heads(), K=_heads(), V=None, gq=None, gk=None, positions=P, frequencies=P, slots=None, Qo=_heads(), Ko=_heads(), Vo=None):
+        return lib.moe_rotary_fwd(ctypes.byref(c) if c is not None else None, Q, K, V, gq, gk, positions, frequencies, slots, Qo, Ko, Vo, None)
+
+    assert call(None) == -1
+    for missing in ("Q", "K", "Qo", "Ko", "positions", "frequencies"):
+        assert call(_rotary(), **{missing: None}) == -1, missing
+    assert call(_rotary(), Q=_heads(p=None)) == -1
+    assert call(_rotary(), V=_heads()) == -1 and call(_rotary(), Vo=_heads()) == -1
+    assert call(_rotary(norm=1)) == -1 and call(_rotary(norm=1), gq=P) == -1 and call(_rotary(), gq=P, gk=P) == -1
+    for bad in (dict(rows=-1), dict(rows=1 << 30), dict(heads=0), dict(kv=0), dict(heads=65535), dict(d=0), dict(d=60), dict(d=264), dict(rot=-2), dict(rot=3), dict(rot=66),
+                dict(interleaved=2), dict(norm=2), dict(norm=1, eps=0.0), dict(norm=1, eps=math.nan), dict(amplitude=math.inf)):
+        assert call(_rotary(**bad), gq=P if bad.get("norm") else None, gk=P if bad.get("norm") else None) == -2, bad
+    assert call(_rotary(dtype=2)) == -5
+    for bad in BAD_HEADS:
+        for which in ("Q", "K", "Qo", "Ko"):
+            assert call(_rotary(), **{which: _heads(**bad)}) == -2, (which, bad)
+    for bad in TWICE:
+        assert call(_rotary(), Qo=_heads(**bad)) == -2, bad
+    assert call(_rotary(out=-1), slots=P) == -2
+    assert call(_rotary(rows=0), Q=_heads(p=None), K=_heads(p=None), Qo=_heads(p=None), Ko=_heads(p=None), positions=None) == 0
+
+
+def test_rotary_backward(lib):
+    def call(c, dQo=_heads(), dKo=_heads(), Q=_heads(), K=_heads(), gq=P, gk=P, positions=P, frequencies=P, dQ=_heads(), dK=_heads(), dgq=P, dgk=P, ws=P):
+        return lib.moe_rotary_bwd(ctypes.byref(c) if c is not None else None, dQo, dKo, Q, K, gq, gk, positions, frequencies, dQ, dK, dgq, dgk, ws, None)
+
+    assert call(None) == -1
+    for missing in ("dQo", "dKo", "Q", "K", "gq", "gk", "positions", "frequencies", "dQ", "dK", "dgq", "dgk"):
+        assert call(_rotary(norm=1), **{missing: None}) == -1, missing
+    assert call(_rotary()) == -1                           # parameters of a norm that is not there
+    assert call(_rotary(norm=1), ws=None) == -4 and call(_rotary(norm=1), ws=vp(0x10010)) == -4
+    for bad in BAD_HEADS:
+        assert call(_rotary(norm=1), dQ=_heads(**bad)) == -2 and call(_rotary(norm=1), K=_heads(**bad)) == -2, bad
+    for bad in TWICE:
+        assert call(_rotary(norm=1), dQ=_heads(**bad)) == -2, bad
+    n = ctypes.c_size_t()
+    assert lib.moe_rotary_workspace_bytes(ctypes.byref(_rotary()), ctypes.byref(n)) == 0 and n.value % 256 == 0 and n.value >= 2 * 64 * 4
+    assert lib.moe_rotary_workspace_bytes(ctypes.byref(_rotary()), None) == -1 and lib.moe_rotary_workspace_bytes(ctypes.byref(_rotary(d=4)), ctypes.byref(n)) == -2
+
+
+def test_attention(lib):
+    def fwd(c, Q=_heads(), K=_heads(), V=_heads(), O=_heads(), lse=P, offsets=P, begin=None, end=None, ws=P):
+        return lib.moe_attn_fwd(ctypes.byref(c) if c is not None else None, Q, K, V, O, lse, offsets, begin, end, ws, None)
+
+    def bwd(c, dO=_heads(), Q=_heads(), K=_heads(), V=_heads(), O=_heads(), lse=P, offsets=P, begin=None, end=None, dQ=_heads(), dK=_heads(), dV=_heads(), ws=P):
+        return lib.moe_attn_bwd(ctypes.byref(c) if c is not None else None, dO, Q, K, V, O, lse, offsets, begin, end, dQ, dK, dV, ws, None)
+
+    for call, tensors, outs in ((fwd, ("Q", "K", "V", "O"), ("O",)), (bwd, ("dO", "Q", "K", "V", "O", "dQ", "dK", "dV"), ("dQ", "dK", "dV"))):
+        assert call(None) == -1
+        for missing in (*tensors, "offsets"):
+            assert call(_attn(), **{missing: None}) == -1, missing
+        assert call(_attn(), begin=P) == -1 and call(_attn(), end=P) == -1
+        for bad in (dict(q=-1), dict(q=1 << 30), dict(k=-1), dict(k=1 << 30), dict(seqs=-1), dict(seqs=65536), dict(heads=0), dict(kv=0), dict(heads=3), dict(heads=1026), dict(d=0),
+                    dict(d=12), dict(d=136), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(q=(1 << 30) - 1, heads=64),
+                    dict(k=(1 << 30) - 1, heads=64, kv=64)):
+            assert call(_attn(**bad)) == -2, bad
+        assert call(_attn(dtype=7)) == -5
+        for which in tensors:
+            for bad in BAD_HEADS:
+                assert call(_attn(), **{which: _heads(**bad)}) == -2, (which, bad)
+        for which in outs:
+            for bad in TWICE:
+                if which in ("dK", "dV") and bad in (dict(row=3 * 64),):
+                    continue                               # two heads: that is room enough
+                assert call(_attn(), **{which: _heads(**bad)}) == -2, (which, bad)
+        assert call(_attn(), ws=None) == -4 and call(_attn(), ws=vp(0x10080)) == -4
+        assert call(_attn(q=0, k=0, seqs=0), offsets=None) == 0
+    assert bwd(_attn(), lse=None) == -1
+    n, more = ctypes.c_size_t(), ctypes.c_size_t()
+    assert lib.moe_attn_workspace_bytes(ctypes.byref(_attn(q=100, heads=8)), ctypes.byref(n)) == 0 and n.value % 256 == 0 and n.value >= 100 * 8 * 4
+    assert lib.moe_attn_workspace_bytes(ctypes.byref(_attn()), None) == -1 and lib.moe_attn_workspace_bytes(ctypes.byref(_attn(d=4)), ctypes.byref(n)) == -2
+    # calls of fewer rows need no more
+    for big, small in ((dict(q=4000, k=90000, seqs=64), dict(q=64, k=90000, seqs=64)), (dict(q=64, k=90000, seqs=64), dict(q=1, k=90000, seqs=1)), (dict(q=3, k=400, seqs=3), dict(q=3, k=400, seqs=1))):
+        for s, to in ((big, n), (small, more)):
+            assert lib.moe_attn_workspace_bytes(ctypes.byref(_attn(**s)), ctypes.byref(to)) == 0
+        assert more.value <= n.value, (big, small)
+
+
+@pytest.mark.parametrize("kind", ["native", "python"])
+def test_call_objects(monkeypatch, kind):
+    """Their number of arguments is the entry point's; tensors that are on no device, of another type, shape or order are refused by name."""
+    if kind == "python":
+        monkeypatch.setattr(binding, "_call_class", binding.PythonCall)
+    else:
+        assert binding._call_type() is not binding.PythonCall
+    lib = binding.load()
+    monkeypatch.setattr(binding, "_on_device", lambda index: 0)
+    r = binding.Rotary(heads=4, kv_heads=2, d=64, dtype="bf16", norm=True, alloc_workspace=False)
+    a = binding.Attention(heads=4, kv_heads=2, d=64, dtype="bf16", rows=8, seqs=2, alloc_workspace=False)
+    assert len(r._fwd(8, 8)) == len(lib.moe_rotary_fwd.argtypes) and len(r._bwd(8)) == len(lib.moe_rotary_bwd.argtypes)
+    assert len(a._spec(8, 8, 2, False)) == len(lib.moe_attn_fwd.argtypes) and len(a._spec(8, 8, 2, True)) == len(lib.moe_attn_bwd.argtypes)
+    q, k = torch.zeros(8, 4, 64, dtype=torch.bfloat16), torch.zeros(8, 2, 64, dtype=torch.bfloat16)
+    pos, f = torch.zeros(8, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
+    with pytest.raises(ValueError, match="Q: need a device tensor"):
+        r.fwd(q, k, pos, f, q, k)
+    with pytest.raises(ValueError, match="no workspace"):
+        r.bwd(q, k, pos, f, q, k)
+    with pytest.raises(ValueError, match="no workspace"):
+        a.fwd(q, k, k, q, torch.zeros(3, dtype=torch.int32))
+    # without tensors the library refuses
+    call = binding._call_type()(binding._entry("moe_rotary_fwd"), r._fwd(8, 8), binding._argument)
+    assert call(*[None] * 11, 0) == -1
+    with pytest.raises(TypeError):
+        call(None)
+    with pytest.raises(AttributeError):
+        call("no tensor", *[None] * 10, 0)
+    call = binding._call_type()(binding._entry("moe_attn_bwd"), a._spec(0, 0, 0, True), binding._argument)
+    assert call(*[None] * 12, 0, 0) == -1
+
+
+def test_checks_of_a_tensor_of_heads(monkeypatch):
+    class Device(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 1
+
+    t = torch.zeros(8, 4, 64, dtype=torch.bfloat16).as_subclass(Device)
+    ok = (torch.bfloat16, 8, 4, 64, "Q", 1)
+    at = binding._heads(t, *ok)
+    assert (at.struct.p, at.struct.row, at.struct.head) == (t.data_ptr(), 256, 64)
+    assert binding._heads(None, *ok) is None
+    for said, what in (((torch.bfloat16, 8, 4, 64, "Q", 0), "device 1"), ((torch.float32, 8, 4, 64, "Q", 1), "dtype"), ((torch.bfloat16, 7, 4, 64, "Q", 1), "shape"),
+                       ((torch.bfloat16, 8, 64, 4, "Q", 1), "shape")):
+        with pytest.raises(ValueError, match=what):
+            binding._heads(t, *said)
+    with pytest.raises(ValueError, match="beside each other"):
+        binding._heads(t.transpose(1, 2), torch.bfloat16, 8, 64, 4, "Q", 1)
+    with pytest.raises(ValueError, match="on device 1, expected 0"):
+        binding._ptr(t, torch.bfloat16, 1, "gamma", 0)
+
+
+def test_the_current_device(monkeypatch):
+    monkeypatch.setattr(binding, "_stream", lambda: 4711)
+    for n in (0, 1):
+        monkeypatch.setattr(binding, "_current_device", lambda: n)
+        if n == 0:
+            assert binding._on_device(0) == 4711
+        else:
+            with pytest.raises(ValueError, match="current device"):
+                binding._on_device(0)
+    with pytest.raises(ValueError):
+        binding._device_index("cpu")
+    assert binding._device_index("cuda") == 0 and binding._device_index("cuda:3") == 3
+
+
+def test_sizes_that_are_refused():
+    for bad in (dict(heads=2 ** 32 + 4), dict(d=2 ** 32 + 64), dict(rot=2 ** 32)):
+        with pytest.raises(ValueError):
+            binding.Rotary(**{**dict(heads=4, kv_heads=2, d=64, dtype="bf16", alloc_workspace=False), **bad})
+    with pytest.raises(binding.MoeError):
+        binding.Attention(heads=4, kv_heads=3, d=64, dtype="bf16", rows=8, seqs=1, alloc_workspace=False)
+    a = binding.Attention(heads=4, kv_heads=2, d=64, dtype="bf16", rows=8, seqs=1, alloc_workspace=False)
+    for sizes in ((9, 8, 1), (8, 9, 1), (8, 8, 2), (8, 8, -1)):
+        with pytest.raises(ValueError):
+            a._spec(*sizes, False)
