@@ -19,8 +19,23 @@ typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.402823466e38f;
 
-// Lanes 32 apart exchange.
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+// What two lanes that are 32 apart have, in both of them.
+struct Halves { float low, high; };
+__device__ __forceinline__ Halves halves_of(float v)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return Halves{__uint_as_float(both[0]), __uint_as_float(both[1])};
+}
+// The highest of three; a NaN is passed over.  (fmaxf first makes every operand canonical, an instruction each.)
+__device__ __forceinline__ float highest_of(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float sum_of_halves(float v) { const Halves h = halves_of(v); return h.low + h.high; }
+// In a branch that all lanes take together, and rarely: what stands in it is not worked out beside the branch.
+#define RARELY() asm volatile("")
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <typename ET> struct Frag;
@@ -85,33 +100,70 @@ template <typename ET, int DP> struct Tile {
             }
         }
     }
-    // By rows: rows `row0` .. + 31 (a multiple of 32) of the tile at `base`, columns 16 t .. + 15.
-    __device__ __forceinline__ frag by_rows(uint32_t base, int row0, int t) const
+    // A lane's addresses in the tile at `base`; what follows adds constants to them that fit an instruction (the compiler would rather add them to the base and
+    // add the base again for each).
+    struct RowsAt { uint32_t at[T]; };
+    struct KeysAt { uint32_t at[DB][2]; };
+    __device__ __forceinline__ RowsAt rows_at(uint32_t base) const
     {
+        RowsAt r;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            r.at[t] = base + (rows0 ^ (t << (sizeof(ET) == 2 ? 5 : 6)));
+            asm("" : "+v"(r.at[t]));
+        }
+        return r;
+    }
+    __device__ __forceinline__ KeysAt keys_at(uint32_t base) const
+    {
+        KeysAt k;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                k.at[b][u] = base + (keys0[u] ^ (b << (sizeof(ET) == 2 ? 6 : 7)));
+                asm("" : "+v"(k.at[b][u]));
+            }
+        return k;
+    }
+    // By rows: rows `row0` .. + 31 (a multiple of 32) of the tile `beyond` bytes on, columns 16 t .. + 15.
+    static __device__ __forceinline__ frag by_rows(const RowsAt& r, int row0, int t, int beyond = 0)
+    {
+        const int more = row0 * ROW + beyond;
         if constexpr (sizeof(ET) == 2) {
-            return __builtin_bit_cast(frag, *(const LDS_PTR(s16x8))(uintptr_t)(base + row0 * ROW + (rows0 ^ (t << 5))));
+            return __builtin_bit_cast(frag, *(const LDS_PTR(s16x8))(uintptr_t)(r.at[t] + more));
         } else {
-            const uint32_t a = base + row0 * ROW;
-            const f32x4 x = *(const LDS_PTR(f32x4))(uintptr_t)(a + (rows0 ^ (t << 6))), y = *(const LDS_PTR(f32x4))(uintptr_t)(a + (rows0 ^ (t << 6) ^ 16));
+            const f32x4 x = *(const LDS_PTR(f32x4))(uintptr_t)(r.at[t] + more), y = *(const LDS_PTR(f32x4))(uintptr_t)((r.at[t] ^ 16) + more);
             return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
     // By keys: rows `row0` .. + 15 (a multiple of 16), columns 32 db .. + 31.
-    __device__ __forceinline__ frag by_keys(uint32_t base, int row0, int db) const
+    static __device__ __forceinline__ frag by_keys(const KeysAt& k, int row0, int db, int beyond = 0)
     {
-        const uint32_t a = base + row0 * ROW;
+        const int more = row0 * ROW + beyond;
         if constexpr (sizeof(ET) == 2) {
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(a + (keys0[0] ^ (db << 6))));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(a + (keys0[1] ^ (db << 6))));
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(k.at[db][0] + more));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(k.at[db][1] + more));
             return __builtin_bit_cast(frag, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             frag f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = *(const LDS_PTR(float))(uintptr_t)(a + (e & 3) * ROW + (keys0[e >> 2] ^ (db << 7) ^ ((e & 3) << 6)));
+            for (int e = 0; e < 8; ++e) f[e] = *(const LDS_PTR(float))(uintptr_t)((k.at[db][e >> 2] ^ ((e & 3) << 6)) + more + (e & 3) * ROW);
             return f;
         }
     }
 };
+
+__device__ __forceinline__ rsrc_t tile_rsrc(const char* base, uint32_t bytes)
+{
+    const unsigned long long b = (unsigned long long)base;
+    return rsrc_t{(int)(unsigned)b, (int)(unsigned)((b >> 32) & 0xffffull), (int)bytes, 0x00020000};
+}
+// dma16 that reads of LDS may pass: they are of other tiles of the ring, and the barriers keep them on their sides.
+__device__ __forceinline__ void tile_dma(rsrc_t r, uint32_t lds_base, uint32_t voff)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(lds_base), "v"(voff), "s"(r));
+}
 
 // Requests of a tile of ROWS rows, straight into LDS, by WAVES waves: P 16-byte pieces of each lane.  Columns from the head's width on and rows past the
 // sequence arrive as zeros.
@@ -129,17 +181,44 @@ template <typename ET, int DP, int ROWS, int WAVES> struct Request {
             off[i] = piece * 16 < d * (int)sizeof(ET) ? row * row_bytes + piece * 16 : 0xfffffff0u;
         }
     }
-    // rows: how many of the tile's rows, from `first` on, are the sequence's (none and fewer: zeros all over)
+    // rows: how many of the tile's rows, from `first` on, are the sequence's (none and fewer: zeros all over).  ROWS rows of 2^23 bytes at most: 32 bits do.
     __device__ __forceinline__ void operator()(const char* first, int rows, uint32_t row_bytes, int d, uint32_t base, int wave) const
     {
-        const rsrc_t r = make_rsrc(first, rows > 0 ? (long long)(rows < ROWS ? rows - 1 : ROWS - 1) * row_bytes + d * (int)sizeof(ET) : 0);
+        const rsrc_t r = tile_rsrc(first, rows > 0 ? (uint32_t)(rows < ROWS ? rows - 1 : ROWS - 1) * row_bytes + d * (int)sizeof(ET) : 0);
 #pragma unroll
-        for (int i = 0; i < P; ++i) dma16(r, base + (i * WAVES + wave) * 1024, off[i], 0);
+        for (int i = 0; i < P; ++i) tile_dma(r, base + (i * WAVES + wave) * 1024, off[i]);
     }
 };
 
 // Everything a wave asked of LDS has arrived; then the block meets.
 #define LDS_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
+
+// What was loaded into registers has arrived: said here once, or the compiler waits for it, and for every request since, each time around a loop that uses it.
+template <typename T, int N> __device__ __forceinline__ void arrived(const T (&v)[N])
+{
+#ifdef __HIP_DEVICE_COMPILE__                              // the host's pass knows no registers of this width
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" :: "v"(v[i]));
+#endif
+}
+
+// The two halves of a block of eight waves work in turn: while the waves of one feed the matrix cores, those of the other, which share their SIMDs, work on
+// scores with the vector units (both at the same time would take the two one after the other).  A phase ends for both at a barrier; what is written before it
+// stays before it.
+#define PHASE_END() do { __builtin_amdgcn_sched_barrier(0); LDS_BARRIER(); __builtin_amdgcn_sched_barrier(0); } while (0)
+
+// The order of a run of N matrix instructions of bf16, the first ROWS of them with a fragment by rows each, the others with one by keys: fragments are
+// requested AHEAD of the instruction that takes them, the first AHEAD before the run.  Left alone the compiler requests each right before it is needed, and the
+// matrix cores wait for LDS every time.  To be called at the end of the run, in the same basic block.
+template <int N, int ROWS, int AHEAD, int I = 0> __device__ __forceinline__ void pace()
+{
+    constexpr int MATRIX = 0x8, LDS_READ = 0x100;
+    if constexpr (I < N) {
+        __builtin_amdgcn_sched_group_barrier(MATRIX, 1, 0);
+        if constexpr (I + AHEAD < N) __builtin_amdgcn_sched_group_barrier(LDS_READ, I + AHEAD < ROWS ? 1 : 2, 0);
+        pace<N, ROWS, AHEAD, I + 1>();
+    }
+}
 
 // Tensors of rows x heads x d: element (r, h, c) lies `row` r + `head` h + c elements from the first; here in bytes.
 struct heads_t {

@@ -2,14 +2,12 @@
 //
 // One pass over the keys with a running maximum and sum.  A wave has 32 queries and all of their results: with S^T = K Q^T a lane holds 16 scores of ONE
 // query per 32 keys, so maximum and sum stay in the lane (its other half is 32 lanes on), and the exponentials are the second operand of O^T = V^T P^T
-// as they lie.  The maximum in use is let go stale by up to 2^8: rescaling the results is rare after the first tiles and exact either way.
+// as they lie.  The maximum in use is let go stale: rescaling the results is rare after the first tiles and exact either way.
 #include "attn.h"
 
 #include <type_traits>
 
 namespace {
-
-constexpr int KEYS = 64;                                   // keys of a tile
 
 // What a wave knows of its 32 queries while it goes over the keys.
 template <typename ET, int DP> struct Rows {
@@ -28,8 +26,13 @@ template <typename ET, int DP> struct Rows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
     }
-    // Scores of NB x 32 keys from row block 0 of the tile at `base`.
-    template <int NB> __device__ __forceinline__ void scores(const tile& t, uint32_t base, f32x16 (&s)[NB]) const
+    // Scores of NB x 32 keys from row block 0 of the tile on; the first PRE fragments, in the order of the products, are there already.
+    template <int NB, int PRE> static __device__ __forceinline__ void request(const typename tile::RowsAt& at, frag (&pre)[PRE])
+    {
+#pragma unroll
+        for (int i = 0; i < PRE; ++i) pre[i] = tile::by_rows(at, 32 * (i % NB), i / NB);
+    }
+    template <int NB, int PRE> __device__ __forceinline__ void scores(const typename tile::RowsAt& at, const frag (&pre)[PRE], f32x16 (&s)[NB]) const
     {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -38,64 +41,82 @@ template <typename ET, int DP> struct Rows {
 #pragma unroll
         for (int k = 0; k < tile::T; ++k)
 #pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] = Frag<ET>::mma(t.by_rows(base, 32 * b, k), q[k], s[b]);
+            for (int b = 0; b < NB; ++b) s[b] = Frag<ET>::mma(k * NB + b < PRE ? pre[k * NB + b < PRE ? k * NB + b : 0] : tile::by_rows(at, 32 * b, k), q[k], s[b]);
     }
     // Keys past `limit` are hidden from this lane's query; `first` is the key of row 0.
     template <int NB> static __device__ __forceinline__ void hide(f32x16 (&s)[NB], int first, int limit, int hi)
     {
+        RARELY();
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = first + 32 * b + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? -INFINITY : s[b][i];
     }
-    // Scores to exponentials under the running maximum.
-    template <int NB> __device__ __forceinline__ void soften(f32x16 (&s)[NB], float scale2)
+    // Exponentials of the scores over the maximum in use, as they go into the products, and their sum.  Only where a lane's sum of them passes STALE (one of them
+    // does, or none of the row's keys came before) is the highest score looked for, the results so far scaled down to it and the exponentials formed again: a
+    // maximum of every tile takes a tenth of the vector instructions.  Scores past fp32's range as exponents end there too.
+    static constexpr float STALE = 1024.0f;
+    template <int NB> __device__ __forceinline__ void soften(const f32x16 (&s)[NB], float scale2, frag (&p)[2 * NB])
     {
-        float top = LOWEST;
+        float now = powers(s, scale2, p);
+        if (__any(now > STALE)) {
+            RARELY();
+            float top = s[0][0];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, other_half(top)) * scale2;
-        if (__any(top > most + 8.0f)) {
-            const float next = fmaxf(most, top), down = exp2_fast(most - next);
+            for (int i = 1; i < 16 * NB; i += 2) top = highest_of(top, s[i / 16][i % 16], s[(i + 1 < 16 * NB ? i + 1 : i) / 16][(i + 1 < 16 * NB ? i + 1 : i) % 16]);
+            const Halves h = halves_of(top);
+            const float next = highest_of(most, h.low * scale2, h.high * scale2), down = exp2_fast(most - next);
             most = next;
             sum *= down;
 #pragma unroll
             for (int b = 0; b < tile::DB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= down;
+            now = powers(s, scale2, p);
         }
+        sum += now;
+    }
+    template <int NB> __device__ __forceinline__ float powers(const f32x16 (&s)[NB], float scale2, frag (&p)[2 * NB]) const
+    {
+        float part[4];                                     // sums side by side: a wave alone on the vector units waits for each it needs at once
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) {
+            f32x16 e;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[b][i] = exp2_fast(fmaf(s[b][i], scale2, -most));
-                sum += s[b][i];
+                e[i] = exp2_fast(fmaf(s[b][i], scale2, -most));
+                part[i & 3] = b == 0 && i < 4 ? e[i] : part[i & 3] + e[i];
             }
+            p[2 * b] = Frag<ET>::pack(e, 0);
+            p[2 * b + 1] = Frag<ET>::pack(e, 1);
+        }
+        return (part[0] + part[1]) + (part[2] + part[3]);
     }
-    template <int NB> __device__ __forceinline__ void add(const tile& t, uint32_t base, const f32x16 (&s)[NB])
+    // Results of the keys whose exponentials are p.
+    template <int N> __device__ __forceinline__ void add(const typename tile::KeysAt& at, const frag (&p)[N])
     {
 #pragma unroll
-        for (int k = 0; k < 2 * NB; ++k) {
-            const frag p = Frag<ET>::pack(s[k >> 1], k & 1);
+        for (int k = 0; k < N; ++k)
 #pragma unroll
-            for (int b = 0; b < tile::DB; ++b) o[b] = Frag<ET>::mma(t.by_keys(base, 16 * k, b), p, o[b]);
-        }
+            for (int b = 0; b < tile::DB; ++b) o[b] = Frag<ET>::mma(tile::by_keys(at, 16 * k, b), p[k], o[b]);
     }
 };
 
-constexpr int stages_for(int stage_bytes) { return 4 * stage_bytes <= 144 * 1024 ? 4 : 2; }
+// Keys of a tile: five tiles of keys and values fit LDS.
+template <typename ET, int DP> constexpr int keys_of() { return DP * (int)sizeof(ET) <= 256 ? 64 : 32; }
+constexpr int STAGES = 5, WAVES = 8, SIDE = WAVES * 32;
+constexpr int AHEAD = 6;                                   // fragments under way
 
-// A block has WAVES x 32 queries of one head; keys and values of 64 rows at a time go through a ring in LDS.
-template <typename ET, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_kernel(attn_args a)
+// A block has 256 queries of one head, 32 a wave; keys and values go through a ring of five tiles in LDS.  In its matrix phase j a wave forms the scores of
+// tile j + 1 and adds tile j's values; in its vector phase the scores become exponentials, and the first fragments of the next matrix phase arrive.
+template <typename ET, int DP>
+__global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
 {
+    constexpr int KEYS = keys_of<ET, DP>(), NB = KEYS / 32;
     typedef Tile<ET, DP> tile;
     typedef Request<ET, DP, KEYS, WAVES> request;
-    constexpr int SIDE = WAVES * 32;
+    typedef typename Frag<ET>::type frag;
     constexpr uint32_t STAGE = 2 * request::BYTES;
-    constexpr int STAGES = stages_for(STAGE);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
@@ -104,7 +125,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_kernel(
     const Sequence s = find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, gridDim.x / a.heads - 1 - slot, lane);      // later tiles see more keys and go first
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.n) return;
     const int shift = s.m - s.n, first = s.tile * SIDE + wave * 32, row = first + col;     // of the sequence's queries
-    // how many keys the block's, this wave's last query sees; the last key that this lane's sees
+    // how many keys the block's, this wave's last query sees; the last key that this lane's, the wave's first sees
     const int block_keys = a.causal ? min(s.m, max(0, min(s.n, (s.tile + 1) * SIDE) + shift)) : s.m;
     const int wave_keys = first >= s.n ? 0 : a.causal ? min(s.m, max(0, min(s.n, first + 32) + shift)) : s.m;
     const int limit = (a.causal ? min(s.m, row + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, first + shift + 1) : s.m) - 1;
@@ -115,10 +136,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_kernel(
     const char* V = row_of(a.V, kv, s.k0);
     const tile t(lane);
     const request ask_k(lane, wave, a.K.row, a.d), ask_v(lane, wave, a.V.row, a.d);
-    auto ask = [&](int j) {
-        const uint32_t at = ring + (j % STAGES) * STAGE;
-        ask_k(K + (long long)j * KEYS * a.K.row, s.m - j * KEYS, a.K.row, a.d, at, wave);
-        ask_v(V + (long long)j * KEYS * a.V.row, s.m - j * KEYS, a.V.row, a.d, at + request::BYTES, wave);
+    int asked = 0, asked_at = 0;                           // rows asked for, and the place of the next ones in the ring
+    auto ask = [&]() {                                     // the next tile; past the last one: zeros that nobody reads
+        const uint32_t at = ring + asked_at;
+        ask_k(K, s.m - asked, a.K.row, a.d, at, wave);
+        ask_v(V, s.m - asked, a.V.row, a.d, at + request::BYTES, wave);
+        K += (long long)KEYS * a.K.row;
+        V += (long long)KEYS * a.V.row;
+        asked += KEYS;
+        asked_at = asked_at == (STAGES - 1) * (int)STAGE ? 0 : asked_at + STAGE;
     };
     Rows<ET, DP> r;
     r.clear();
@@ -129,24 +155,66 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_kernel(
             r.q[k] = row < s.n && 16 * k + 8 * hi < a.d ? Frag<ET>::load(q + (16 * k + 8 * hi) * sizeof(ET)) : Frag<ET>::zero();
     }
     if (tiles > 0) {
-#pragma unroll
-        for (int j = 0; j < STAGES - 1; ++j) ask(j);
-        for (int j = 0; j < tiles; ++j) {
-            WAIT_VMCNT((STAGES - 2) * 2 * request::P);     // tile j has arrived
-            LDS_BARRIER();                                 // everyone's part of it, and nobody reads tile j - 1 any more
-            ask(j + STAGES - 1);                           // past the last tile: zeros that nobody reads
-            if (j >= wave_tiles) continue;
-            const uint32_t at = ring + (j % STAGES) * STAGE;
-            f32x16 x[2];
-            r.scores(t, at, x);
+        constexpr int N = NB * tile::T + 2 * NB * tile::DB, PRE = AHEAD < NB * tile::T ? AHEAD : NB * tile::T;
+        f32x16 x[NB];
+        frag p[2 * NB], pre[PRE];
+        int at = 0, next = STAGE;                          // tile j's place in the ring, and that of the one after it
+        auto step = [&](int& place) { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
+        auto soften = [&](int j) {
             if (j * KEYS + KEYS - 1 > least) r.hide(x, j * KEYS, limit, hi);
-            r.soften(x, a.scale2);
-            r.add(t, at + request::BYTES, x);
+            r.soften(x, a.scale2, p);
+        };
+#pragma unroll
+        for (int j = 0; j < STAGES - 1; ++j) ask();
+        arrived(r.q);
+        WAIT_VMCNT(2 * 2 * request::P);                    // tiles 0 and 1 have arrived
+        PHASE_END();
+        if (wave >= WAVES / 2) PHASE_END();                // the second half is a phase behind
+        if (wave_tiles > 0) {
+            const auto rows = t.rows_at(ring);
+            r.template request<NB>(rows, pre);
+            r.scores(rows, pre, x);
         }
+        PHASE_END();
+        if (wave_tiles > 0) {
+            if (wave_tiles > 1) r.template request<NB>(t.rows_at(ring + next), pre);
+            soften(0);
+        }
+        WAIT_VMCNT(2 * request::P);                        // tile 2
+        PHASE_END();
+        int j = 0;
+        for (; j < wave_tiles - 1; ++j) {
+            const auto rows = t.rows_at(ring + next);
+            const auto keys = t.keys_at(ring + at + request::BYTES);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            r.scores(rows, pre, x);
+            ask();                                         // in the place of tile j - 1, which the second half was done with a phase ago
+            r.add(keys, p);
+            if constexpr (sizeof(ET) == 2) pace<N, NB * tile::T, PRE>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+            WAIT_VMCNT(2 * request::P);                    // tile j + 3 has arrived
+            PHASE_END();
+            step(at);
+            step(next);
+            r.template request<NB>(t.rows_at(ring + next), pre);       // whole tiles, also past the wave's last
+            soften(j + 1);
+            PHASE_END();
+        }
+        for (; j < tiles; ++j) {                           // this wave's last one, and those that only others see
+            ask();
+            if (j < wave_tiles) r.add(t.keys_at(ring + at + request::BYTES), p);
+            WAIT_VMCNT(2 * request::P);
+            PHASE_END();
+            step(at);
+            PHASE_END();
+        }
+        if (wave < WAVES / 2) PHASE_END();
         WAIT_VMCNT(0);
     }
     if (row >= s.n) return;
-    const float sum = r.sum + other_half(r.sum), by = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;     // a row that sees nothing is zero; NaN stays
+    const float sum = sum_of_halves(r.sum), by = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;     // a row that sees nothing is zero; NaN stays
     char* o = a.O.p + (long long)head * a.O.head + (long long)(s.q0 + row) * a.O.row;
 #pragma unroll
     for (int b = 0; b < tile::DB; ++b)
@@ -202,11 +270,12 @@ __device__ __forceinline__ void few_store(const attn_args& a, const Sequence& s,
     store_four<ET>(o + c * sizeof(ET), v0, v1, v2, v3);
 }
 
-template <typename ET, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 1) void attend_few_kernel(attn_args a)
+template <typename ET, int DP, int FEW_WAVES>
+__global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_few_kernel(attn_args a)
 {
     typedef Tile<ET, DP> tile;
     typedef Request<ET, DP, FEW_KEYS, 1> request;
+    typedef typename Frag<ET>::type frag;
     constexpr int PITCH = DP + 4;
     constexpr uint32_t STAGE = 2 * request::BYTES;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -219,6 +288,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_few_kernel(attn_args a)
     const FewRow me = few_row(a, s, kv, col);
     const int shift = s.m - s.n, keys = few_keys(a, s);
     const int limit = (a.causal ? min(s.m, me.token + shift + 1) : s.m) - 1;
+    const int least = (a.causal ? min(s.m, (int)((long long)s.tile * 32 / a.group) + shift + 1) : s.m) - 1;
     const Parts parts(a, keys);
     const int begin = part * parts.chunk, end = min(parts.tiles, begin + parts.chunk);
     if (part >= parts.used) return;
@@ -243,41 +313,45 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attend_few_kernel(attn_args a)
     if (begin + wave < end) {
         ask(begin + wave, 0);
         int at = 0;
-        for (int j = begin + wave; j < end; j += WAVES) {
+        for (int j = begin + wave; j < end; j += FEW_WAVES) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot asked for next has been read
-            ask(j + WAVES, at ^ 1);
+            ask(j + FEW_WAVES, at ^ 1);
             WAIT_VMCNT(2 * request::P);
             f32x16 x[1];
-            r.scores(t, ring + at * STAGE, x);
-            r.hide(x, j * FEW_KEYS, limit, hi);
-            r.soften(x, a.scale2);
-            r.add(t, ring + at * STAGE + request::BYTES, x);
+            frag pre[1];
+            const auto rows = t.rows_at(ring + at * STAGE);
+            r.template request<1>(rows, pre);
+            r.scores(rows, pre, x);
+            if (j * FEW_KEYS + FEW_KEYS - 1 > least) r.hide(x, j * FEW_KEYS, limit, hi);
+            frag p[2];
+            r.soften(x, a.scale2, p);
+            r.add(t.keys_at(ring + at * STAGE + request::BYTES), p);
             at ^= 1;
         }
         WAIT_VMCNT(0);
     }
     LDS_BARRIER();                                         // the rings are done with: each wave's results take their place, a row of PITCH floats a query
     float* mine = reinterpret_cast<float*>(lds);
-    float* sums = mine + WAVES * 32 * PITCH;
+    float* sums = mine + FEW_WAVES * 32 * PITCH;
 #pragma unroll
     for (int b = 0; b < tile::DB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *(f32x4*)&mine[(wave * 32 + col) * PITCH + 32 * b + 8 * i + 4 * hi] = f32x4{r.o[b][4 * i], r.o[b][4 * i + 1], r.o[b][4 * i + 2], r.o[b][4 * i + 3]};
-    const float sum = r.sum + other_half(r.sum);
+    const float sum = sum_of_halves(r.sum);
     if (hi == 0) {
         sums[wave * 64 + col] = r.most;
         sums[wave * 64 + 32 + col] = sum;
     }
     __syncthreads();
     constexpr int QUADS = 32 * DP / 4;
-    for (int i = threadIdx.x; i < QUADS; i += WAVES * 64) {
+    for (int i = threadIdx.x; i < QUADS; i += FEW_WAVES * 64) {
         const int q = i / (DP / 4), c = i % (DP / 4) * 4;
         float most = LOWEST, total = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, sums[w * 64 + q]);
+        for (int w = 0; w < FEW_WAVES; ++w) most = fmaxf(most, sums[w * 64 + q]);
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
+        for (int w = 0; w < FEW_WAVES; ++w) {
             const float down = exp2_fast(sums[w * 64 + q] - most);
             const f32x4 x = *(const f32x4*)&mine[(w * 32 + q) * PITCH + c];
             total = fmaf(sums[w * 64 + 32 + q], down, total);
@@ -328,34 +402,33 @@ __global__ __launch_bounds__(256) void attend_join_kernel(attn_args a)
     }
 }
 
-template <typename ET, int DP, int WAVES> hipError_t launch_rows(const attn_args& a, hipStream_t st)
+template <typename ET, int DP> hipError_t launch_rows(const attn_args& a, hipStream_t st)
 {
-    constexpr int stage = 2 * Request<ET, DP, KEYS, WAVES>::BYTES;
-    constexpr size_t bytes = (size_t)stage * stages_for(stage);
+    constexpr size_t bytes = (size_t)STAGES * 2 * Request<ET, DP, keys_of<ET, DP>(), WAVES>::BYTES;
     static PerDeviceOnce once;
-    const hipError_t e = allow_lds(attend_kernel<ET, DP, WAVES>, bytes, once);
+    const hipError_t e = allow_lds(attend_kernel<ET, DP>, bytes, once);
     if (e != hipSuccess) return e;
-    const long long slots = a.q_rows / (WAVES * 32) + a.seqs;
-    hipLaunchKernelGGL((attend_kernel<ET, DP, WAVES>), dim3((unsigned)(slots * a.heads)), dim3(WAVES * 64), bytes, st, a);
+    const long long slots = a.q_rows / SIDE + a.seqs;
+    hipLaunchKernelGGL((attend_kernel<ET, DP>), dim3((unsigned)(slots * a.heads)), dim3(WAVES * 64), bytes, st, a);
     return hipGetLastError();
 }
 
 template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st)
 {
-    constexpr int WAVES = few_waves<ET, DP>();
-    constexpr size_t ring = (size_t)WAVES * FEW_STAGES * 2 * Request<ET, DP, FEW_KEYS, 1>::BYTES, join = (size_t)WAVES * (32 * (DP + 4) + 64) * 4;
+    constexpr int FEW_WAVES = few_waves<ET, DP>();
+    constexpr size_t ring = (size_t)FEW_WAVES * FEW_STAGES * 2 * Request<ET, DP, FEW_KEYS, 1>::BYTES, join = (size_t)FEW_WAVES * (32 * (DP + 4) + 64) * 4;
     constexpr size_t bytes = ring > join ? ring : join;
     static PerDeviceOnce once;
-    hipError_t e = allow_lds(attend_few_kernel<ET, DP, WAVES>, bytes, once);
+    hipError_t e = allow_lds(attend_few_kernel<ET, DP, FEW_WAVES>, bytes, once);
     if (e != hipSuccess) return e;
     // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do
     const long long units = ((long long)a.q_rows * a.group / 32 + a.seqs) * a.kv_heads;
     const long long tiles = ((long long)a.k_rows / a.seqs + FEW_KEYS - 1) / FEW_KEYS;
-    const long long want = ATTN_PARTS / units, most = (tiles + 2 * WAVES - 1) / (2 * WAVES);
+    const long long want = ATTN_PARTS / units, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);
     a.splits = (int)(want < most ? want : most);
     if (a.splits < 1) a.splits = 1;
-    a.chunk = (int)((tiles / a.splits + WAVES) / WAVES * WAVES);
-    hipLaunchKernelGGL((attend_few_kernel<ET, DP, WAVES>), dim3((unsigned)(units * a.splits)), dim3(WAVES * 64), bytes, st, a);
+    a.chunk = (int)((tiles / a.splits + FEW_WAVES) / FEW_WAVES * FEW_WAVES);
+    hipLaunchKernelGGL((attend_few_kernel<ET, DP, FEW_WAVES>), dim3((unsigned)(units * a.splits)), dim3(FEW_WAVES * 64), bytes, st, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     hipLaunchKernelGGL((attend_join_kernel<ET, DP>), dim3((unsigned)units), dim3(256), 0, st, a);
@@ -366,7 +439,7 @@ template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t
 {
     // few rows: what a kv head has of an average sequence fits one block's 32 twice over
     if ((long long)a.q_rows * a.group <= 64ll * a.seqs) return launch_few<ET, DP>(a, st);
-    return launch_rows<ET, DP, 8>(a, st);
+    return launch_rows<ET, DP>(a, st);
 }
 
 }  // namespace

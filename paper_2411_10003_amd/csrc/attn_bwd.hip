@@ -63,7 +63,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kern
 #pragma unroll
             for (int e = 0; e < 8; ++e) D = fmaf(Frag<ET>::at(dO[k], e), Frag<ET>::at(o, e), D);
         }
-        D += other_half(D);
+        D = sum_of_halves(D);
         const long long at = (long long)head * a.q_rows + s.q0 + row;
         if (row < s.n) {
             lse2 = a.lse[at] * LOG2E;
@@ -78,11 +78,16 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kern
     if (tiles > 0) {
 #pragma unroll
         for (int j = 0; j < STAGES - 1; ++j) ask(j);
+        arrived(q);
+        arrived(dO);
+        asm volatile("" :: "v"(D), "v"(lse2));
         for (int j = 0; j < tiles; ++j) {
             WAIT_VMCNT((STAGES - 2) * 2 * request::P);     // tile j has arrived
             LDS_BARRIER();                                 // everyone's part of it, and nobody reads tile j - 1 any more
             ask(j + STAGES - 1);
             const uint32_t at = ring + (j % STAGES) * STAGE;
+            const auto rows = t.rows_at(at);
+            const auto keys = t.keys_at(at);
 #pragma unroll
             for (int h = 0; h < KEYS / 32; ++h) {
                 const int key = j * KEYS + 32 * h;
@@ -92,20 +97,21 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kern
                 for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < tile::T; ++k) {
-                    x = Frag<ET>::mma(t.by_rows(at, 32 * h, k), q[k], x);
-                    y = Frag<ET>::mma(t.by_rows(at + request::BYTES, 32 * h, k), dO[k], y);
+                    x = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k), q[k], x);
+                    y = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), dO[k], y);
                 }
-                const bool cut = key + 31 > least;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse2)) * (y[i] - D);
-                    if (cut && key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit) x[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse2)) * (y[i] - D);
+                if (key + 31 > least) {
+                    RARELY();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? 0.0f : x[i];
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const frag ds = Frag<ET>::pack(x, k);
 #pragma unroll
-                    for (int b = 0; b < tile::DB; ++b) g[b] = Frag<ET>::mma(t.by_keys(at, 32 * h + 16 * k, b), ds, g[b]);
+                    for (int b = 0; b < tile::DB; ++b) g[b] = Frag<ET>::mma(tile::by_keys(keys, 32 * h + 16 * k, b), ds, g[b]);
                 }
             }
         }
@@ -185,6 +191,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
     if (steps > 0) {
 #pragma unroll
         for (int j = 0; j < STAGES - 1; ++j) ask();
+        arrived(K);
+        arrived(V);
         int j = start, read_at = 0;
         for (int u = 0; u < steps; ++u) {
             WAIT_VMCNT((STAGES - 2) * (2 * request::P + 2));
@@ -192,9 +200,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
             ask();
             const uint32_t at = ring + read_at * STAGE, stats = at + 2 * request::BYTES + wave * 2 * STATS;
             if (++read_at == STAGES) read_at = 0;
+            const auto rows = t.rows_at(at);
+            const auto keys = t.keys_at(at);
             const int tile_first = j * QUERIES;
             if (++j == start + tiles) j = start;
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < QUERIES / 32; ++h) {
                 const int query = tile_first + 32 * h;
                 if (query >= s.n || query + 31 < first - shift && a.causal) continue;
@@ -203,10 +213,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
                 for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < tile::T; ++k) {
-                    x = Frag<ET>::mma(t.by_rows(at, 32 * h, k), K[k], x);
-                    y = Frag<ET>::mma(t.by_rows(at + request::BYTES, 32 * h, k), V[k], y);
+                    x = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k), K[k], x);
+                    y = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), V[k], y);
                 }
-                const bool cut = query < last;
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
                     const uint32_t row = stats + (32 * h + 8 * i4 + 4 * hi) * 4;
@@ -216,7 +225,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
                         const int i = 4 * i4 + e;
                         x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse[e] * LOG2E));
                         y[i] = x[i] * (y[i] - D[e]);
-                        if (cut && query + 8 * i4 + 4 * hi + e < mine) x[i] = y[i] = 0.0f;
+                    }
+                }
+                if (query < last) {
+                    RARELY();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const bool hidden = query + 8 * (i >> 2) + 4 * hi + (i & 3) < mine;
+                        x[i] = hidden ? 0.0f : x[i];
+                        y[i] = hidden ? 0.0f : y[i];
                     }
                 }
 #pragma unroll
@@ -224,8 +241,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
                     const frag p = Frag<ET>::pack(x, k), ds = Frag<ET>::pack(y, k);
 #pragma unroll
                     for (int b = 0; b < tile::DB; ++b) {
-                        dV[b] = Frag<ET>::mma(p, t.by_keys(at + request::BYTES, 32 * h + 16 * k, b), dV[b]);
-                        dK[b] = Frag<ET>::mma(ds, t.by_keys(at, 32 * h + 16 * k, b), dK[b]);
+                        dV[b] = Frag<ET>::mma(p, tile::by_keys(keys, 32 * h + 16 * k, b, request::BYTES), dV[b]);
+                        dK[b] = Frag<ET>::mma(ds, tile::by_keys(keys, 32 * h + 16 * k, b), dK[b]);
                     }
                 }
             }
@@ -280,6 +297,6 @@ hipError_t launch_attn_bwd(const moe_attn_t& c, const moe_heads_t& dO, const moe
     a.dQ = in_bytes(dQ, size), a.dK = in_bytes(dK, size), a.dV = in_bytes(dV, size);
     a.lse = const_cast<float*>(lse), a.D = (float*)ws;
     a.offsets = offsets, a.k_begin = k_begin, a.k_end = k_end;
-    if (c.dtype == MOE_BF16) return c.d <= 64 ? attend_bwd<bf16_t, 64, 4>(a, st) : attend_bwd<bf16_t, 128, 4>(a, st);
+    if (c.dtype == MOE_BF16) return c.d <= 64 ? attend_bwd<bf16_t, 64, 8>(a, st) : attend_bwd<bf16_t, 128, 8>(a, st);
     return c.d <= 64 ? attend_bwd<float, 64, 4>(a, st) : attend_bwd<float, 128, 4>(a, st);
 }
