@@ -207,18 +207,22 @@ template <typename T, int N> __device__ __forceinline__ void arrived(const T (&v
 // stays before it.
 #define PHASE_END() do { __builtin_amdgcn_sched_barrier(0); LDS_BARRIER(); __builtin_amdgcn_sched_barrier(0); } while (0)
 
-// The order of a run of N matrix instructions of bf16, the first ROWS of them with a fragment by rows each, the others with one by keys: fragments are
-// requested AHEAD of the instruction that takes them, the first AHEAD before the run.  Left alone the compiler requests each right before it is needed, and the
-// matrix cores wait for LDS every time.  To be called at the end of the run, in the same basic block.
-template <int N, int ROWS, int AHEAD, int I = 0> __device__ __forceinline__ void pace()
+// The order of a run of N matrix instructions of bf16, instruction i with READS::of(i) requests of LDS: they are under way AHEAD instructions before it, those of
+// the first AHEAD before the run.  Left alone the compiler requests each right before it is needed, and the matrix cores wait for LDS every time.  To be
+// called at the end of the run, in the same basic block.
+template <typename READS, int N, int AHEAD, int I = 0> __device__ __forceinline__ void pace()
 {
     constexpr int MATRIX = 0x8, LDS_READ = 0x100;
     if constexpr (I < N) {
         __builtin_amdgcn_sched_group_barrier(MATRIX, 1, 0);
-        if constexpr (I + AHEAD < N) __builtin_amdgcn_sched_group_barrier(LDS_READ, I + AHEAD < ROWS ? 1 : 2, 0);
-        pace<N, ROWS, AHEAD, I + 1>();
+        if constexpr (I + AHEAD < N)
+            if constexpr (READS::of(I + AHEAD) > 0) __builtin_amdgcn_sched_group_barrier(LDS_READ, READS::of(I + AHEAD), 0);
+        pace<READS, N, AHEAD, I + 1>();
     }
 }
+// A fragment by rows is one request, one by keys two.
+template <int ROWS> struct RowsThenKeys { static constexpr int of(int i) { return i < ROWS ? 1 : 2; } };
+template <int KEYS> struct KeysThenRows { static constexpr int of(int i) { return i < KEYS ? 2 : 1; } };
 
 // Tensors of rows x heads x d: element (r, h, c) lies `row` r + `head` h + c elements from the first; here in bytes.
 struct heads_t {
@@ -228,7 +232,8 @@ struct heads_t {
 };
 struct attn_args {
     heads_t Q, K, V, O, dO, dQ, dK, dV;
-    float *lse, *D;                        // [heads][q_rows]
+    float* lse;                            // [heads][q_rows]
+    float2* stats;                         // [heads][q_rows]: lse log2 e, <dO, O>
     const int32_t *offsets, *k_begin, *k_end;
     int q_rows, k_rows, seqs, heads, kv_heads, group, d, causal, splits, chunk;
     float scale, scale2;                   // scale2 = scale log2 e: exponentials are powers of two

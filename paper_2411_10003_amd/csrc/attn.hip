@@ -191,7 +191,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
             r.scores(rows, pre, x);
             ask();                                         // in the place of tile j - 1, which the second half was done with a phase ago
             r.add(keys, p);
-            if constexpr (sizeof(ET) == 2) pace<N, NB * tile::T, PRE>();
+            if constexpr (sizeof(ET) == 2) pace<RowsThenKeys<NB * tile::T>, N, PRE>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
             WAIT_VMCNT(2 * request::P);                    // tile j + 3 has arrived
@@ -444,13 +444,13 @@ template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t
 
 }  // namespace
 
-// The kept parts of a forward call of few rows, or a row's <dO, O> of a backward call.
+// The kept parts of a forward call of few rows, or the rows' statistics of a backward call.
 size_t attn_workspace_bytes(const moe_attn_t& c)
 {
     const int dp = c.d <= 64 ? 64 : 128;
     const long long units = ((long long)c.q_rows * (c.heads / c.kv_heads) / 32 + c.seqs) * c.kv_heads, each = c.k_rows / (FEW_KEYS * 4) + 1;
     const size_t parts = units < ATTN_PARTS && units * each < ATTN_PARTS ? units * each : ATTN_PARTS;
-    const size_t fwd = parts * (32 * dp + PARTIAL_MORE) * sizeof(float), bwd = (size_t)c.heads * c.q_rows * sizeof(float);
+    const size_t fwd = parts * (32 * dp + PARTIAL_MORE) * sizeof(float), bwd = (size_t)c.heads * c.q_rows * sizeof(float2);
     return ((fwd > bwd ? fwd : bwd) + 256) / 256 * 256;
 }
 

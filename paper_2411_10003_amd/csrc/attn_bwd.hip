@@ -6,26 +6,37 @@
 // the second has 32 keys and goes over the queries of all heads that share them.  Scores and <dO, v> are formed in both, 7 products for the 5 of the formulas.
 #include "attn.h"
 
+#include <type_traits>
+
 namespace {
 
-constexpr int KEYS = 64, QUERIES = 64;                     // rows of a tile
-constexpr int stages_for(int stage_bytes) { return 4 * stage_bytes <= 156 * 1024 ? 4 : 2; }
+constexpr int STAGES = 5, WAVES = 8, SIDE = WAVES * 32;
+constexpr int AHEAD = 4;                                   // matrix instructions whose fragments are under way
 
 // 4 bytes a lane from a buffer into LDS at lds_base + lane * 4.
 __device__ __forceinline__ void dma4(rsrc_t r, uint32_t lds_base, uint32_t voff)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds_base), "v"(voff), "s"(r) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds_base), "v"(voff), "s"(r));
+}
+__device__ __forceinline__ void clear(f32x16& x)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
 }
 
-template <typename ET, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kernel(attn_args a)
+// Keys of a tile of the first kernel: five tiles of keys and values fit LDS.
+template <typename ET, int DP> constexpr int keys_of() { return DP * (int)sizeof(ET) <= 256 ? 64 : 32; }
+
+// A block has 256 queries of one head, 32 a wave.  In its matrix phase j a wave adds tile j - 1's keys to the gradient and forms the scores and <dO, v> of tile j;
+// in its vector phase these become ds.
+template <typename ET, int DP>
+__global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
 {
+    constexpr int KEYS = keys_of<ET, DP>(), NB = KEYS / 32;
     typedef Tile<ET, DP> tile;
     typedef Request<ET, DP, KEYS, WAVES> request;
     typedef typename Frag<ET>::type frag;
-    constexpr int SIDE = WAVES * 32;
     constexpr uint32_t STAGE = 2 * request::BYTES;
-    constexpr int STAGES = stages_for(STAGE);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
@@ -37,17 +48,22 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kern
     const int block_keys = a.causal ? min(s.m, max(0, min(s.n, (s.tile + 1) * SIDE) + shift)) : s.m;
     const int wave_keys = first >= s.n ? 0 : a.causal ? min(s.m, max(0, min(s.n, first + 32) + shift)) : s.m;
     const int limit = (a.causal ? min(s.m, row + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, first + shift + 1) : s.m) - 1;
-    const int tiles = (block_keys + KEYS - 1) / KEYS;
+    const int tiles = (block_keys + KEYS - 1) / KEYS, wave_tiles = (wave_keys + KEYS - 1) / KEYS;
 
     const int kv = head / a.group;
     const char* K = row_of(a.K, kv, s.k0);
     const char* V = row_of(a.V, kv, s.k0);
     const tile t(lane);
     const request ask_k(lane, wave, a.K.row, a.d), ask_v(lane, wave, a.V.row, a.d);
-    auto ask = [&](int j) {
-        const uint32_t at = ring + (j % STAGES) * STAGE;
-        ask_k(K + (long long)j * KEYS * a.K.row, s.m - j * KEYS, a.K.row, a.d, at, wave);
-        ask_v(V + (long long)j * KEYS * a.V.row, s.m - j * KEYS, a.V.row, a.d, at + request::BYTES, wave);
+    int asked = 0, asked_at = 0;                           // rows asked for, and the place of the next ones in the ring
+    auto step = [&](int& place) { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
+    auto ask = [&]() {                                     // the next tile; past the last one: zeros that nobody reads
+        ask_k(K, s.m - asked, a.K.row, a.d, ring + asked_at, wave);
+        ask_v(V, s.m - asked, a.V.row, a.d, ring + asked_at + request::BYTES, wave);
+        K += (long long)KEYS * a.K.row;
+        V += (long long)KEYS * a.V.row;
+        asked += KEYS;
+        step(asked_at);
     };
     frag q[tile::T], dO[tile::T];
     float D = 0.0f, lse2 = 0.0f;
@@ -67,54 +83,97 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dq_kern
         const long long at = (long long)head * a.q_rows + s.q0 + row;
         if (row < s.n) {
             lse2 = a.lse[at] * LOG2E;
-            if (hi == 0) a.D[at] = D;
+            if (hi == 0) a.stats[at] = make_float2(lse2, D);
         }
     }
     f32x16 g[tile::DB];
 #pragma unroll
-    for (int b = 0; b < tile::DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) g[b][i] = 0.0f;
+    for (int b = 0; b < tile::DB; ++b) clear(g[b]);
     if (tiles > 0) {
+        constexpr int BY_KEYS = 2 * NB * tile::DB, N = BY_KEYS + 2 * NB * tile::T, PRE = sizeof(ET) == 4 ? 1 : AHEAD < BY_KEYS ? AHEAD : BY_KEYS;
+        f32x16 x[NB], y[NB];
+        frag ds[2 * NB], pre[PRE];
+        int at = 0;                                        // the place of the tile in hand
+        auto scores = [&](int place) {
+            const auto rows = t.rows_at(ring + place);
 #pragma unroll
-        for (int j = 0; j < STAGES - 1; ++j) ask(j);
-        arrived(q);
-        arrived(dO);
-        asm volatile("" :: "v"(D), "v"(lse2));
-        for (int j = 0; j < tiles; ++j) {
-            WAIT_VMCNT((STAGES - 2) * 2 * request::P);     // tile j has arrived
-            LDS_BARRIER();                                 // everyone's part of it, and nobody reads tile j - 1 any more
-            ask(j + STAGES - 1);
-            const uint32_t at = ring + (j % STAGES) * STAGE;
-            const auto rows = t.rows_at(at);
-            const auto keys = t.keys_at(at);
+            for (int h = 0; h < NB; ++h) {
+                clear(x[h]);
+                clear(y[h]);
+            }
 #pragma unroll
-            for (int h = 0; h < KEYS / 32; ++h) {
-                const int key = j * KEYS + 32 * h;
-                if (key >= wave_keys) break;
-                f32x16 x, y;
+            for (int k = 0; k < tile::T; ++k)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < tile::T; ++k) {
-                    x = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k), q[k], x);
-                    y = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), dO[k], y);
+                for (int h = 0; h < NB; ++h) {
+                    x[h] = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k), q[k], x[h]);
+                    y[h] = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), dO[k], y[h]);
                 }
+        };
+        auto add = [&](const typename tile::KeysAt& keys) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse2)) * (y[i] - D);
+            for (int k = 0; k < 2 * NB; ++k)
+#pragma unroll
+                for (int b = 0; b < tile::DB; ++b) {
+                    const int i = k * tile::DB + b;
+                    g[b] = Frag<ET>::mma(i < PRE ? pre[i < PRE ? i : 0] : tile::by_keys(keys, 16 * k, b), ds[k], g[b]);
+                }
+        };
+        auto soften = [&](int j) {                         // and the first fragments of what comes next
+            const auto keys = t.keys_at(ring + at);
+#pragma unroll
+            for (int i = 0; i < PRE; ++i) pre[i] = tile::by_keys(keys, 16 * (i / tile::DB), i % tile::DB);
+#pragma unroll
+            for (int h = 0; h < NB; ++h) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[h][i] = exp2_fast(fmaf(x[h][i], a.scale2, -lse2)) * (y[h][i] - D);
+                const int key = j * KEYS + 32 * h;
                 if (key + 31 > least) {
                     RARELY();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? 0.0f : x[i];
+                    for (int i = 0; i < 16; ++i) x[h][i] = key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? 0.0f : x[h][i];
                 }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const frag ds = Frag<ET>::pack(x, k);
-#pragma unroll
-                    for (int b = 0; b < tile::DB; ++b) g[b] = Frag<ET>::mma(tile::by_keys(keys, 32 * h + 16 * k, b), ds, g[b]);
-                }
+                ds[2 * h] = Frag<ET>::pack(x[h], 0);
+                ds[2 * h + 1] = Frag<ET>::pack(x[h], 1);
             }
+        };
+#pragma unroll
+        for (int j = 0; j < STAGES - 2; ++j) ask();
+        arrived(q);
+        arrived(dO);
+        WAIT_VMCNT(2 * request::P);                        // tiles 0 and 1 have arrived
+        PHASE_END();
+        if (wave >= WAVES / 2) PHASE_END();                // the second half is a phase behind
+        ask();
+        if (wave_tiles > 0) scores(0);
+        WAIT_VMCNT(2 * request::P);                        // tile 2
+        PHASE_END();
+        if (wave_tiles > 0) soften(0);
+        PHASE_END();
+        int j = 1;
+        for (; j < wave_tiles; ++j) {
+            const auto keys = t.keys_at(ring + at);
+            step(at);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            add(keys);
+            ask();                                         // in the place of tile j - 2, which the second half was done with a phase ago
+            scores(at);
+            if constexpr (sizeof(ET) == 2) pace<KeysThenRows<BY_KEYS>, N, PRE>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+            WAIT_VMCNT(2 * request::P);                    // tile j + 2 has arrived
+            PHASE_END();
+            soften(j);
+            PHASE_END();
         }
+        for (; j <= tiles; ++j) {                          // this wave's last one, and those that only others see
+            ask();
+            if (j == wave_tiles) add(t.keys_at(ring + at));
+            WAIT_VMCNT(2 * request::P);
+            PHASE_END();
+            PHASE_END();
+        }
+        if (wave < WAVES / 2) PHASE_END();
         WAIT_VMCNT(0);
     }
     if (row >= s.n) return;
@@ -135,15 +194,65 @@ template <typename ET> __device__ __forceinline__ void store_one(char* p, float 
     else *(float*)p = v;
 }
 
-template <typename ET, int DP, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_kernel(attn_args a)
+// Scores and <dO, v> of 32 queries (rows) and keys (columns) to p and ds; the queries' statistics lie at `stats`, a pair each.
+__device__ __forceinline__ void weigh(f32x16& x, f32x16& y, uint32_t stats, float scale2, int hi)
 {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const f32x4 of = *(const LDS_PTR(f32x4))(uintptr_t)(stats + (8 * (i >> 2) + 4 * hi + (i & 3)) * 8);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            x[i + e] = exp2_fast(fmaf(x[i + e], scale2, -of[2 * e]));
+            y[i + e] = x[i + e] * (y[i + e] - of[2 * e + 1]);
+        }
+    }
+}
+// Queries before `mine` do not see this lane's key; `first` is the query of row 0.
+__device__ __forceinline__ void hide_queries(f32x16& x, f32x16& y, int first, int mine, int hi)
+{
+    RARELY();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const bool hidden = first + 8 * (i >> 2) + 4 * hi + (i & 3) < mine;
+        x[i] = hidden ? 0.0f : x[i];
+        y[i] = hidden ? 0.0f : y[i];
+    }
+}
+
+template <typename ET> __device__ __forceinline__ void store_keys(const attn_args& a, const Sequence& s, int kv, int row, int c, float dk, float dv)
+{
+    store_one<ET>(a.dK.p + (long long)kv * a.dK.head + (long long)(s.k0 + row) * a.dK.row + c * (int)sizeof(ET), dk * a.scale);
+    store_one<ET>(a.dV.p + (long long)kv * a.dV.head + (long long)(s.k0 + row) * a.dV.row + c * (int)sizeof(ET), dv);
+}
+
+// The queries that a block of keys goes over, head by head of those that share them, ROWS at a time.
+template <int ROWS> struct Walk {
+    int first_head, heads, start, tiles, steps;            // tiles of a head from `start` on, where the first query sees the block's first key
+    int head, tile;                                        // the next one to be asked for
+    __device__ __forceinline__ Walk(const attn_args& a, const Sequence& s, int kv, int block)
+    {
+        first_head = kv * a.group, heads = a.group;
+        const int from = a.causal ? max(0, block - (s.m - s.n)) : 0;
+        start = from / ROWS;
+        tiles = max(0, (s.n + ROWS - 1) / ROWS - start);
+        steps = tiles * heads;
+        head = first_head, tile = start;
+    }
+    __device__ __forceinline__ bool there() const { return head < first_head + heads; }
+    __device__ __forceinline__ void next() { if (++tile == start + tiles) { tile = start; ++head; } }
+};
+
+// fp32: a block has WAVES x 32 keys, keys and values in registers.  Its matrix instructions take eight times as long as those of bf16: what a wave does beside them counts
+// for little.
+template <int DP>
+__global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
+{
+    constexpr int WAVES = 4, SIDE = 128, QUERIES = 64, STAGES = 2;
+    typedef float ET;
     typedef Tile<ET, DP> tile;
     typedef Request<ET, DP, QUERIES, WAVES> request;
     typedef typename Frag<ET>::type frag;
-    constexpr int SIDE = WAVES * 32;
-    constexpr uint32_t STATS = QUERIES * 4, STAGE = 2 * request::BYTES + WAVES * 2 * STATS;      // each wave has the rows' statistics to itself
-    constexpr int STAGES = stages_for(STAGE);
+    constexpr uint32_t STATS = QUERIES * 8, STAGE = 2 * request::BYTES + WAVES * STATS;      // each wave has the rows' statistics to itself
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
@@ -152,25 +261,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
     const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
     const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
-    // the first query that sees the block's first key, this lane's, the wave's last
-    const int from = a.causal ? max(0, block - shift) : 0, mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;
-    const int start = from / QUERIES, tiles = max(0, (s.n + QUERIES - 1) / QUERIES - start), steps = tiles * a.group;
+    const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
 
     const tile t(lane);
     const request ask_q(lane, wave, a.Q.row, a.d), ask_o(lane, wave, a.dO.row, a.d);
-    int next_head = kv * a.group, next = start, slot_at = 0;
-    auto ask = [&]() {                                     // the step after the last one asked for; past the end: zeros that nobody reads
-        const bool there = next_head < (kv + 1) * a.group;
+    Walk<QUERIES> walk(a, s, kv, block);
+    int slot_at = 0;
+    auto ask = [&]() {                                     // past the end: zeros that nobody reads
+        const bool there = walk.there();
         const uint32_t at = ring + slot_at * STAGE;
-        const int h = there ? next_head : kv * a.group, rows = there ? s.n - next * QUERIES : 0;
-        const long long q = s.q0 + (long long)next * QUERIES;
+        const int h = there ? walk.head : walk.first_head, rows = there ? s.n - walk.tile * QUERIES : 0;
+        const long long q = s.q0 + (long long)walk.tile * QUERIES;
         ask_q(row_of(a.Q, h, q), rows, a.Q.row, a.d, at, wave);
         ask_o(row_of(a.dO, h, q), rows, a.dO.row, a.d, at + request::BYTES, wave);
-        const long long stats = (long long)h * a.q_rows + q, bytes = rows > 0 ? min(rows, QUERIES) * 4 : 0;
-        dma4(make_rsrc(a.lse + stats, bytes), at + 2 * request::BYTES + wave * 2 * STATS, lane * 4);
-        dma4(make_rsrc(a.D + stats, bytes), at + 2 * request::BYTES + wave * 2 * STATS + STATS, lane * 4);
-        if (++next == start + tiles) { next = start; ++next_head; }
-        if (++slot_at == STAGES) slot_at = 0;
+        const rsrc_t r = tile_rsrc((const char*)(a.stats + (long long)h * a.q_rows + q), rows > 0 ? min(rows, QUERIES) * 8 : 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) dma4(r, at + 2 * request::BYTES + wave * STATS + i * 256, lane * 4 + i * 256);
+        walk.next();
+        slot_at ^= 1;
     };
     frag K[tile::T], V[tile::T];
     {
@@ -185,57 +293,38 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
     }
     f32x16 dK[tile::DB], dV[tile::DB];
 #pragma unroll
-    for (int b = 0; b < tile::DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dK[b][i] = dV[b][i] = 0.0f;
-    if (steps > 0) {
-#pragma unroll
-        for (int j = 0; j < STAGES - 1; ++j) ask();
+    for (int b = 0; b < tile::DB; ++b) {
+        clear(dK[b]);
+        clear(dV[b]);
+    }
+    if (walk.steps > 0) {
+        ask();
         arrived(K);
         arrived(V);
-        int j = start, read_at = 0;
-        for (int u = 0; u < steps; ++u) {
-            WAIT_VMCNT((STAGES - 2) * (2 * request::P + 2));
+        int j = walk.start;
+        for (int u = 0; u < walk.steps; ++u) {
+            WAIT_VMCNT(0);
             LDS_BARRIER();
+            const uint32_t at = ring + (u & 1) * STAGE, stats = at + 2 * request::BYTES + wave * STATS;
             ask();
-            const uint32_t at = ring + read_at * STAGE, stats = at + 2 * request::BYTES + wave * 2 * STATS;
-            if (++read_at == STAGES) read_at = 0;
             const auto rows = t.rows_at(at);
             const auto keys = t.keys_at(at);
             const int tile_first = j * QUERIES;
-            if (++j == start + tiles) j = start;
+            if (++j == walk.start + walk.tiles) j = walk.start;
 #pragma unroll 1
             for (int h = 0; h < QUERIES / 32; ++h) {
                 const int query = tile_first + 32 * h;
-                if (query >= s.n || query + 31 < first - shift && a.causal) continue;
+                if (query >= s.n || (a.causal && query + 31 < first - shift)) continue;
                 f32x16 x, y;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+                clear(x);
+                clear(y);
 #pragma unroll
                 for (int k = 0; k < tile::T; ++k) {
                     x = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k), K[k], x);
                     y = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), V[k], y);
                 }
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const uint32_t row = stats + (32 * h + 8 * i4 + 4 * hi) * 4;
-                    const f32x4 lse = *(const LDS_PTR(f32x4))(uintptr_t)row, D = *(const LDS_PTR(f32x4))(uintptr_t)(row + STATS);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * i4 + e;
-                        x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse[e] * LOG2E));
-                        y[i] = x[i] * (y[i] - D[e]);
-                    }
-                }
-                if (query < last) {
-                    RARELY();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool hidden = query + 8 * (i >> 2) + 4 * hi + (i & 3) < mine;
-                        x[i] = hidden ? 0.0f : x[i];
-                        y[i] = hidden ? 0.0f : y[i];
-                    }
-                }
+                weigh(x, y, stats + 32 * h * 8, a.scale2, hi);
+                if (query < last) hide_queries(x, y, query, mine, hi);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const frag p = Frag<ET>::pack(x, k), ds = Frag<ET>::pack(y, k);
@@ -252,35 +341,203 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void attend_dkv_ker
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int row = first + 8 * (i >> 2) + 4 * hi + (i & 3);
-        if (row >= s.m) continue;
-        char* pk = a.dK.p + (long long)kv * a.dK.head + (long long)(s.k0 + row) * a.dK.row;
-        char* pv = a.dV.p + (long long)kv * a.dV.head + (long long)(s.k0 + row) * a.dV.row;
 #pragma unroll
-        for (int b = 0; b < tile::DB; ++b) {
-            const int c = 32 * b + col;
-            if (c < a.d) {
-                store_one<ET>(pk + c * sizeof(ET), dK[b][i] * a.scale);
-                store_one<ET>(pv + c * sizeof(ET), dV[b][i]);
-            }
-        }
+        for (int b = 0; b < tile::DB; ++b)
+            if (row < s.m && 32 * b + col < a.d) store_keys<ET>(a, s, kv, row, 32 * b + col, dK[b][i], dV[b][i]);
     }
 }
 
-template <typename ET, int DP, int WAVES> hipError_t attend_bwd(const attn_args& a, hipStream_t st)
+// bf16: a block has 256 keys, 32 a wave, and goes over 32 queries at a time.  In its matrix phase u a wave adds the products of tile u - 1 to both gradients and forms
+// the scores and <dO, v> of tile u; in its vector phase these become p and ds.  Registers: 32 rows of two gradients, of keys and of scores; the values, which
+// would be 32 more, lie in LDS (128 columns).  Tiles that causality hides from a wave's keys are worked on with zeros: no wave leaves the common step.
+struct DkvReads {
+    static constexpr int of(int i, int by_keys, bool v_in_lds) { return i < by_keys ? 2 : v_in_lds && ((i - by_keys) & 1) ? 2 : 1; }
+};
+template <int BY_KEYS, bool V_IN_LDS> struct DkvOrder { static constexpr int of(int i) { return DkvReads::of(i, BY_KEYS, V_IN_LDS); } };
+
+template <int DP> struct Dkv {
+    typedef Tile<bf16_t, DP> tile;
+    static constexpr bool V_IN_LDS = DP == 128, APART = DP == 64;      // 32 rows of 64 columns are a request each of four waves: half of them ask for Q, half for dO
+    typedef Request<bf16_t, DP, 32, APART ? WAVES / 2 : WAVES> request;
+    static constexpr int REQUESTS = APART ? 1 : 2 * request::P;
+    static constexpr uint32_t STATS = 1024, STAGE = 2 * request::BYTES + STATS, VALUES = V_IN_LDS ? SIDE * tile::ROW : 0;
+    static constexpr size_t LDS = VALUES + (size_t)STAGES * STAGE;
+};
+
+template <int DP>
+__global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
 {
-    constexpr int stage_q = 2 * Request<ET, DP, KEYS, WAVES>::BYTES, stage_k = 2 * Request<ET, DP, QUERIES, WAVES>::BYTES + WAVES * 2 * QUERIES * 4;
-    constexpr size_t bytes_q = (size_t)stage_q * stages_for(stage_q), bytes_k = (size_t)stage_k * stages_for(stage_k);
-    static PerDeviceOnce once_q, once_k;
-    hipError_t e = allow_lds(attend_dq_kernel<ET, DP, WAVES>, bytes_q, once_q);
-    if (e == hipSuccess) e = allow_lds(attend_dkv_kernel<ET, DP, WAVES>, bytes_k, once_k);
-    if (e != hipSuccess) return e;
-    const long long slots_q = a.q_rows / (WAVES * 32) + a.seqs, slots_k = a.k_rows / (WAVES * 32) + a.seqs;
+    typedef bf16_t ET;
+    typedef Dkv<DP> D;
+    typedef typename D::tile tile;
+    typedef typename D::request request;
+    typedef Frag<ET>::type frag;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const uint32_t values = (uint32_t)(uintptr_t)(LDS_PTR(char))lds, ring = values + D::VALUES;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
+    int kv, slot;
+    head_and_slot(blockIdx.x, a.kv_heads, kv, slot);
+    const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);
+    if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
+    const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
+    const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
+
+    const tile t(lane);
+    const bool second = wave >= WAVES / 2;
+    const request ask_q(lane, D::APART ? wave & 3 : wave, D::APART && second ? a.dO.row : a.Q.row, a.d), ask_o(lane, wave, a.dO.row, a.d);
+    Walk<32> walk(a, s, kv, block);
+    int asked_at = 0;
+    auto step = [&](int& place) { place = place == (STAGES - 1) * (int)D::STAGE ? 0 : place + (int)D::STAGE; };
+    auto ask = [&]() {                                     // past the end: zeros that nobody reads
+        const bool there = walk.there();
+        const uint32_t at = ring + asked_at;
+        const int h = there ? walk.head : walk.first_head, rows = there ? s.n - walk.tile * 32 : 0;
+        const long long q = s.q0 + (long long)walk.tile * 32;
+        if constexpr (D::APART) {
+            const heads_t& x = second ? a.dO : a.Q;
+            ask_q(row_of(x, h, q), rows, x.row, a.d, second ? at + request::BYTES : at, wave & 3);
+        } else {
+            ask_q(row_of(a.Q, h, q), rows, a.Q.row, a.d, at, wave);
+            ask_o(row_of(a.dO, h, q), rows, a.dO.row, a.d, at + request::BYTES, wave);
+        }
+        if (wave == 0)                                     // 32 rows' statistics, one request for all waves
+            dma4(tile_rsrc((const char*)(a.stats + (long long)h * a.q_rows + q), rows > 0 ? min(rows, 32) * 8 : 0), at + 2 * request::BYTES, lane * 4);
+        walk.next();
+        step(asked_at);
+    };
+    // All but the requests of the last `n` tiles have arrived.
+    auto wait = [&](auto n) {
+        if (wave == 0) WAIT_VMCNT(decltype(n)::value * (D::REQUESTS + 1));
+        else WAIT_VMCNT(decltype(n)::value * D::REQUESTS);
+    };
+    frag K[tile::T], V[D::V_IN_LDS ? 1 : tile::T];
+    {
+        const char *pk = row_of(a.K, kv, s.k0 + key), *pv = row_of(a.V, kv, s.k0 + key);
+#pragma unroll
+        for (int k = 0; k < tile::T; ++k) {
+            const int at = (16 * k + 8 * hi) * (int)sizeof(ET);
+            const bool there = key < s.m && 16 * k + 8 * hi < a.d;
+            K[k] = there ? Frag<ET>::load(pk + at) : Frag<ET>::zero();
+            if constexpr (!D::V_IN_LDS) V[k] = there ? Frag<ET>::load(pv + at) : Frag<ET>::zero();
+        }
+    }
+    f32x16 dK[tile::DB], dV[tile::DB];
+#pragma unroll
+    for (int b = 0; b < tile::DB; ++b) {
+        clear(dK[b]);
+        clear(dV[b]);
+    }
+    if (walk.steps > 0) {
+        constexpr int BY_KEYS = 4 * tile::DB, N = BY_KEYS + 2 * tile::T, PRE = AHEAD < BY_KEYS ? AHEAD : BY_KEYS;
+        f32x16 x, y;
+        frag p[2], ds[2], pre[PRE];
+        int at = 0, j = walk.start;                        // the place of the tile in hand, and which of a head's it is
+        if constexpr (D::V_IN_LDS) {
+            const Request<ET, DP, SIDE, WAVES> ask_v(lane, wave, a.V.row, a.d);
+            ask_v(row_of(a.V, kv, s.k0 + block), s.m - block, a.V.row, a.d, values, wave);
+        }
+        auto scores = [&](int place) {
+            const auto rows = t.rows_at(ring + place);
+            typename tile::RowsAt mine;                    // the same rows of the wave's values
+#pragma unroll
+            for (int k = 0; k < tile::T; ++k) mine.at[k] = rows.at[k] + (values + wave * 32 * tile::ROW - ring - place);
+            clear(x);
+            clear(y);
+#pragma unroll
+            for (int k = 0; k < tile::T; ++k) {
+                x = Frag<ET>::mma(tile::by_rows(rows, 0, k), K[k], x);
+                y = Frag<ET>::mma(tile::by_rows(rows, 0, k, request::BYTES), D::V_IN_LDS ? tile::by_rows(mine, 0, k) : V[D::V_IN_LDS ? 0 : k], y);
+            }
+        };
+        // product i of a tile's 4 DB: 16 queries, 32 columns, dV and dK in turn
+        auto operand = [&](const typename tile::KeysAt& keys, int i) { return tile::by_keys(keys, 16 * (i / (2 * tile::DB)), i / 2 % tile::DB, i & 1 ? 0 : request::BYTES); };
+        auto add = [&](const typename tile::KeysAt& keys) {
+#pragma unroll
+            for (int i = 0; i < BY_KEYS; ++i) {
+                const frag f = i < PRE ? pre[i < PRE ? i : 0] : operand(keys, i);
+                const int k = i / (2 * tile::DB), b = i / 2 % tile::DB;
+                if (i & 1) dK[b] = Frag<ET>::mma(ds[k], f, dK[b]);
+                else dV[b] = Frag<ET>::mma(p[k], f, dV[b]);
+            }
+        };
+        auto soften = [&]() {                              // and the first fragments of what comes next
+            const auto keys = t.keys_at(ring + at);
+#pragma unroll
+            for (int i = 0; i < PRE; ++i) pre[i] = operand(keys, i);
+            weigh(x, y, ring + at + 2 * request::BYTES, a.scale2, hi);
+            if (j * 32 < last) hide_queries(x, y, j * 32, mine, hi);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                p[k] = Frag<ET>::pack(x, k);
+                ds[k] = Frag<ET>::pack(y, k);
+            }
+            if (++j == walk.start + walk.tiles) j = walk.start;
+        };
+#pragma unroll
+        for (int i = 0; i < STAGES - 2; ++i) ask();
+        arrived(K);
+        arrived(V);
+        wait(std::integral_constant<int, 1>{});            // tiles 0 and 1, and the values
+        PHASE_END();
+        if (second) PHASE_END();                           // the second half is a phase behind
+        ask();
+        scores(0);
+        wait(std::integral_constant<int, 1>{});            // tile 2
+        PHASE_END();
+        soften();
+        PHASE_END();
+        for (int u = 1; u < walk.steps; ++u) {
+            const auto keys = t.keys_at(ring + at);
+            step(at);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            add(keys);
+            scores(at);
+            pace<DkvOrder<BY_KEYS, D::V_IN_LDS>, N, PRE>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+            ask();                                         // in the place of tile u - 2, which the second half was done with a phase ago
+            wait(std::integral_constant<int, 1>{});        // tile u + 2 has arrived
+            PHASE_END();
+            soften();
+            PHASE_END();
+        }
+        add(t.keys_at(ring + at));
+        if (!second) PHASE_END();
+        WAIT_VMCNT(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int row = first + 8 * (i >> 2) + 4 * hi + (i & 3);
+#pragma unroll
+        for (int b = 0; b < tile::DB; ++b)
+            if (row < s.m && 32 * b + col < a.d) store_keys<ET>(a, s, kv, row, 32 * b + col, dK[b][i], dV[b][i]);
+    }
+}
+
+template <typename ET, int DP> hipError_t attend_bwd(const attn_args& a, hipStream_t st)
+{
+    hipError_t e = hipSuccess;
     if (a.q_rows > 0) {
-        hipLaunchKernelGGL((attend_dq_kernel<ET, DP, WAVES>), dim3((unsigned)(slots_q * a.heads)), dim3(WAVES * 64), bytes_q, st, a);
+        constexpr size_t bytes = (size_t)STAGES * 2 * Request<ET, DP, keys_of<ET, DP>(), WAVES>::BYTES;
+        static PerDeviceOnce once;
+        if ((e = allow_lds(attend_dq_kernel<ET, DP>, bytes, once)) != hipSuccess) return e;
+        const long long slots = a.q_rows / SIDE + a.seqs;
+        hipLaunchKernelGGL((attend_dq_kernel<ET, DP>), dim3((unsigned)(slots * a.heads)), dim3(WAVES * 64), bytes, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.k_rows == 0) return hipSuccess;
-    hipLaunchKernelGGL((attend_dkv_kernel<ET, DP, WAVES>), dim3((unsigned)(slots_k * a.kv_heads)), dim3(WAVES * 64), bytes_k, st, a);
+    static PerDeviceOnce once;
+    if constexpr (sizeof(ET) == 2) {
+        if ((e = allow_lds(attend_dkv_kernel<DP>, Dkv<DP>::LDS, once)) != hipSuccess) return e;
+        const long long slots = a.k_rows / SIDE + a.seqs;
+        hipLaunchKernelGGL((attend_dkv_kernel<DP>), dim3((unsigned)(slots * a.kv_heads)), dim3(WAVES * 64), Dkv<DP>::LDS, st, a);
+    } else {
+        constexpr size_t bytes = 2 * (2 * Request<float, DP, 64, 4>::BYTES + 4 * 64 * 8);
+        if ((e = allow_lds(attend_dkv_f32_kernel<DP>, bytes, once)) != hipSuccess) return e;
+        const long long slots = a.k_rows / 128 + a.seqs;
+        hipLaunchKernelGGL((attend_dkv_f32_kernel<DP>), dim3((unsigned)(slots * a.kv_heads)), dim3(256), bytes, st, a);
+    }
     return hipGetLastError();
 }
 
@@ -295,8 +552,8 @@ hipError_t launch_attn_bwd(const moe_attn_t& c, const moe_heads_t& dO, const moe
     attn_args a = attn_make(c);
     a.Q = in_bytes(Q, size), a.K = in_bytes(K, size), a.V = in_bytes(V, size), a.O = in_bytes(O, size), a.dO = in_bytes(dO, size);
     a.dQ = in_bytes(dQ, size), a.dK = in_bytes(dK, size), a.dV = in_bytes(dV, size);
-    a.lse = const_cast<float*>(lse), a.D = (float*)ws;
+    a.lse = const_cast<float*>(lse), a.stats = (float2*)ws;
     a.offsets = offsets, a.k_begin = k_begin, a.k_end = k_end;
-    if (c.dtype == MOE_BF16) return c.d <= 64 ? attend_bwd<bf16_t, 64, 8>(a, st) : attend_bwd<bf16_t, 128, 8>(a, st);
-    return c.d <= 64 ? attend_bwd<float, 64, 4>(a, st) : attend_bwd<float, 128, 4>(a, st);
+    if (c.dtype == MOE_BF16) return c.d <= 64 ? attend_bwd<bf16_t, 64>(a, st) : attend_bwd<bf16_t, 128>(a, st);
+    return c.d <= 64 ? attend_bwd<float, 64>(a, st) : attend_bwd<float, 128>(a, st);
 }
