@@ -46,7 +46,7 @@ template <typename ET, int DP> struct Rows {
     // Keys past `limit` are hidden from this lane's query; `first` is the key of row 0.
     template <int NB> static __device__ __forceinline__ void hide(f32x16 (&s)[NB], int first, int limit, int hi)
     {
-        RARELY();
+        APART();
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -59,8 +59,8 @@ template <typename ET, int DP> struct Rows {
     template <int NB> __device__ __forceinline__ void soften(const f32x16 (&s)[NB], float scale2, frag (&p)[2 * NB])
     {
         float now = powers(s, scale2, p);
-        if (__any(now > STALE)) {
-            RARELY();
+        RARELY(__any(now > STALE)) {
+            APART();
             float top = s[0][0];
 #pragma unroll
             for (int i = 1; i < 16 * NB; i += 2) top = highest_of(top, s[i / 16][i % 16], s[(i + 1 < 16 * NB ? i + 1 : i) / 16][(i + 1 < 16 * NB ? i + 1 : i) % 16]);
@@ -122,14 +122,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int head, slot;
     head_and_slot(blockIdx.x, a.heads, head, slot);
-    const Sequence s = find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, gridDim.x / a.heads - 1 - slot, lane);      // later tiles see more keys and go first
+    const Sequence s = find_tile<SIDE>(a, false, slot, gridDim.x / a.heads, gridDim.x, lane);
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.n) return;
     const int shift = s.m - s.n, first = s.tile * SIDE + wave * 32, row = first + col;     // of the sequence's queries
     // how many keys the block's, this wave's last query sees; the last key that this lane's, the wave's first sees
     const int block_keys = a.causal ? min(s.m, max(0, min(s.n, (s.tile + 1) * SIDE) + shift)) : s.m;
     const int wave_keys = first >= s.n ? 0 : a.causal ? min(s.m, max(0, min(s.n, first + 32) + shift)) : s.m;
     const int limit = (a.causal ? min(s.m, row + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, first + shift + 1) : s.m) - 1;
-    const int tiles = (block_keys + KEYS - 1) / KEYS, wave_tiles = (wave_keys + KEYS - 1) / KEYS;
+    const int tiles = uniform((block_keys + KEYS - 1) / KEYS), wave_tiles = uniform((wave_keys + KEYS - 1) / KEYS);
 
     const int kv = head / a.group;
     const char* K = row_of(a.K, kv, s.k0);
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
     const tile t(lane);
     const request ask_k(lane, wave, a.K.row, a.d), ask_v(lane, wave, a.V.row, a.d);
     int asked = 0, asked_at = 0;                           // rows asked for, and the place of the next ones in the ring
-    auto ask = [&]() {                                     // the next tile; past the last one: zeros that nobody reads
+    auto ask = [&]() INLINE {                                     // the next tile; past the last one: zeros that nobody reads
         const uint32_t at = ring + asked_at;
         ask_k(K, s.m - asked, a.K.row, a.d, at, wave);
         ask_v(V, s.m - asked, a.V.row, a.d, at + request::BYTES, wave);
@@ -159,9 +159,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
         f32x16 x[NB];
         frag p[2 * NB], pre[PRE];
         int at = 0, next = STAGE;                          // tile j's place in the ring, and that of the one after it
-        auto step = [&](int& place) { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
-        auto soften = [&](int j) {
-            if (j * KEYS + KEYS - 1 > least) r.hide(x, j * KEYS, limit, hi);
+        auto step = [&](int& place) INLINE { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
+        auto soften = [&](int j) INLINE {
+            RARELY(j * KEYS + KEYS - 1 > least) r.hide(x, j * KEYS, limit, hi);
             r.soften(x, a.scale2, p);
         };
 #pragma unroll
@@ -176,14 +176,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
             r.scores(rows, pre, x);
         }
         PHASE_END();
-        if (wave_tiles > 0) {
-            if (wave_tiles > 1) r.template request<NB>(t.rows_at(ring + next), pre);
-            soften(0);
-        }
-        WAIT_VMCNT(2 * request::P);                        // tile 2
-        PHASE_END();
         int j = 0;
+        auto vector_phase = [&](int j) INLINE {
+            r.template request<NB>(t.rows_at(ring + next), pre);       // whole tiles, also past the wave's last
+            soften(j);
+        };
+        if (wave_tiles > 0) vector_phase(0);
+        // The loop closes at the end of a vector phase, ahead of its barrier: a jump waits for its instructions, and after the barrier everyone would wait with it.
         for (; j < wave_tiles - 1; ++j) {
+            WAIT_VMCNT(2 * request::P);                    // tile 2 has arrived, the first time round; later nothing is left to wait for
+            PHASE_END();
             const auto rows = t.rows_at(ring + next);
             const auto keys = t.keys_at(ring + at + request::BYTES);
             __builtin_amdgcn_sched_barrier(0);
@@ -198,10 +200,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
             PHASE_END();
             step(at);
             step(next);
-            r.template request<NB>(t.rows_at(ring + next), pre);       // whole tiles, also past the wave's last
-            soften(j + 1);
-            PHASE_END();
+            vector_phase(j + 1);
         }
+        PHASE_END();
         for (; j < tiles; ++j) {                           // this wave's last one, and those that only others see
             ask();
             if (j < wave_tiles) r.add(t.keys_at(ring + at + request::BYTES), p);
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_few_kernel(attn_args
     const char* V = row_of(a.V, kv, s.k0);
     const tile t(lane);
     const request ask_k(lane, 0, a.K.row, a.d), ask_v(lane, 0, a.V.row, a.d);
-    auto ask = [&](int j, int at) {
+    auto ask = [&](int j, int at) INLINE {
         const int rows = j < end ? s.m - j * FEW_KEYS : 0;
         ask_k(K + (long long)j * FEW_KEYS * a.K.row, rows, a.K.row, a.d, ring + at * STAGE, 0);
         ask_v(V + (long long)j * FEW_KEYS * a.V.row, rows, a.V.row, a.d, ring + at * STAGE + request::BYTES, 0);
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_few_kernel(attn_args
             const auto rows = t.rows_at(ring + at * STAGE);
             r.template request<1>(rows, pre);
             r.scores(rows, pre, x);
-            if (j * FEW_KEYS + FEW_KEYS - 1 > least) r.hide(x, j * FEW_KEYS, limit, hi);
+            RARELY(j * FEW_KEYS + FEW_KEYS - 1 > least) r.hide(x, j * FEW_KEYS, limit, hi);
             frag p[2];
             r.soften(x, a.scale2, p);
             r.add(t.keys_at(ring + at * STAGE + request::BYTES), p);

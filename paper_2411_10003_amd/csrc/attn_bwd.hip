@@ -42,13 +42,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int head, slot;
     head_and_slot(blockIdx.x, a.heads, head, slot);
-    const Sequence s = find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, gridDim.x / a.heads - 1 - slot, lane);
+    const Sequence s = find_tile<SIDE>(a, false, slot, gridDim.x / a.heads, gridDim.x, lane);
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.n) return;
     const int shift = s.m - s.n, first = s.tile * SIDE + wave * 32, row = first + col;
     const int block_keys = a.causal ? min(s.m, max(0, min(s.n, (s.tile + 1) * SIDE) + shift)) : s.m;
     const int wave_keys = first >= s.n ? 0 : a.causal ? min(s.m, max(0, min(s.n, first + 32) + shift)) : s.m;
     const int limit = (a.causal ? min(s.m, row + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, first + shift + 1) : s.m) - 1;
-    const int tiles = (block_keys + KEYS - 1) / KEYS, wave_tiles = (wave_keys + KEYS - 1) / KEYS;
+    const int tiles = uniform((block_keys + KEYS - 1) / KEYS), wave_tiles = uniform((wave_keys + KEYS - 1) / KEYS);
 
     const int kv = head / a.group;
     const char* K = row_of(a.K, kv, s.k0);
@@ -56,8 +56,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
     const tile t(lane);
     const request ask_k(lane, wave, a.K.row, a.d), ask_v(lane, wave, a.V.row, a.d);
     int asked = 0, asked_at = 0;                           // rows asked for, and the place of the next ones in the ring
-    auto step = [&](int& place) { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
-    auto ask = [&]() {                                     // the next tile; past the last one: zeros that nobody reads
+    auto step = [&](int& place) INLINE { place = place == (STAGES - 1) * (int)STAGE ? 0 : place + STAGE; };
+    auto ask = [&]() INLINE {                                     // the next tile; past the last one: zeros that nobody reads
         ask_k(K, s.m - asked, a.K.row, a.d, ring + asked_at, wave);
         ask_v(V, s.m - asked, a.V.row, a.d, ring + asked_at + request::BYTES, wave);
         K += (long long)KEYS * a.K.row;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
         f32x16 x[NB], y[NB];
         frag ds[2 * NB], pre[PRE];
         int at = 0;                                        // the place of the tile in hand
-        auto scores = [&](int place) {
+        auto scores = [&](int place) INLINE {
             const auto rows = t.rows_at(ring + place);
 #pragma unroll
             for (int h = 0; h < NB; ++h) {
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
                     y[h] = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), dO[k], y[h]);
                 }
         };
-        auto add = [&](const typename tile::KeysAt& keys) {
+        auto add = [&](const typename tile::KeysAt& keys) INLINE {
 #pragma unroll
             for (int k = 0; k < 2 * NB; ++k)
 #pragma unroll
@@ -118,17 +118,19 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
                     g[b] = Frag<ET>::mma(i < PRE ? pre[i < PRE ? i : 0] : tile::by_keys(keys, 16 * k, b), ds[k], g[b]);
                 }
         };
-        auto soften = [&](int j) {                         // and the first fragments of what comes next
+        auto request_first = [&]() INLINE {                       // of the tile in hand's keys
             const auto keys = t.keys_at(ring + at);
 #pragma unroll
             for (int i = 0; i < PRE; ++i) pre[i] = tile::by_keys(keys, 16 * (i / tile::DB), i % tile::DB);
+        };
+        auto soften = [&](int j) INLINE {
 #pragma unroll
             for (int h = 0; h < NB; ++h) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[h][i] = exp2_fast(fmaf(x[h][i], a.scale2, -lse2)) * (y[h][i] - D);
                 const int key = j * KEYS + 32 * h;
-                if (key + 31 > least) {
-                    RARELY();
+                RARELY(key + 31 > least) {
+                    APART();
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[h][i] = key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? 0.0f : x[h][i];
                 }
@@ -140,36 +142,41 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
         for (int j = 0; j < STAGES - 2; ++j) ask();
         arrived(q);
         arrived(dO);
-        WAIT_VMCNT(2 * request::P);                        // tiles 0 and 1 have arrived
+        WAIT_VMCNT(2 * 2 * request::P);                    // tile 0 has arrived
         PHASE_END();
         if (wave >= WAVES / 2) PHASE_END();                // the second half is a phase behind
         ask();
         if (wave_tiles > 0) scores(0);
-        WAIT_VMCNT(2 * request::P);                        // tile 2
+        WAIT_VMCNT(2 * 2 * request::P);                    // tile 1
         PHASE_END();
-        if (wave_tiles > 0) soften(0);
-        PHASE_END();
-        int j = 1;
-        for (; j < wave_tiles; ++j) {
+        int j = 0;
+        auto vector_phase = [&](int j) INLINE {
+            request_first();
+            soften(j);
+        };
+        if (wave_tiles > 0) vector_phase(0);
+        // The loop closes at the end of a vector phase, ahead of its barrier: a jump waits for its instructions, and after the barrier everyone would wait with it.
+        for (; j < wave_tiles - 1; ++j) {
+            PHASE_END();
             const auto keys = t.keys_at(ring + at);
             step(at);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             add(keys);
-            ask();                                         // in the place of tile j - 2, which the second half was done with a phase ago
+            ask();                                         // in the place of tile j - 1, which the second half was done with a phase ago
             scores(at);
             if constexpr (sizeof(ET) == 2) pace<KeysThenRows<BY_KEYS>, N, PRE>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
-            WAIT_VMCNT(2 * request::P);                    // tile j + 2 has arrived
+            WAIT_VMCNT(2 * 2 * request::P);                // tile j + 2 has arrived
             PHASE_END();
-            soften(j);
-            PHASE_END();
+            vector_phase(j + 1);
         }
-        for (; j <= tiles; ++j) {                          // this wave's last one, and those that only others see
+        PHASE_END();
+        for (; j < tiles; ++j) {                           // this wave's last one, and those that only others see
             ask();
-            if (j == wave_tiles) add(t.keys_at(ring + at));
-            WAIT_VMCNT(2 * request::P);
+            if (j == wave_tiles - 1) add(t.keys_at(ring + at));
+            WAIT_VMCNT(2 * 2 * request::P);
             PHASE_END();
             PHASE_END();
         }
@@ -210,7 +217,7 @@ __device__ __forceinline__ void weigh(f32x16& x, f32x16& y, uint32_t stats, floa
 // Queries before `mine` do not see this lane's key; `first` is the query of row 0.
 __device__ __forceinline__ void hide_queries(f32x16& x, f32x16& y, int first, int mine, int hi)
 {
-    RARELY();
+    APART();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const bool hidden = first + 8 * (i >> 2) + 4 * hi + (i & 3) < mine;
@@ -234,7 +241,7 @@ template <int ROWS> struct Walk {
         first_head = kv * a.group, heads = a.group;
         const int from = a.causal ? max(0, block - (s.m - s.n)) : 0;
         start = from / ROWS;
-        tiles = max(0, (s.n + ROWS - 1) / ROWS - start);
+        tiles = uniform(max(0, (s.n + ROWS - 1) / ROWS - start));
         steps = tiles * heads;
         head = first_head, tile = start;
     }
@@ -258,7 +265,7 @@ __global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int kv, slot;
     head_and_slot(blockIdx.x, a.kv_heads, kv, slot);
-    const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);
+    const Sequence s = find_tile<SIDE>(a, true, slot, 0, gridDim.x, lane);
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
     const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
     const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
     const request ask_q(lane, wave, a.Q.row, a.d), ask_o(lane, wave, a.dO.row, a.d);
     Walk<QUERIES> walk(a, s, kv, block);
     int slot_at = 0;
-    auto ask = [&]() {                                     // past the end: zeros that nobody reads
+    auto ask = [&]() INLINE {                                     // past the end: zeros that nobody reads
         const bool there = walk.there();
         const uint32_t at = ring + slot_at * STAGE;
         const int h = there ? walk.head : walk.first_head, rows = there ? s.n - walk.tile * QUERIES : 0;
@@ -324,7 +331,7 @@ __global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
                     y = Frag<ET>::mma(tile::by_rows(rows, 32 * h, k, request::BYTES), V[k], y);
                 }
                 weigh(x, y, stats + 32 * h * 8, a.scale2, hi);
-                if (query < last) hide_queries(x, y, query, mine, hi);
+                RARELY(query < last) hide_queries(x, y, query, mine, hi);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const frag p = Frag<ET>::pack(x, k), ds = Frag<ET>::pack(y, k);
@@ -357,9 +364,9 @@ template <int BY_KEYS, bool V_IN_LDS> struct DkvOrder { static constexpr int of(
 
 template <int DP> struct Dkv {
     typedef Tile<bf16_t, DP> tile;
-    static constexpr bool V_IN_LDS = DP == 128, APART = DP == 64;      // 32 rows of 64 columns are a request each of four waves: half of them ask for Q, half for dO
-    typedef Request<bf16_t, DP, 32, APART ? WAVES / 2 : WAVES> request;
-    static constexpr int REQUESTS = APART ? 1 : 2 * request::P;
+    static constexpr bool V_IN_LDS = DP == 128, HALVES = DP == 64;      // 32 rows of 64 columns are a request each of four waves: half of them ask for Q, half for dO
+    typedef Request<bf16_t, DP, 32, HALVES ? WAVES / 2 : WAVES> request;
+    static constexpr int REQUESTS = HALVES ? 1 : 2 * request::P;
     static constexpr uint32_t STATS = 1024, STAGE = 2 * request::BYTES + STATS, VALUES = V_IN_LDS ? SIDE * tile::ROW : 0;
     static constexpr size_t LDS = VALUES + (size_t)STAGES * STAGE;
 };
@@ -377,23 +384,23 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int kv, slot;
     head_and_slot(blockIdx.x, a.kv_heads, kv, slot);
-    const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);
+    const Sequence s = find_tile<SIDE>(a, true, slot, 0, gridDim.x, lane);
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
     const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
     const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
 
     const tile t(lane);
     const bool second = wave >= WAVES / 2;
-    const request ask_q(lane, D::APART ? wave & 3 : wave, D::APART && second ? a.dO.row : a.Q.row, a.d), ask_o(lane, wave, a.dO.row, a.d);
+    const request ask_q(lane, D::HALVES ? wave & 3 : wave, D::HALVES && second ? a.dO.row : a.Q.row, a.d), ask_o(lane, wave, a.dO.row, a.d);
     Walk<32> walk(a, s, kv, block);
     int asked_at = 0;
-    auto step = [&](int& place) { place = place == (STAGES - 1) * (int)D::STAGE ? 0 : place + (int)D::STAGE; };
-    auto ask = [&]() {                                     // past the end: zeros that nobody reads
+    auto step = [&](int& place) INLINE { place = place == (STAGES - 1) * (int)D::STAGE ? 0 : place + (int)D::STAGE; };
+    auto ask = [&]() INLINE {                                     // past the end: zeros that nobody reads
         const bool there = walk.there();
         const uint32_t at = ring + asked_at;
         const int h = there ? walk.head : walk.first_head, rows = there ? s.n - walk.tile * 32 : 0;
         const long long q = s.q0 + (long long)walk.tile * 32;
-        if constexpr (D::APART) {
+        if constexpr (D::HALVES) {
             const heads_t& x = second ? a.dO : a.Q;
             ask_q(row_of(x, h, q), rows, x.row, a.d, second ? at + request::BYTES : at, wave & 3);
         } else {
@@ -406,7 +413,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
         step(asked_at);
     };
     // All but the requests of the last `n` tiles have arrived.
-    auto wait = [&](auto n) {
+    auto wait = [&](auto n) INLINE {
         if (wave == 0) WAIT_VMCNT(decltype(n)::value * (D::REQUESTS + 1));
         else WAIT_VMCNT(decltype(n)::value * D::REQUESTS);
     };
@@ -436,7 +443,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
             const Request<ET, DP, SIDE, WAVES> ask_v(lane, wave, a.V.row, a.d);
             ask_v(row_of(a.V, kv, s.k0 + block), s.m - block, a.V.row, a.d, values, wave);
         }
-        auto scores = [&](int place) {
+        auto scores = [&](int place) INLINE {
             const auto rows = t.rows_at(ring + place);
             typename tile::RowsAt mine;                    // the same rows of the wave's values
 #pragma unroll
@@ -450,8 +457,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
             }
         };
         // product i of a tile's 4 DB: 16 queries, 32 columns, dV and dK in turn
-        auto operand = [&](const typename tile::KeysAt& keys, int i) { return tile::by_keys(keys, 16 * (i / (2 * tile::DB)), i / 2 % tile::DB, i & 1 ? 0 : request::BYTES); };
-        auto add = [&](const typename tile::KeysAt& keys) {
+        auto operand = [&](const typename tile::KeysAt& keys, int i) INLINE { return tile::by_keys(keys, 16 * (i / (2 * tile::DB)), i / 2 % tile::DB, i & 1 ? 0 : request::BYTES); };
+        auto add = [&](const typename tile::KeysAt& keys) INLINE {
 #pragma unroll
             for (int i = 0; i < BY_KEYS; ++i) {
                 const frag f = i < PRE ? pre[i < PRE ? i : 0] : operand(keys, i);
@@ -460,33 +467,36 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
                 else dV[b] = Frag<ET>::mma(p[k], f, dV[b]);
             }
         };
-        auto soften = [&]() {                              // and the first fragments of what comes next
+        auto request_first = [&]() INLINE {                       // of the tile in hand's products
             const auto keys = t.keys_at(ring + at);
 #pragma unroll
             for (int i = 0; i < PRE; ++i) pre[i] = operand(keys, i);
+        };
+        auto soften = [&]() INLINE {
             weigh(x, y, ring + at + 2 * request::BYTES, a.scale2, hi);
-            if (j * 32 < last) hide_queries(x, y, j * 32, mine, hi);
+            RARELY(j * 32 < last) hide_queries(x, y, j * 32, mine, hi);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 p[k] = Frag<ET>::pack(x, k);
                 ds[k] = Frag<ET>::pack(y, k);
             }
-            if (++j == walk.start + walk.tiles) j = walk.start;
+            RARELY(++j == walk.start + walk.tiles) j = walk.start;
         };
 #pragma unroll
         for (int i = 0; i < STAGES - 2; ++i) ask();
         arrived(K);
         arrived(V);
-        wait(std::integral_constant<int, 1>{});            // tiles 0 and 1, and the values
+        wait(std::integral_constant<int, 2>{});            // the values and tile 0
         PHASE_END();
         if (second) PHASE_END();                           // the second half is a phase behind
         ask();
         scores(0);
-        wait(std::integral_constant<int, 1>{});            // tile 2
+        wait(std::integral_constant<int, 2>{});            // tile 1
         PHASE_END();
+        request_first();
         soften();
-        PHASE_END();
-        for (int u = 1; u < walk.steps; ++u) {
+        for (int u = 1; u < walk.steps; ++u) {             // closes as the one above
+            PHASE_END();
             const auto keys = t.keys_at(ring + at);
             step(at);
             __builtin_amdgcn_sched_barrier(0);
@@ -497,11 +507,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
             ask();                                         // in the place of tile u - 2, which the second half was done with a phase ago
-            wait(std::integral_constant<int, 1>{});        // tile u + 2 has arrived
+            wait(std::integral_constant<int, 2>{});        // tile u + 1 has arrived
             PHASE_END();
+            request_first();
             soften();
-            PHASE_END();
         }
+        PHASE_END();
         add(t.keys_at(ring + at));
         if (!second) PHASE_END();
         WAIT_VMCNT(0);
