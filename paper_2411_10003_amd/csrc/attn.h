@@ -279,49 +279,6 @@ __device__ __forceinline__ Sequence find_sequence(const attn_args& a, const int3
     return s;
 }
 
-// The same with the blocks in the order of their work, the most first: `rank` is a block's place in it.  A causal sequence's tile of queries goes over as many tiles of
-// keys as its number says, its tile of keys over as many tiles of queries as come after it: level r has the tiles whose work is r + 1, one of each sequence that is
-// long enough, and the levels come from the highest down (blocks in the sequences' order leave the last CUs at work alone: four sequences of 8192, backward, 7.7 -> LATER ms).
-// For up to 64 sequences, one a lane; more of them are short enough to even out, and up to a block a CU the order does not matter.
-__device__ __forceinline__ int sum_of_lanes(int v)
-{
-    int sum = 0;
-    for (int bit = 0; __any(v >> bit); ++bit) sum += __popcll(__ballot((v >> bit) & 1)) << bit;
-    return sum;
-}
-template <int SIDE>
-__device__ __forceinline__ Sequence find_ranked(const attn_args& a, bool of_keys, int rank, int lane)
-{
-    const bool in = lane < a.seqs;
-    const int at = in ? lane : 0;
-    const int q0 = clamped(a.offsets[at], a.q_rows), q1 = clamped(a.offsets[at + 1], a.q_rows), k0 = clamped(a.k_begin[at], a.k_rows), k1 = clamped(a.k_end[at], a.k_rows);
-    const int n = max(0, q1 - q0), m = max(0, k1 - k0), tiles = in ? ((of_keys ? m : n) + SIDE - 1) / SIDE : 0;
-    // the level: the lowest whose blocks and those before it are more than `rank`
-    int low = 0, high = 0;
-    for (int bit = 1; __any(tiles >= bit); bit <<= 1) high = 2 * bit - 1;
-    while (low < high) {
-        const int mid = (low + high + 1) >> 1;
-        if (sum_of_lanes(max(0, tiles - mid)) > rank) low = mid;
-        else high = mid - 1;
-    }
-    const uint64_t here = __ballot(tiles > low);
-    int which = rank - sum_of_lanes(max(0, tiles - low - 1));
-    const bool mine = tiles > low && __popcll(here & ((1ull << lane) - 1)) == which;
-    const uint64_t found = __ballot(mine);
-    const int from = found ? __ffsll((unsigned long long)found) - 1 : 0;
-    Sequence s;
-    s.q0 = uniform(__shfl(q0, from, 64)), s.n = uniform(__shfl(n, from, 64)), s.k0 = uniform(__shfl(k0, from, 64)), s.m = uniform(__shfl(m, from, 64));
-    s.tile = uniform(found ? (of_keys ? __shfl(tiles, from, 64) - 1 - low : low) : -1);
-    return s;
-}
-template <int SIDE>
-__device__ __forceinline__ Sequence find_tile(const attn_args& a, bool of_keys, int slot, int slots, int blocks, int lane)
-{
-    if (blocks > 256 && a.seqs > 1 && a.seqs <= 64) return find_ranked<SIDE>(a, of_keys, slot, lane);
-    // a sequence's later queries see more keys, its earlier keys are seen by more queries: those go first
-    return of_keys ? find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane) : find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, slots - 1 - slot, lane);
-}
-
 // Blocks go to the eight XCDs in turn: where the heads are a multiple of eight, an XCD works on heads / 8 neighbouring ones, whose keys and values are the
 // same ones where heads share them, and its L2 holds those only.
 __device__ __forceinline__ void head_and_slot(int id, int heads, int& head, int& slot)

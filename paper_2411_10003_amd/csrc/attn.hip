@@ -122,7 +122,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int head, slot;
     head_and_slot(blockIdx.x, a.heads, head, slot);
-    const Sequence s = find_tile<SIDE>(a, false, slot, gridDim.x / a.heads, gridDim.x, lane);
+    const Sequence s = find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, gridDim.x / a.heads - 1 - slot, lane);      // later tiles see more keys and go first
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.n) return;
     const int shift = s.m - s.n, first = s.tile * SIDE + wave * 32, row = first + col;     // of the sequence's queries
     // how many keys the block's, this wave's last query sees; the last key that this lane's, the wave's first sees

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dq_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int head, slot;
     head_and_slot(blockIdx.x, a.heads, head, slot);
-    const Sequence s = find_tile<SIDE>(a, false, slot, gridDim.x / a.heads, gridDim.x, lane);
+    const Sequence s = find_sequence<SIDE>(a, a.offsets, a.q_rows, 1, gridDim.x / a.heads - 1 - slot, lane);      // later tiles see more keys and go first
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.n) return;
     const int shift = s.m - s.n, first = s.tile * SIDE + wave * 32, row = first + col;
     const int block_keys = a.causal ? min(s.m, max(0, min(s.n, (s.tile + 1) * SIDE) + shift)) : s.m;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int kv, slot;
     head_and_slot(blockIdx.x, a.kv_heads, kv, slot);
-    const Sequence s = find_tile<SIDE>(a, true, slot, 0, gridDim.x, lane);
+    const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);      // earlier tiles are seen by more queries and go first
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
     const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
     const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     int kv, slot;
     head_and_slot(blockIdx.x, a.kv_heads, kv, slot);
-    const Sequence s = find_tile<SIDE>(a, true, slot, 0, gridDim.x, lane);
+    const Sequence s = find_sequence<SIDE>(a, a.k_begin, a.k_rows, 1, slot, lane);      // earlier tiles are seen by more queries and go first
     if (s.tile < 0 || (long long)s.tile * SIDE >= s.m) return;
     const int shift = s.m - s.n, block = s.tile * SIDE, first = block + wave * 32, key = first + col;
     const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the wave's last
