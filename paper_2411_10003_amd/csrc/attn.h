@@ -279,6 +279,31 @@ __device__ __forceinline__ Sequence find_sequence(const attn_args& a, const int3
     return s;
 }
 
+// Small calls: blocks of 32 rows whose waves share the work along the other axis, each through a ring of its own in LDS, and join at the end.
+constexpr int FEW_KEYS = 32, FEW_STAGES = 2;
+template <typename ET, int DP> constexpr int few_waves() { return DP * (int)sizeof(ET) <= 256 ? 4 : 2; }
+// Where row r of a block's 32 lies: token by token, the heads that share a kv head beside each other.
+struct FewRow { int token, head; bool there; };
+__device__ __forceinline__ FewRow few_row(const attn_args& a, const Sequence& s, int kv, int r)
+{
+    const long long i = (long long)s.tile * 32 + r;
+    FewRow f;
+    f.token = (int)(i / a.group);
+    f.head = kv * a.group + (int)(i % a.group);
+    f.there = f.token < s.n;
+    return f;
+}
+
+// Keys that the last of a block's rows sees.
+__device__ __forceinline__ int few_keys(const attn_args& a, const Sequence& s)
+{
+    const int last = min(s.n - 1, (int)(((long long)s.tile * 32 + 31) / a.group));
+    return a.causal ? min(s.m, max(0, last + 1 + s.m - s.n)) : s.m;
+}
+// Blocks of 32 rows, and whether a call of so many larger blocks is one for them: up to one for each CU, the longest of which all the others would wait for.
+inline long long few_units(const attn_args& a) { return ((long long)a.q_rows * a.group / 32 + a.seqs) * a.kv_heads; }
+inline bool is_small(long long blocks) { return blocks <= 256; }
+
 // Blocks go to the eight XCDs in turn: where the heads are a multiple of eight, an XCD works on heads / 8 neighbouring ones, whose keys and values are the
 // same ones where heads share them, and its L2 holds those only.
 __device__ __forceinline__ void head_and_slot(int id, int heads, int& head, int& slot)

@@ -231,29 +231,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
 // Few rows (answering a token at a time): a block has 32 rows of one sequence, token by token the heads that share a kv head beside each other, and one
 // part of the keys; its waves take tiles of 32 keys in turn, each through a ring of its own, and join at the end.  Bound by the keys and values,
 // read once for all heads that share them.  With more than one part the unscaled results go to the workspace and a second launch joins them.
-constexpr int FEW_KEYS = 32, FEW_STAGES = 2;
-template <typename ET, int DP> constexpr int few_waves() { return DP * (int)sizeof(ET) <= 256 ? 4 : 2; }
 constexpr int PARTIAL_MORE = 64;                           // of a part's 32 rows: maximum and sum
 template <int DP> constexpr int partial_floats() { return 32 * DP + PARTIAL_MORE; }
 
-// Where row r of a block's 32 lies: token and head.
-struct FewRow { int token, head; bool there; };
-__device__ __forceinline__ FewRow few_row(const attn_args& a, const Sequence& s, int kv, int r)
-{
-    const long long i = (long long)s.tile * 32 + r;
-    FewRow f;
-    f.token = (int)(i / a.group);
-    f.head = kv * a.group + (int)(i % a.group);
-    f.there = f.token < s.n;
-    return f;
-}
-
-// Keys that the last of a block's rows sees, and how they are cut: `chunk` tiles a part as the launch has it, more where that does not reach the end.
-__device__ __forceinline__ int few_keys(const attn_args& a, const Sequence& s)
-{
-    const int last = min(s.n - 1, (int)(((long long)s.tile * 32 + 31) / a.group));
-    return a.causal ? min(s.m, max(0, last + 1 + s.m - s.n)) : s.m;
-}
+// How the keys that a block's rows see are cut: `chunk` tiles a part as the launch has it, more where that does not reach the end.
 struct Parts {
     int tiles, chunk, used;
     __device__ __forceinline__ Parts(const attn_args& a, int keys)
@@ -423,7 +404,7 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
     hipError_t e = allow_lds(attend_few_kernel<ET, DP, FEW_WAVES>, bytes, once);
     if (e != hipSuccess) return e;
     // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do
-    const long long units = ((long long)a.q_rows * a.group / 32 + a.seqs) * a.kv_heads;
+    const long long units = few_units(a);
     const long long tiles = ((long long)a.k_rows / a.seqs + FEW_KEYS - 1) / FEW_KEYS;
     const long long want = ATTN_PARTS / units, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);
     a.splits = (int)(want < most ? want : most);
@@ -439,7 +420,7 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
 template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t st)
 {
     // few rows: what a kv head has of an average sequence fits one block's 32 twice over
-    if ((long long)a.q_rows * a.group <= 64ll * a.seqs) return launch_few<ET, DP>(a, st);
+    if ((long long)a.q_rows * a.group <= 64ll * a.seqs || is_small(((long long)a.q_rows / SIDE + a.seqs) * a.heads)) return launch_few<ET, DP>(a, st);
     return launch_rows<ET, DP>(a, st);
 }
 

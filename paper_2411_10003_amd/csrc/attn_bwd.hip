@@ -526,30 +526,273 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
     }
 }
 
-template <typename ET, int DP> hipError_t attend_bwd(const attn_args& a, hipStream_t st)
+template <typename ET, int DP> struct FewDkv { static constexpr uint32_t STAGE = 2 * Request<ET, DP, 32, 1>::BYTES + 256; };
+
+// Small calls, dQ: a block has 32 rows of a sequence and kv head, its waves take tiles of 32 keys in turn.
+template <typename ET, int DP, int FEW_WAVES>
+__global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_args a)
 {
-    hipError_t e = hipSuccess;
-    if (a.q_rows > 0) {
-        constexpr size_t bytes = (size_t)STAGES * 2 * Request<ET, DP, keys_of<ET, DP>(), WAVES>::BYTES;
-        static PerDeviceOnce once;
-        if ((e = allow_lds(attend_dq_kernel<ET, DP>, bytes, once)) != hipSuccess) return e;
-        const long long slots = a.q_rows / SIDE + a.seqs;
-        hipLaunchKernelGGL((attend_dq_kernel<ET, DP>), dim3((unsigned)(slots * a.heads)), dim3(WAVES * 64), bytes, st, a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+    typedef Tile<ET, DP> tile;
+    typedef Request<ET, DP, FEW_KEYS, 1> request;
+    typedef typename Frag<ET>::type frag;
+    constexpr int PITCH = DP + 4;
+    constexpr uint32_t STAGE = 2 * request::BYTES;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
+    const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * FEW_STAGES * STAGE;
+    const int kv = blockIdx.x % a.kv_heads;
+    const Sequence s = find_sequence<32>(a, a.offsets, a.q_rows, a.group, blockIdx.x / a.kv_heads, lane);
+    if (s.tile < 0 || (long long)s.tile * 32 >= (long long)s.n * a.group) return;
+    const FewRow me = few_row(a, s, kv, col);
+    const int shift = s.m - s.n, tiles = uniform((few_keys(a, s) + FEW_KEYS - 1) / FEW_KEYS);
+    const int limit = (a.causal ? min(s.m, me.token + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, (int)((long long)s.tile * 32 / a.group) + shift + 1) : s.m) - 1;
+
+    const char* K = row_of(a.K, kv, s.k0);
+    const char* V = row_of(a.V, kv, s.k0);
+    const tile t(lane);
+    const request ask_k(lane, 0, a.K.row, a.d), ask_v(lane, 0, a.V.row, a.d);
+    auto ask = [&](int j, int at) INLINE {
+        const int rows = j < tiles ? s.m - j * FEW_KEYS : 0;
+        ask_k(K + (long long)j * FEW_KEYS * a.K.row, rows, a.K.row, a.d, ring + at * STAGE, 0);
+        ask_v(V + (long long)j * FEW_KEYS * a.V.row, rows, a.V.row, a.d, ring + at * STAGE + request::BYTES, 0);
+    };
+    if (wave < tiles) ask(wave, 0);
+    frag q[tile::T], dO[tile::T];
+    float D = 0.0f, lse2 = 0.0f;
+    {
+        const long long row = s.q0 + me.token;
+        const char *pq = row_of(a.Q, me.head, row), *pd = row_of(a.dO, me.head, row), *po = row_of(a.O, me.head, row);
+#pragma unroll
+        for (int k = 0; k < tile::T; ++k) {
+            const int at = (16 * k + 8 * hi) * (int)sizeof(ET);
+            const bool there = me.there && 16 * k + 8 * hi < a.d;
+            q[k] = there ? Frag<ET>::load(pq + at) : Frag<ET>::zero();
+            dO[k] = there ? Frag<ET>::load(pd + at) : Frag<ET>::zero();
+            const frag o = there ? Frag<ET>::load(po + at) : Frag<ET>::zero();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) D = fmaf(Frag<ET>::at(dO[k], e), Frag<ET>::at(o, e), D);
+        }
+        D = sum_of_halves(D);
+        const long long at = (long long)me.head * a.q_rows + row;
+        if (me.there) {
+            lse2 = a.lse[at] * LOG2E;
+            if (hi == 0 && wave == 0) a.stats[at] = make_float2(lse2, D);
+        }
     }
-    if (a.k_rows == 0) return hipSuccess;
-    static PerDeviceOnce once;
-    if constexpr (sizeof(ET) == 2) {
+    f32x16 g[tile::DB];
+#pragma unroll
+    for (int b = 0; b < tile::DB; ++b) clear(g[b]);
+    arrived(q);
+    arrived(dO);
+    if (wave < tiles) {
+        int at = 0;
+        for (int j = wave; j < tiles; j += FEW_WAVES) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot asked for next has been read
+            ask(j + FEW_WAVES, at ^ 1);
+            WAIT_VMCNT(2 * request::P);
+            const auto rows = t.rows_at(ring + at * STAGE);
+            const auto keys = t.keys_at(ring + at * STAGE);
+            f32x16 x, y;
+            clear(x);
+            clear(y);
+#pragma unroll
+            for (int k = 0; k < tile::T; ++k) {
+                x = Frag<ET>::mma(tile::by_rows(rows, 0, k), q[k], x);
+                y = Frag<ET>::mma(tile::by_rows(rows, 0, k, request::BYTES), dO[k], y);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = exp2_fast(fmaf(x[i], a.scale2, -lse2)) * (y[i] - D);
+            const int key = j * FEW_KEYS;
+            RARELY(key + 31 > least) {
+                APART();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = key + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? 0.0f : x[i];
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const frag ds = Frag<ET>::pack(x, k);
+#pragma unroll
+                for (int b = 0; b < tile::DB; ++b) g[b] = Frag<ET>::mma(tile::by_keys(keys, 16 * k, b), ds, g[b]);
+            }
+            at ^= 1;
+        }
+        WAIT_VMCNT(0);
+    }
+    LDS_BARRIER();                                         // the rings are done with: each wave's sums take their place
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int b = 0; b < tile::DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *(f32x4*)&sums[(wave * 32 + col) * PITCH + 32 * b + 8 * i + 4 * hi] = f32x4{g[b][4 * i], g[b][4 * i + 1], g[b][4 * i + 2], g[b][4 * i + 3]};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * DP / 4; i += FEW_WAVES * 64) {
+        const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+        const FewRow f = few_row(a, s, kv, r);
+        if (!f.there || c >= a.d) continue;
+        f32x4 v = *(const f32x4*)&sums[r * PITCH + c];
+#pragma unroll
+        for (int w = 1; w < FEW_WAVES; ++w) {
+            const f32x4 x = *(const f32x4*)&sums[(w * 32 + r) * PITCH + c];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        }
+        store_four<ET>(a.dQ.p + (long long)f.head * a.dQ.head + (long long)(s.q0 + f.token) * a.dQ.row + c * (int)sizeof(ET), v[0] * a.scale, v[1] * a.scale, v[2] * a.scale,
+                       v[3] * a.scale);
+    }
+}
+
+// Small calls, dK and dV: a block has 32 keys, its waves take tiles of 32 queries, of all heads that share the keys, in turn.
+template <typename ET, int DP, int FEW_WAVES>
+__global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dkv_few_kernel(attn_args a)
+{
+    typedef Tile<ET, DP> tile;
+    typedef Request<ET, DP, 32, 1> request;
+    typedef typename Frag<ET>::type frag;
+    constexpr int PITCH = DP + 4, REQUESTS = 2 * request::P + 1;
+    constexpr uint32_t STAGE = FewDkv<ET, DP>::STAGE;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
+    const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * FEW_STAGES * STAGE;
+    const int kv = blockIdx.x % a.kv_heads;
+    const Sequence s = find_sequence<32>(a, a.k_begin, a.k_rows, 1, blockIdx.x / a.kv_heads, lane);
+    if (s.tile < 0 || (long long)s.tile * 32 >= s.m) return;
+    const int shift = s.m - s.n, first = s.tile * 32, key = first + col;
+    const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the block's last
+
+    const tile t(lane);
+    const request ask_q(lane, 0, a.Q.row, a.d), ask_o(lane, 0, a.dO.row, a.d);
+    const Walk<32> walk(a, s, kv, first);
+    auto ask = [&](int u, int at) INLINE {
+        const int h = u < walk.steps ? u / walk.tiles : 0, j = u < walk.steps ? walk.start + u - h * walk.tiles : 0, rows = u < walk.steps ? s.n - j * 32 : 0;
+        const long long q = s.q0 + (long long)j * 32;
+        const int head = walk.first_head + h;
+        ask_q(row_of(a.Q, head, q), rows, a.Q.row, a.d, ring + at * STAGE, 0);
+        ask_o(row_of(a.dO, head, q), rows, a.dO.row, a.d, ring + at * STAGE + request::BYTES, 0);
+        dma4(tile_rsrc((const char*)(a.stats + (long long)head * a.q_rows + q), rows > 0 ? min(rows, 32) * 8 : 0), ring + at * STAGE + 2 * request::BYTES, lane * 4);
+    };
+    if (wave < walk.steps) ask(wave, 0);
+    frag K[tile::T], V[tile::T];
+    {
+        const char *pk = row_of(a.K, kv, s.k0 + key), *pv = row_of(a.V, kv, s.k0 + key);
+#pragma unroll
+        for (int k = 0; k < tile::T; ++k) {
+            const int at = (16 * k + 8 * hi) * (int)sizeof(ET);
+            const bool there = key < s.m && 16 * k + 8 * hi < a.d;
+            K[k] = there ? Frag<ET>::load(pk + at) : Frag<ET>::zero();
+            V[k] = there ? Frag<ET>::load(pv + at) : Frag<ET>::zero();
+        }
+    }
+    f32x16 dK[tile::DB], dV[tile::DB];
+#pragma unroll
+    for (int b = 0; b < tile::DB; ++b) {
+        clear(dK[b]);
+        clear(dV[b]);
+    }
+    arrived(K);
+    arrived(V);
+    if (wave < walk.steps) {
+        int at = 0;
+        for (int u = wave; u < walk.steps; u += FEW_WAVES) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot asked for next has been read
+            ask(u + FEW_WAVES, at ^ 1);
+            WAIT_VMCNT(REQUESTS);
+            const auto rows = t.rows_at(ring + at * STAGE);
+            const auto keys = t.keys_at(ring + at * STAGE);
+            const int query = (walk.start + u % walk.tiles) * 32;
+            f32x16 x, y;
+            clear(x);
+            clear(y);
+#pragma unroll
+            for (int k = 0; k < tile::T; ++k) {
+                x = Frag<ET>::mma(tile::by_rows(rows, 0, k), K[k], x);
+                y = Frag<ET>::mma(tile::by_rows(rows, 0, k, request::BYTES), V[k], y);
+            }
+            weigh(x, y, ring + at * STAGE + 2 * request::BYTES, a.scale2, hi);
+            RARELY(query < last) hide_queries(x, y, query, mine, hi);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const frag p = Frag<ET>::pack(x, k), ds = Frag<ET>::pack(y, k);
+#pragma unroll
+                for (int b = 0; b < tile::DB; ++b) {
+                    dV[b] = Frag<ET>::mma(p, tile::by_keys(keys, 16 * k, b, request::BYTES), dV[b]);
+                    dK[b] = Frag<ET>::mma(ds, tile::by_keys(keys, 16 * k, b), dK[b]);
+                }
+            }
+            at ^= 1;
+        }
+        WAIT_VMCNT(0);
+    }
+    // one gradient after the other through the place of the rings
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        LDS_BARRIER();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int b = 0; b < tile::DB; ++b) sums[(wave * 32 + 8 * (i >> 2) + 4 * hi + (i & 3)) * PITCH + 32 * b + col] = which ? dV[b][i] : dK[b][i];
+        __syncthreads();
+        const heads_t& to = which ? a.dV : a.dK;
+        const float by = which ? 1.0f : a.scale;
+        for (int i = threadIdx.x; i < 32 * DP / 4; i += FEW_WAVES * 64) {
+            const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+            if (first + r >= s.m || c >= a.d) continue;
+            f32x4 v = *(const f32x4*)&sums[r * PITCH + c];
+#pragma unroll
+            for (int w = 1; w < FEW_WAVES; ++w) {
+                const f32x4 x = *(const f32x4*)&sums[(w * 32 + r) * PITCH + c];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += x[e];
+            }
+            store_four<ET>(to.p + (long long)kv * to.head + (long long)(s.k0 + first + r) * to.row + c * (int)sizeof(ET), v[0] * by, v[1] * by, v[2] * by, v[3] * by);
+        }
+    }
+}
+
+template <typename ET, int DP> hipError_t launch_dq(const attn_args& a, hipStream_t st)
+{
+    const long long blocks = ((long long)a.q_rows / SIDE + a.seqs) * a.heads;
+    static PerDeviceOnce once, once_few;
+    hipError_t e;
+    if (is_small(blocks)) {
+        constexpr int W = few_waves<ET, DP>();
+        constexpr size_t join = (size_t)W * 32 * (DP + 4) * 4, ring = (size_t)W * FEW_STAGES * 2 * Request<ET, DP, FEW_KEYS, 1>::BYTES, bytes = ring > join ? ring : join;
+        if ((e = allow_lds(attend_dq_few_kernel<ET, DP, W>, bytes, once_few)) != hipSuccess) return e;
+        hipLaunchKernelGGL((attend_dq_few_kernel<ET, DP, W>), dim3((unsigned)few_units(a)), dim3(W * 64), bytes, st, a);
+    } else {
+        constexpr size_t bytes = (size_t)STAGES * 2 * Request<ET, DP, keys_of<ET, DP>(), WAVES>::BYTES;
+        if ((e = allow_lds(attend_dq_kernel<ET, DP>, bytes, once)) != hipSuccess) return e;
+        hipLaunchKernelGGL((attend_dq_kernel<ET, DP>), dim3((unsigned)blocks), dim3(WAVES * 64), bytes, st, a);
+    }
+    return hipGetLastError();
+}
+
+template <typename ET, int DP> hipError_t launch_dkv(const attn_args& a, hipStream_t st)
+{
+    const long long blocks = ((long long)a.k_rows / SIDE + a.seqs) * a.kv_heads;
+    static PerDeviceOnce once, once_few;
+    hipError_t e;
+    if (is_small(blocks)) {
+        constexpr int W = few_waves<ET, DP>();
+        constexpr size_t join = (size_t)W * 32 * (DP + 4) * 4, ring = (size_t)W * FEW_STAGES * FewDkv<ET, DP>::STAGE, bytes = ring > join ? ring : join;
+        if ((e = allow_lds(attend_dkv_few_kernel<ET, DP, W>, bytes, once_few)) != hipSuccess) return e;
+        hipLaunchKernelGGL((attend_dkv_few_kernel<ET, DP, W>), dim3((unsigned)((a.k_rows / 32 + a.seqs) * a.kv_heads)), dim3(W * 64), bytes, st, a);
+    } else if constexpr (sizeof(ET) == 2) {
         if ((e = allow_lds(attend_dkv_kernel<DP>, Dkv<DP>::LDS, once)) != hipSuccess) return e;
-        const long long slots = a.k_rows / SIDE + a.seqs;
-        hipLaunchKernelGGL((attend_dkv_kernel<DP>), dim3((unsigned)(slots * a.kv_heads)), dim3(WAVES * 64), Dkv<DP>::LDS, st, a);
+        hipLaunchKernelGGL((attend_dkv_kernel<DP>), dim3((unsigned)blocks), dim3(WAVES * 64), Dkv<DP>::LDS, st, a);
     } else {
         constexpr size_t bytes = 2 * (2 * Request<float, DP, 64, 4>::BYTES + 4 * 64 * 8);
         if ((e = allow_lds(attend_dkv_f32_kernel<DP>, bytes, once)) != hipSuccess) return e;
-        const long long slots = a.k_rows / 128 + a.seqs;
-        hipLaunchKernelGGL((attend_dkv_f32_kernel<DP>), dim3((unsigned)(slots * a.kv_heads)), dim3(256), bytes, st, a);
+        hipLaunchKernelGGL((attend_dkv_f32_kernel<DP>), dim3((unsigned)((a.k_rows / 128 + a.seqs) * a.kv_heads)), dim3(256), bytes, st, a);
     }
     return hipGetLastError();
+}
+
+template <typename ET, int DP> hipError_t attend_bwd(const attn_args& a, hipStream_t st)
+{
+    const hipError_t e = a.q_rows > 0 ? launch_dq<ET, DP>(a, st) : hipSuccess;         // leaves the statistics that the other one reads
+    return e != hipSuccess || a.k_rows == 0 ? e : launch_dkv<ET, DP>(a, st);
 }
 
 }  // namespace

@@ -63,6 +63,31 @@ def test_groups_of_heads(heads, kv, dtype):
     _check(Q, K, V, lens, dtype)
 
 
+# More blocks of 256 queries, or of 256 keys, than there are CUs: fewer are worked on by the kernels of few rows.
+MANY = [300, 1, 0, 257, 64, 513, 31, 700, 256]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv,d,layout", [(18, 18, 128, "fused"), (36, 18, 64, "heads"), (20, 20, 72, "apart"), (40, 20, 32, "fused"), (24, 24, 8, "heads")])
+def test_many_blocks(heads, kv, d, layout, causal, dtype):
+    Q, K, V = A.tensors(sum(MANY), (heads, kv, kv), d, A.TYPES[dtype], layout, heads + d)
+    _check(Q, K, V, MANY, dtype, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_blocks_more_and_fewer_keys(causal, dtype):
+    keys = [500, 70, 64, 0, 64, 512, 300, 65, 1000]
+    Q, = A.tensors(sum(MANY), (20,), 64, A.TYPES[dtype], "apart", 3)
+    K, V = A.tensors(sum(keys), (20, 20), 64, A.TYPES[dtype], "fused", 4)
+    K[500:570], V[500:570] = math.nan, math.inf            # the keys of one sequence, whose only query is not looked at
+    at = binding.Attention(heads=20, kv_heads=20, d=64, dtype=dtype, rows=sum(MANY), k_rows=sum(keys), seqs=len(MANY), causal=causal, device=G.DEV)
+    O, lse = _run(at, Q, K, V, A.offsets(MANY), _where(keys))
+    wO, bO, wl, bl = A.forward(Q, K, V, [p for i, p in enumerate(_parts(MANY, keys)) if i != 1], 64 ** -0.5, causal)
+    assert A.near(O, wO, bO) and A.near(lse, wl, bl)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("lens", [[1], [2, 1], [255], [256], [257], [31, 32, 33], [63, 64, 65, 66], [0, 0, 129, 0], [511, 513], [1] * 70 + [200], [1500, 3]])
 def test_lengths(lens, causal):
@@ -123,12 +148,11 @@ def test_layouts_and_rows_of_no_sequence(layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("few", [False, True])
-def test_values_out_of_the_ordinary(few, dtype):
+@pytest.mark.parametrize("n,heads", [(3, 2), (400, 2), (400, 44)])
+def test_values_out_of_the_ordinary(n, heads, dtype):
     """Scores far apart, equal ones, all zeros; a NaN or an infinity in a query stays in its row, one in a key in the rows that see it, one of another
     sequence or behind the end nowhere."""
-    t, heads, kv, d = A.TYPES[dtype], 2, 1, 64
-    n, m = (3, 400) if few else (400, 400)
+    t, kv, d, m = A.TYPES[dtype], 1, 64, 400
     lens, keys = [n, n, n], [m, m, m]
     Q, = A.tensors(3 * n, (heads,), d, t, "apart", 11)
     K, V = A.tensors(3 * m, (kv, kv), d, t, "apart", 12)
@@ -161,9 +185,10 @@ def _check_some(Q, K, V, lens, keys, dtype, which):
     return O, lse
 
 
-def test_offsets_that_are_wrong():
+@pytest.mark.parametrize("heads", [4, 64])
+def test_offsets_that_are_wrong(heads):
     """Held inside the tensors, whatever they are: sequences that are right stay right, nothing outside is written."""
-    t, heads, d, rows = torch.bfloat16, 4, 64, 600
+    t, d, rows = torch.bfloat16, 64, 600
     Q, K, V = A.tensors(rows, (heads, heads, heads), d, t, "apart", 13)
     at = binding.Attention(heads=heads, kv_heads=heads, d=d, dtype="bf16", rows=rows, seqs=4, device=G.DEV)
     guard = torch.full((rows + 40, heads, d), 7.0, dtype=t, device=G.DEV)
@@ -177,10 +202,10 @@ def test_offsets_that_are_wrong():
         assert (guard[:20] == 7.0).all() and (guard[20 + rows:] == 7.0).all()
 
 
-@pytest.mark.parametrize("lens", [[700, 33, 0, 600], [1] * 8])
-def test_captured(lens):
+@pytest.mark.parametrize("lens,heads", [([700, 33, 0, 600], 8), ([700, 33, 0, 600], 32), ([1] * 8, 8)])
+def test_captured(lens, heads):
     """A graph replayed on new inputs and new lengths among eager calls: each replay what the eager call gives."""
-    heads, kv, d, rows = 8, 2, 128, sum(lens)
+    kv, d, rows = heads // 4, 128, sum(lens)
     keys = [n + 500 for n in lens]
     Q, = A.tensors(rows, (heads,), d, torch.bfloat16, "apart", 1)
     K, V = A.tensors(sum(keys), (kv, kv), d, torch.bfloat16, "apart", 2)
@@ -220,24 +245,24 @@ def test_two_streams():
     assert all(torch.equal(o, want) for o in outs)
 
 
-@pytest.mark.parametrize("few", [False, True])
-def test_keys_past_32_bits(few):
+@pytest.mark.parametrize("n,heads", [(2, 2), (300, 2), (300, 160)])
+def test_keys_past_32_bits(n, heads):
     """A cache whose rows lie 4 MB apart: the last of them more than 2^32 bytes in."""
     d, m, row = 64, 2500, 2 ** 21 - 8
-    n = 2 if few else 300
     whole = torch.empty(m * row, dtype=torch.bfloat16, device=G.DEV)
     K, V = (whole.as_strided((m, 1, d), (row, d, 1), o) for o in (0, 1024))
     for x, y in zip((K, V), A.tensors(m, (1, 1), d, torch.bfloat16, "apart", 3)):
         x.copy_(y)
-    Q, = A.tensors(n, (2,), d, torch.bfloat16, "apart", 4)
+    Q, = A.tensors(n, (heads,), d, torch.bfloat16, "apart", 4)
     _check(Q, K, V, [n], "bf16", keys=[m], begin=[0])
 
 
 def test_long_sequence():
     """16384 keys for the last 600 queries, and one query for all of them."""
-    Q, = A.tensors(600, (2,), 128, torch.bfloat16, "apart", 3)
-    K, V = A.tensors(16384, (1, 1), 128, torch.bfloat16, "apart", 4)
+    Q, = A.tensors(600, (88,), 128, torch.bfloat16, "apart", 3)
+    K, V = A.tensors(16384, (2, 2), 128, torch.bfloat16, "apart", 4)
     _check(Q, K, V, [600], "bf16", keys=[16384])
+    _check(Q[:, :4], K, V, [600], "bf16", keys=[16384])
     _check(Q[:1], K, V, [1], "bf16", keys=[16384])
 
 

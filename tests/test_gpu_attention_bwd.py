@@ -8,7 +8,7 @@ import torch
 import attn_util as A
 import gpu_util as G
 from paper_2411_10003_amd import binding
-from test_gpu_attention import _parts, _where
+from test_gpu_attention import MANY, _parts, _where
 
 pytestmark = pytest.mark.gpu
 
@@ -62,6 +62,24 @@ def test_groups_of_heads(heads, kv, dtype):
     lens = [5, 257, 33, 512]
     Q, K, V = A.tensors(sum(lens), (heads, kv, kv), 64, A.TYPES[dtype], "apart", heads * 10 + kv)
     _check(Q, K, V, lens, dtype, layout="heads")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv,d,layout", [(18, 18, 128, "fused"), (36, 18, 64, "heads"), (20, 20, 72, "apart"), (40, 20, 32, "fused"), (24, 24, 8, "heads"), (36, 2, 128, "apart")])
+def test_many_blocks(heads, kv, d, layout, causal, dtype):
+    """The kernels of large calls; with two kv heads the first of them and that of few keys."""
+    Q, K, V = A.tensors(sum(MANY), (heads, kv, kv), d, A.TYPES[dtype], layout, heads + d)
+    _check(Q, K, V, MANY, dtype, causal=causal, layout="heads" if layout == "heads" else "apart")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_blocks_more_and_fewer_keys(causal, dtype):
+    keys = [500, 70, 64, 0, 64, 512, 300, 65, 1000]
+    Q, = A.tensors(sum(MANY), (20,), 64, A.TYPES[dtype], "apart", 3)
+    K, V = A.tensors(sum(keys), (20, 20), 64, A.TYPES[dtype], "fused", 4)
+    _check(Q, K, V, MANY, dtype, causal=causal, keys=keys)
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -145,9 +163,10 @@ def test_gradient_against_differences():
         assert allowed < 0.5 * abs(got), (i, got, allowed)  # a factor of two or a sign would show
 
 
-def test_values_out_of_the_ordinary():
+@pytest.mark.parametrize("heads,kv", [(4, 2), (120, 60)])
+def test_values_out_of_the_ordinary(heads, kv):
     """Scores far apart; a NaN of one sequence stays in it."""
-    lens, heads, kv, d = [200, 150, 170], 4, 2, 64
+    lens, d = [200, 150, 170], 64
     Q, K, V = A.tensors(520, (heads, kv, kv), d, torch.bfloat16, "apart", 8)
     Q[3] *= 40.0
     Q[4] = 0.0
@@ -163,9 +182,10 @@ def test_values_out_of_the_ordinary():
         assert torch.equal(a[:200], b[:200]) and torch.equal(a[350:], b[350:])
 
 
-def test_captured():
+@pytest.mark.parametrize("heads,kv", [(4, 2), (96, 48)])
+def test_captured(heads, kv):
     """Forward and backward in one graph, replayed on new inputs among eager calls; the graph's calls have a workspace of their own."""
-    lens, heads, kv, d, rows = [300, 1, 0, 211], 4, 2, 128, 512
+    lens, d, rows = [300, 1, 0, 211], 128, 512
     off = A.offsets(lens)
     make = lambda: binding.Attention(heads=heads, kv_heads=kv, d=d, dtype="bf16", rows=rows, seqs=4, device=G.DEV)  # noqa: E731
     ats = [make(), make()]
