@@ -241,7 +241,7 @@ struct attn_args {
     const int32_t *offsets, *k_begin, *k_end;
     int q_rows, k_rows, seqs, heads, kv_heads, group, d, causal, splits, chunk;
     float scale, scale2;                   // scale2 = scale log2 e: exponentials are powers of two
-    float* partial;
+    float *partial, *partial_k;
 };
 inline heads_t in_bytes(const moe_heads_t& t, int size) { return heads_t{(char*)t.p, (uint32_t)(t.row * size), t.head * size}; }
 __device__ __forceinline__ const char* row_of(const heads_t& t, int head, long long row) { return t.p + (long long)head * t.head + row * t.row; }
@@ -303,6 +303,16 @@ __device__ __forceinline__ int few_keys(const attn_args& a, const Sequence& s)
 // Blocks of 32 rows, and whether a call of so many larger blocks is one for them: up to one for each CU, the longest of which all the others would wait for.
 inline long long few_units(const attn_args& a) { return ((long long)a.q_rows * a.group / 32 + a.seqs) * a.kv_heads; }
 inline bool is_small(long long blocks) { return blocks <= 256; }
+// How the tiles of 32 along a block's other axis are cut into parts, blocks of their own: `chunk` tiles a part as the launch has it, more where that does not reach the
+// end.  Parts past the end have nothing to do; a part that is alone writes its rows itself, others are joined by a later launch.
+struct Parts {
+    int chunk, used;
+    __device__ __forceinline__ Parts(const attn_args& a, int tiles)
+    {
+        chunk = max(a.chunk, (tiles + a.splits - 1) / a.splits);
+        used = max(1, (tiles + chunk - 1) / chunk);
+    }
+};
 
 // Blocks go to the eight XCDs in turn: where the heads are a multiple of eight, an XCD works on heads / 8 neighbouring ones, whose keys and values are the
 // same ones where heads share them, and its L2 holds those only.

@@ -234,17 +234,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
 constexpr int PARTIAL_MORE = 64;                           // of a part's 32 rows: maximum and sum
 template <int DP> constexpr int partial_floats() { return 32 * DP + PARTIAL_MORE; }
 
-// How the keys that a block's rows see are cut: `chunk` tiles a part as the launch has it, more where that does not reach the end.
-struct Parts {
-    int tiles, chunk, used;
-    __device__ __forceinline__ Parts(const attn_args& a, int keys)
-    {
-        tiles = (keys + FEW_KEYS - 1) / FEW_KEYS;
-        chunk = max(a.chunk, (tiles + a.splits - 1) / a.splits);
-        used = max(1, (tiles + chunk - 1) / chunk);
-    }
-};
-
 template <typename ET, int DP>
 __device__ __forceinline__ void few_store(const attn_args& a, const Sequence& s, const FewRow& f, int c, float v0, float v1, float v2, float v3)
 {
@@ -271,8 +260,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_few_kernel(attn_args
     const int shift = s.m - s.n, keys = few_keys(a, s);
     const int limit = (a.causal ? min(s.m, me.token + shift + 1) : s.m) - 1;
     const int least = (a.causal ? min(s.m, (int)((long long)s.tile * 32 / a.group) + shift + 1) : s.m) - 1;
-    const Parts parts(a, keys);
-    const int begin = part * parts.chunk, end = min(parts.tiles, begin + parts.chunk);
+    const int tiles = (keys + FEW_KEYS - 1) / FEW_KEYS;
+    const Parts parts(a, tiles);
+    const int begin = part * parts.chunk, end = min(tiles, begin + parts.chunk);
     if (part >= parts.used) return;
 
     const char* K = row_of(a.K, kv, s.k0);
@@ -361,7 +351,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(attn_args a)
     const int unit = blockIdx.x, kv = unit % a.kv_heads;
     const Sequence s = find_sequence<32>(a, a.offsets, a.q_rows, a.group, unit / a.kv_heads, threadIdx.x & 63);
     if (s.tile < 0 || (long long)s.tile * 32 >= (long long)s.n * a.group) return;
-    const Parts parts(a, few_keys(a, s));
+    const Parts parts(a, (few_keys(a, s) + FEW_KEYS - 1) / FEW_KEYS);
     if (parts.used == 1) return;                           // written already
     for (int i = threadIdx.x; i < 32 * DP / 4; i += 256) {
         const int q = i / (DP / 4), c = i % (DP / 4) * 4;
@@ -426,13 +416,16 @@ template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t
 
 }  // namespace
 
-// The kept parts of a forward call of few rows, or the rows' statistics of a backward call.
+// The kept parts of a forward call of few rows, or the rows' statistics and the kept parts of a small backward call; of this or any smaller call.
 size_t attn_workspace_bytes(const moe_attn_t& c)
 {
-    const int dp = c.d <= 64 ? 64 : 128;
-    const long long units = ((long long)c.q_rows * (c.heads / c.kv_heads) / 32 + c.seqs) * c.kv_heads, each = c.k_rows / (FEW_KEYS * 4) + 1;
-    const size_t parts = units < ATTN_PARTS && units * each < ATTN_PARTS ? units * each : ATTN_PARTS;
-    const size_t fwd = parts * (32 * dp + PARTIAL_MORE) * sizeof(float), bwd = (size_t)c.heads * c.q_rows * sizeof(float2);
+    const size_t row = 32 * (c.d <= 64 ? 64 : 128);
+    const long long group = c.heads / c.kv_heads, units = ((long long)c.q_rows * group / 32 + c.seqs) * c.kv_heads, units_k = ((long long)c.k_rows / 32 + c.seqs) * c.kv_heads;
+    auto most = [](long long units, long long each, long long all) { return (size_t)(units < all && units * each < all ? units * each : all); };
+    const size_t fwd = most(units, c.k_rows / (FEW_KEYS * 4) + 1, ATTN_PARTS) * (row + PARTIAL_MORE) * sizeof(float);
+    const size_t dq = most(units, c.k_rows / (32 * ATTN_PART_TILES) + 1, ATTN_BWD_PARTS) * row * sizeof(float);
+    const size_t dkv = most(units_k, group * c.q_rows / (32 * ATTN_PART_TILES) + 1, ATTN_BWD_PARTS) * 2 * row * sizeof(float);
+    const size_t bwd = attn_stats_bytes(c.heads, c.q_rows) + (dq > dkv ? dq : dkv);            // one after the other
     return ((fwd > bwd ? fwd : bwd) + 256) / 256 * 256;
 }
 

@@ -540,11 +540,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_a
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * FEW_STAGES * STAGE;
-    const int kv = blockIdx.x % a.kv_heads;
-    const Sequence s = find_sequence<32>(a, a.offsets, a.q_rows, a.group, blockIdx.x / a.kv_heads, lane);
+    const int part = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, kv = unit % a.kv_heads;
+    const Sequence s = find_sequence<32>(a, a.offsets, a.q_rows, a.group, unit / a.kv_heads, lane);
     if (s.tile < 0 || (long long)s.tile * 32 >= (long long)s.n * a.group) return;
     const FewRow me = few_row(a, s, kv, col);
     const int shift = s.m - s.n, tiles = uniform((few_keys(a, s) + FEW_KEYS - 1) / FEW_KEYS);
+    const Parts parts(a, tiles);
+    const int begin = part * parts.chunk + wave, end = uniform(min(tiles, (part + 1) * parts.chunk));
+    if (part >= parts.used) return;
     const int limit = (a.causal ? min(s.m, me.token + shift + 1) : s.m) - 1, least = (a.causal ? min(s.m, (int)((long long)s.tile * 32 / a.group) + shift + 1) : s.m) - 1;
 
     const char* K = row_of(a.K, kv, s.k0);
@@ -552,11 +555,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_a
     const tile t(lane);
     const request ask_k(lane, 0, a.K.row, a.d), ask_v(lane, 0, a.V.row, a.d);
     auto ask = [&](int j, int at) INLINE {
-        const int rows = j < tiles ? s.m - j * FEW_KEYS : 0;
+        const int rows = j < end ? s.m - j * FEW_KEYS : 0;
         ask_k(K + (long long)j * FEW_KEYS * a.K.row, rows, a.K.row, a.d, ring + at * STAGE, 0);
         ask_v(V + (long long)j * FEW_KEYS * a.V.row, rows, a.V.row, a.d, ring + at * STAGE + request::BYTES, 0);
     };
-    if (wave < tiles) ask(wave, 0);
+    if (begin < end) ask(begin, 0);
     frag q[tile::T], dO[tile::T];
     float D = 0.0f, lse2 = 0.0f;
     {
@@ -576,7 +579,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_a
         const long long at = (long long)me.head * a.q_rows + row;
         if (me.there) {
             lse2 = a.lse[at] * LOG2E;
-            if (hi == 0 && wave == 0) a.stats[at] = make_float2(lse2, D);
+            if (hi == 0 && wave == 0 && part == 0) a.stats[at] = make_float2(lse2, D);
         }
     }
     f32x16 g[tile::DB];
@@ -584,9 +587,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_a
     for (int b = 0; b < tile::DB; ++b) clear(g[b]);
     arrived(q);
     arrived(dO);
-    if (wave < tiles) {
+    if (begin < end) {
         int at = 0;
-        for (int j = wave; j < tiles; j += FEW_WAVES) {
+        for (int j = begin; j < end; j += FEW_WAVES) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot asked for next has been read
             ask(j + FEW_WAVES, at ^ 1);
             WAIT_VMCNT(2 * request::P);
@@ -637,6 +640,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dq_few_kernel(attn_a
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
+        if (parts.used > 1) {
+            *(f32x4*)&a.partial[((size_t)blockIdx.x * 32 + r) * DP + c] = v;
+            continue;
+        }
         store_four<ET>(a.dQ.p + (long long)f.head * a.dQ.head + (long long)(s.q0 + f.token) * a.dQ.row + c * (int)sizeof(ET), v[0] * a.scale, v[1] * a.scale, v[2] * a.scale,
                        v[3] * a.scale);
     }
@@ -654,8 +661,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dkv_few_kernel(attn_
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
     const uint32_t ring = (uint32_t)(uintptr_t)(LDS_PTR(char))lds + wave * FEW_STAGES * STAGE;
-    const int kv = blockIdx.x % a.kv_heads;
-    const Sequence s = find_sequence<32>(a, a.k_begin, a.k_rows, 1, blockIdx.x / a.kv_heads, lane);
+    const int part = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, kv = unit % a.kv_heads;
+    const Sequence s = find_sequence<32>(a, a.k_begin, a.k_rows, 1, unit / a.kv_heads, lane);
     if (s.tile < 0 || (long long)s.tile * 32 >= s.m) return;
     const int shift = s.m - s.n, first = s.tile * 32, key = first + col;
     const int mine = a.causal ? key - shift : 0, last = a.causal ? first + 31 - shift : 0;      // the first query that sees this lane's key, the block's last
@@ -663,15 +670,18 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dkv_few_kernel(attn_
     const tile t(lane);
     const request ask_q(lane, 0, a.Q.row, a.d), ask_o(lane, 0, a.dO.row, a.d);
     const Walk<32> walk(a, s, kv, first);
+    const Parts parts(a, walk.steps);
+    const int begin = part * parts.chunk + wave, end = uniform(min(walk.steps, (part + 1) * parts.chunk));
+    if (part >= parts.used) return;
     auto ask = [&](int u, int at) INLINE {
-        const int h = u < walk.steps ? u / walk.tiles : 0, j = u < walk.steps ? walk.start + u - h * walk.tiles : 0, rows = u < walk.steps ? s.n - j * 32 : 0;
+        const int h = u < end ? u / walk.tiles : 0, j = u < end ? walk.start + u - h * walk.tiles : 0, rows = u < end ? s.n - j * 32 : 0;
         const long long q = s.q0 + (long long)j * 32;
         const int head = walk.first_head + h;
         ask_q(row_of(a.Q, head, q), rows, a.Q.row, a.d, ring + at * STAGE, 0);
         ask_o(row_of(a.dO, head, q), rows, a.dO.row, a.d, ring + at * STAGE + request::BYTES, 0);
         dma4(tile_rsrc((const char*)(a.stats + (long long)head * a.q_rows + q), rows > 0 ? min(rows, 32) * 8 : 0), ring + at * STAGE + 2 * request::BYTES, lane * 4);
     };
-    if (wave < walk.steps) ask(wave, 0);
+    if (begin < end) ask(begin, 0);
     frag K[tile::T], V[tile::T];
     {
         const char *pk = row_of(a.K, kv, s.k0 + key), *pv = row_of(a.V, kv, s.k0 + key);
@@ -691,9 +701,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dkv_few_kernel(attn_
     }
     arrived(K);
     arrived(V);
-    if (wave < walk.steps) {
+    if (begin < end) {
         int at = 0;
-        for (int u = wave; u < walk.steps; u += FEW_WAVES) {
+        for (int u = begin; u < end; u += FEW_WAVES) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot asked for next has been read
             ask(u + FEW_WAVES, at ^ 1);
             WAIT_VMCNT(REQUESTS);
@@ -745,12 +755,52 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 1) void attend_dkv_few_kernel(attn_
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += x[e];
             }
-            store_four<ET>(to.p + (long long)kv * to.head + (long long)(s.k0 + first + r) * to.row + c * (int)sizeof(ET), v[0] * by, v[1] * by, v[2] * by, v[3] * by);
+            if (parts.used > 1) *(f32x4*)&a.partial_k[(((size_t)blockIdx.x * 2 + which) * 32 + r) * DP + c] = v;
+            else store_four<ET>(to.p + (long long)kv * to.head + (long long)(s.k0 + first + r) * to.row + c * (int)sizeof(ET), v[0] * by, v[1] * by, v[2] * by, v[3] * by);
         }
     }
 }
 
-template <typename ET, int DP> hipError_t launch_dq(const attn_args& a, hipStream_t st)
+// The parts of small calls' gradients, joined in their order: blockIdx.x is a unit of the one kernel (of_keys 0) or the other.
+template <typename ET, int DP>
+__global__ __launch_bounds__(256) void attend_bwd_join_kernel(attn_args a, int of_keys)
+{
+    const int unit = blockIdx.x, kv = unit % a.kv_heads, lane = threadIdx.x & 63;
+    const Sequence s = of_keys ? find_sequence<32>(a, a.k_begin, a.k_rows, 1, unit / a.kv_heads, lane) : find_sequence<32>(a, a.offsets, a.q_rows, a.group, unit / a.kv_heads, lane);
+    if (s.tile < 0 || (long long)s.tile * 32 >= (of_keys ? (long long)s.m : (long long)s.n * a.group)) return;
+    const Parts parts(a, of_keys ? Walk<32>(a, s, kv, s.tile * 32).steps : (few_keys(a, s) + FEW_KEYS - 1) / FEW_KEYS);
+    if (parts.used == 1) return;                           // written already
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < (of_keys ? 2 : 1) * 32 * DP / 4; i += 256 * gridDim.y) {
+        const int which = i / (32 * DP / 4), r = i / (DP / 4) % 32, c = i % (DP / 4) * 4;
+        const FewRow f = few_row(a, s, kv, r);
+        if ((of_keys ? s.tile * 32 + r >= s.m : !f.there) || c >= a.d) continue;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < parts.used; ++p) {
+            const size_t from = (size_t)unit * a.splits + p;
+            const f32x4 x = *(const f32x4*)(of_keys ? &a.partial_k[((from * 2 + which) * 32 + r) * DP + c] : &a.partial[(from * 32 + r) * DP + c]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        }
+        const float by = which ? 1.0f : a.scale;
+        char* to = of_keys ? (which ? a.dV.p + (long long)kv * a.dV.head + (long long)(s.k0 + s.tile * 32 + r) * a.dV.row
+                                    : a.dK.p + (long long)kv * a.dK.head + (long long)(s.k0 + s.tile * 32 + r) * a.dK.row)
+                           : a.dQ.p + (long long)f.head * a.dQ.head + (long long)(s.q0 + f.token) * a.dQ.row;
+        store_four<ET>(to + c * (int)sizeof(ET), v[0] * by, v[1] * by, v[2] * by, v[3] * by);
+    }
+}
+
+// Parts of a small call's blocks where those leave CUs without one: enough for ATTN_BWD_PARTS blocks in all, of ATTN_PART_TILES tiles at least for sequences eight times as
+// long as the average (fp32, 2003 rows in six sequences: the keys' gradients 108 -> 63 us with their join).
+inline void cut(attn_args& a, long long units, long long tiles_of_all)
+{
+    const long long longest = a.seqs > 8 ? tiles_of_all * 8 / a.seqs : tiles_of_all;
+    const long long want = units < 256 ? ATTN_BWD_PARTS / units : 1, most = longest / ATTN_PART_TILES;
+    a.splits = (int)(want < most ? want : most);
+    if (a.splits < 1) a.splits = 1;
+    a.chunk = ATTN_PART_TILES;
+}
+
+template <typename ET, int DP> hipError_t launch_dq(attn_args a, hipStream_t st)
 {
     const long long blocks = ((long long)a.q_rows / SIDE + a.seqs) * a.heads;
     static PerDeviceOnce once, once_few;
@@ -759,7 +809,11 @@ template <typename ET, int DP> hipError_t launch_dq(const attn_args& a, hipStrea
         constexpr int W = few_waves<ET, DP>();
         constexpr size_t join = (size_t)W * 32 * (DP + 4) * 4, ring = (size_t)W * FEW_STAGES * 2 * Request<ET, DP, FEW_KEYS, 1>::BYTES, bytes = ring > join ? ring : join;
         if ((e = allow_lds(attend_dq_few_kernel<ET, DP, W>, bytes, once_few)) != hipSuccess) return e;
-        hipLaunchKernelGGL((attend_dq_few_kernel<ET, DP, W>), dim3((unsigned)few_units(a)), dim3(W * 64), bytes, st, a);
+        const long long units = few_units(a);
+        cut(a, units, a.k_rows / 32);
+        hipLaunchKernelGGL((attend_dq_few_kernel<ET, DP, W>), dim3((unsigned)(units * a.splits)), dim3(W * 64), bytes, st, a);
+        if ((e = hipGetLastError()) != hipSuccess || a.splits == 1) return e;
+        hipLaunchKernelGGL((attend_bwd_join_kernel<ET, DP>), dim3((unsigned)units, 32 * DP / 4 / 256), dim3(256), 0, st, a, 0);
     } else {
         constexpr size_t bytes = (size_t)STAGES * 2 * Request<ET, DP, keys_of<ET, DP>(), WAVES>::BYTES;
         if ((e = allow_lds(attend_dq_kernel<ET, DP>, bytes, once)) != hipSuccess) return e;
@@ -768,7 +822,7 @@ template <typename ET, int DP> hipError_t launch_dq(const attn_args& a, hipStrea
     return hipGetLastError();
 }
 
-template <typename ET, int DP> hipError_t launch_dkv(const attn_args& a, hipStream_t st)
+template <typename ET, int DP> hipError_t launch_dkv(attn_args a, hipStream_t st)
 {
     const long long blocks = ((long long)a.k_rows / SIDE + a.seqs) * a.kv_heads;
     static PerDeviceOnce once, once_few;
@@ -777,7 +831,11 @@ template <typename ET, int DP> hipError_t launch_dkv(const attn_args& a, hipStre
         constexpr int W = few_waves<ET, DP>();
         constexpr size_t join = (size_t)W * 32 * (DP + 4) * 4, ring = (size_t)W * FEW_STAGES * FewDkv<ET, DP>::STAGE, bytes = ring > join ? ring : join;
         if ((e = allow_lds(attend_dkv_few_kernel<ET, DP, W>, bytes, once_few)) != hipSuccess) return e;
-        hipLaunchKernelGGL((attend_dkv_few_kernel<ET, DP, W>), dim3((unsigned)((a.k_rows / 32 + a.seqs) * a.kv_heads)), dim3(W * 64), bytes, st, a);
+        const long long units = ((long long)a.k_rows / 32 + a.seqs) * a.kv_heads;
+        cut(a, units, (long long)a.group * a.q_rows / 32);
+        hipLaunchKernelGGL((attend_dkv_few_kernel<ET, DP, W>), dim3((unsigned)(units * a.splits)), dim3(W * 64), bytes, st, a);
+        if ((e = hipGetLastError()) != hipSuccess || a.splits == 1) return e;
+        hipLaunchKernelGGL((attend_bwd_join_kernel<ET, DP>), dim3((unsigned)units, 2 * 32 * DP / 4 / 256), dim3(256), 0, st, a, 1);
     } else if constexpr (sizeof(ET) == 2) {
         if ((e = allow_lds(attend_dkv_kernel<DP>, Dkv<DP>::LDS, once)) != hipSuccess) return e;
         hipLaunchKernelGGL((attend_dkv_kernel<DP>), dim3((unsigned)blocks), dim3(WAVES * 64), Dkv<DP>::LDS, st, a);
@@ -807,7 +865,9 @@ hipError_t launch_attn_bwd(const moe_attn_t& c, const moe_heads_t& dO, const moe
     a.Q = in_bytes(Q, size), a.K = in_bytes(K, size), a.V = in_bytes(V, size), a.O = in_bytes(O, size), a.dO = in_bytes(dO, size);
     a.dQ = in_bytes(dQ, size), a.dK = in_bytes(dK, size), a.dV = in_bytes(dV, size);
     a.lse = const_cast<float*>(lse), a.stats = (float2*)ws;
+    a.partial = (float*)((char*)ws + attn_stats_bytes(c.heads, c.q_rows));
     a.offsets = offsets, a.k_begin = k_begin, a.k_end = k_end;
+    a.partial_k = a.partial;                               // the first kernel's parts are joined before the second one runs
     if (c.dtype == MOE_BF16) return c.d <= 64 ? attend_bwd<bf16_t, 64>(a, st) : attend_bwd<bf16_t, 128>(a, st);
     return c.d <= 64 ? attend_bwd<float, 64>(a, st) : attend_bwd<float, 128>(a, st);
 }
