@@ -444,7 +444,7 @@ int moe_rotary_workspace_bytes(const moe_rotary_t* cfg, size_t* bytes)
     const int rc = check_rotary(cfg);
     if (rc != MOE_OK) return rc;
     if (!bytes) return MOE_ERR_NULL;
-    *bytes = align256((size_t)ROTARY_PARTIALS * 2 * cfg->d * sizeof(float));
+    *bytes = align256((size_t)ROTARY_PARTIALS * cfg->d * sizeof(float));
     return MOE_OK;
 }
 

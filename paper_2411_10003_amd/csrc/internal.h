@@ -135,7 +135,9 @@ constexpr int ATTN_PARTS = 2048;       // parts of keys that a forward call of f
 constexpr int ATTN_BWD_PARTS = 1024;   // parts that each kernel of a small backward call may cut its blocks' work into, all together,
 constexpr int ATTN_PART_TILES = 16;    // of so many tiles of 32 at least
 inline size_t attn_stats_bytes(int heads, int q_rows) { return ((size_t)heads * q_rows * 2 * sizeof(float) + 255) / 256 * 256; }
-constexpr int ROTARY_PARTIALS = 512;   // blocks of the rotation's gradient, each with one partial sum of the norms' parameters
+// Blocks of the rotation's gradient with norms, each with a partial sum of one norm's parameters: as many as the registers let 256 CUs hold at once.
+// 32768 rows of 32 and 8 heads of 128, bf16, us: 512 blocks 223, 768 210, 1024 239.
+constexpr int ROTARY_PARTIALS = 768;
 hipError_t launch_rotary_fwd(const moe_rotary_t& c, const moe_heads_t& Q, const moe_heads_t& K, const moe_heads_t* V, const float* gamma_q, const float* gamma_k,
                              const int32_t* positions, const double* frequencies, const int32_t* slots, const moe_heads_t& Qo, const moe_heads_t& Ko,
                              const moe_heads_t* Vo, hipStream_t st);
