@@ -374,6 +374,7 @@ inline rotary_args make_args(const moe_rotary_t& c, const int32_t* positions, co
 // 32768 rows of 32 and 8 heads of 128 with norms, bf16, us: 2 rows a block 170, 4 rows 130 to 137, 9 rows 145.  7999 rows of 12 and 4 heads of 80: at least 256 blocks
 // 13.0, 1024 11.1, 4096 19.6.  The gradient with norms has no such bound on its blocks below ROTARY_PARTIALS: 512 tiny rows need 9.0 us so, 21.3 by few blocks.
 constexpr int ROUNDS = 6, LEAST = 1024;
+constexpr int MOST_BLOCKS = 1 << 22;                       // of a launch: its threads are counted in 32 bits
 inline int rows_at_once(const moe_rotary_t& c, int heads, int least)
 {
     int tph = 1;
@@ -403,19 +404,35 @@ hipError_t launch_rotary_fwd(const moe_rotary_t& c, const moe_heads_t& Q, const 
     if (V) a.side[a.sides++] = make_side(V, nullptr, Vo, nullptr, c.kv_heads, size);
     const bool few = c.rows <= 1024;
     a.rows_at_once = few ? 1 : rows_at_once(c, c.heads + c.kv_heads, LEAST);
-    const dim3 grid((unsigned)((c.rows + a.rows_at_once - 1) / a.rows_at_once), few ? a.sides : 1);
-    return by_head(c.d, c.rot, c.interleaved, [&](auto TPH, auto PAIRS) {
-        auto go = [&](auto ET, auto NORM, auto NT) {
-            hipLaunchKernelGGL((rotary_kernel<decltype(ET), decltype(TPH)::value, decltype(PAIRS)::value, decltype(NORM)::value, decltype(NT)::value>), grid, dim3(THREADS), 0, st, a);
-            return hipGetLastError();
-        };
-        const bool nt = streams_rows(c, size);
-        auto typed = [&](auto ET) {
-            if (c.norm) return nt ? go(ET, std::true_type{}, std::true_type{}) : go(ET, std::true_type{}, std::false_type{});
-            return nt ? go(ET, std::false_type{}, std::true_type{}) : go(ET, std::false_type{}, std::false_type{});
-        };
-        return size == 2 ? typed(bf16_t{}) : typed(float{});
-    });
+    auto launch = [&](int blocks) {
+        const dim3 grid(blocks, few ? a.sides : 1);
+        return by_head(c.d, c.rot, c.interleaved, [&](auto TPH, auto PAIRS) {
+            auto go = [&](auto ET, auto NORM, auto NT) {
+                hipLaunchKernelGGL((rotary_kernel<decltype(ET), decltype(TPH)::value, decltype(PAIRS)::value, decltype(NORM)::value, decltype(NT)::value>), grid, dim3(THREADS), 0, st, a);
+                return hipGetLastError();
+            };
+            const bool nt = streams_rows(c, size);
+            auto typed = [&](auto ET) {
+                if (c.norm) return nt ? go(ET, std::true_type{}, std::true_type{}) : go(ET, std::true_type{}, std::false_type{});
+                return nt ? go(ET, std::false_type{}, std::true_type{}) : go(ET, std::false_type{}, std::false_type{});
+            };
+            return size == 2 ? typed(bf16_t{}) : typed(float{});
+        });
+    };
+    // as many rows a launch as MOST_BLOCKS have; the pointers move on to the next ones, not those of a cache
+    const int most = (int)(((long long)MOST_BLOCKS * a.rows_at_once < c.rows) ? (long long)MOST_BLOCKS * a.rows_at_once : c.rows);
+    for (int left = c.rows; left > 0; left -= most) {
+        a.rows = left < most ? left : most;
+        const hipError_t e = launch((a.rows + a.rows_at_once - 1) / a.rows_at_once);
+        if (e != hipSuccess) return e;
+        a.positions += a.rows;
+        for (int k = 0; k < a.sides; ++k) {
+            a.side[k].in += a.rows * a.side[k].in_row;
+            if (k == 0 || !slots) a.side[k].out += a.rows * a.side[k].out_row;
+        }
+        if (slots) a.slots += a.rows;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_rotary_bwd(const moe_rotary_t& c, const moe_heads_t& dQo, const moe_heads_t& dKo, const moe_heads_t* Q, const moe_heads_t* K,
@@ -435,9 +452,14 @@ hipError_t launch_rotary_bwd(const moe_rotary_t& c, const moe_heads_t& dQo, cons
         a.rows_at_once = rows_at_once(c, c.heads, c.norm ? 64 : LEAST);
         a.rows_at_once_k = rows_at_once(c, c.kv_heads, c.norm ? 16 : LEAST / 4);
         const long long all_q = ((long long)c.rows + a.rows_at_once - 1) / a.rows_at_once, all_k = ((long long)c.rows + a.rows_at_once_k - 1) / a.rows_at_once_k;
-        const long long most_q = c.norm ? (long long)ROTARY_PARTIALS * c.heads / (c.heads + c.kv_heads) : all_q, most_k = c.norm ? ROTARY_PARTIALS - most_q : all_k;
-        a.blocks_q = (int)(all_q < most_q ? all_q : most_q > 1 ? most_q : 1);
-        blocks = a.blocks_q + (int)(all_k < most_k ? all_k : most_k > 1 ? most_k : 1);
+        long long most_q = MOST_BLOCKS, most_k = MOST_BLOCKS;
+        if (c.norm) {                                      // one at least of either, ROTARY_PARTIALS in all
+            most_q = (long long)ROTARY_PARTIALS * c.heads / (c.heads + c.kv_heads);
+            most_q = most_q < 1 ? 1 : most_q < ROTARY_PARTIALS ? most_q : ROTARY_PARTIALS - 1;
+            most_k = ROTARY_PARTIALS - most_q;
+        }
+        a.blocks_q = (int)(all_q < most_q ? all_q : most_q);
+        blocks = a.blocks_q + (int)(all_k < most_k ? all_k : most_k);
         e = by_head(c.d, c.rot, c.interleaved, [&](auto TPH, auto PAIRS) {
             auto go = [&](auto ET, auto NORM, auto NT) {
                 hipLaunchKernelGGL((rotary_bwd_kernel<decltype(ET), decltype(TPH)::value, decltype(PAIRS)::value, decltype(NORM)::value, decltype(NT)::value>), dim3(blocks), dim3(THREADS), 0, st, a);

@@ -108,6 +108,40 @@ def test_many_rows(rows, heads, kv, d):
     _check(rows, heads, kv, d, "bf16", rot=d // 8 * 4, interleaved=True, norm=False, layout="heads", amplitude=1.2)
 
 
+@pytest.mark.parametrize("rows,heads,kv,d", [(2000, 1, 1000, 8), (1500, 700, 1, 8), (900, 1, 1, 128)])
+def test_partial_sums_stay_in_the_workspace(rows, heads, kv, d):
+    """However the heads are shared out between queries and keys: more blocks than partial sums of either, and what lies behind the workspace stays."""
+    Q, K, V, gammas, dQo, dKo, pos = _inputs(rows, heads, kv, d, "bf16", 5, "apart")
+    f = binding.rotary_frequencies(d, device=G.DEV)
+    r = binding.Rotary(heads=heads, kv_heads=kv, d=d, dtype="bf16", norm=True, device=G.DEV, alloc_workspace=False)
+    room = torch.full((r.workspace_bytes + 4096,), 0x5a, dtype=torch.uint8, device=G.DEV)
+    r.ws = room[:r.workspace_bytes]
+    dQ, dK, dgq, dgk = torch.empty_like(Q), torch.empty_like(K), *(torch.empty(d, device=G.DEV) for _ in range(2))
+    r.bwd(dQo, dKo, pos, f, dQ, dK, Q=Q, K=K, gamma_q=gammas[0], gamma_k=gammas[1], dgamma_q=dgq, dgamma_k=dgk)
+    assert bool((room[r.workspace_bytes:] == 0x5a).all())
+    for got, dy, x, gamma, dg in ((dQ, dQo, Q, gammas[0], dgq), (dK, dKo, K, gammas[1], dgk)):
+        want, bound, wg, bg = _backward(dy, x, gamma, pos, f, d, False, 1.0, 1e-6)
+        assert A.near(got, want, bound) and A.near(dg, wg, bg)
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^24 + 5 rows of 256 elements, in place; looked at: the ends and where one launch gives way to the next."""
+    rows, d = 2 ** 24 + 5, 256
+    x = torch.ones(rows, 2, d, dtype=torch.bfloat16, device=G.DEV)
+    look = torch.tensor([0, 1, 2 ** 24 - 5, 2 ** 24 - 1, 2 ** 24, 2 ** 24 + 3, rows - 1], device=G.DEV)
+    x[look] = torch.randn(len(look), 2, d, generator=torch.Generator(device=G.DEV).manual_seed(3), device=G.DEV).to(torch.bfloat16)
+    before = x[look].clone()
+    f, pos = binding.rotary_frequencies(d, device=G.DEV), torch.arange(rows, dtype=torch.int32, device=G.DEV)
+    r = binding.Rotary(heads=1, kv_heads=1, d=d, dtype="bf16", device=G.DEV)
+    r.fwd(x[:, :1], x[:, 1:], pos, f, x[:, :1], x[:, 1:])
+    want, bound = _forward(before, None, pos[look], f, d, False, 1.0, 1e-6)
+    assert A.near(x[look], want, bound)
+    before = x[look].clone()
+    r.bwd(x[:, :1], x[:, 1:], pos, f, x[:, :1], x[:, 1:])
+    want, bound, _, _ = _backward(before, None, None, pos[look], f, d, False, 1.0, 1e-6)
+    assert A.near(x[look], want, bound)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_far_positions(dtype):
     """Angles of positions up to 2^31: their products with the frequencies are far past what 32 bits tell apart."""
