@@ -370,7 +370,7 @@ int moe_rotary_bwd(const moe_rotary_t* cfg, const moe_heads_t* dQo, const moe_he
  * products with the zeros of a mask, may reach queries of its own sequence that causality hides it from by up to 63 keys.  Memory past a sequence's end is
  * not read into any result.
  * Limits: 0 <= q_rows, k_rows < 2^30, 0 <= seqs <= 65535, heads a multiple of kv_heads, heads <= 1024, d a multiple of 8 up to 128, scale > 0 and finite,
- * (q_rows / 32 + seqs) * heads < 2^30. */
+ * (q_rows / 256 + seqs) * heads < 2^22, (k_rows / 256 + seqs) * kv_heads < 2^22. */
 typedef struct {
     int q_rows, k_rows, seqs;
     int heads, kv_heads, d;
@@ -391,7 +391,8 @@ int moe_attn_fwd(const moe_attn_t* cfg, const moe_heads_t* Q, const moe_heads_t*
 
 /* Gradient of moe_attn_fwd.  With p_ij = exp(a_ij - lse_i), D_i = <dO_i, O_i>, ds_ij = p_ij (<dO_i, v_j> - D_i):
  *   dQ_i = scale sum_j ds_ij k_j;  dK_j = scale sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i, the last two over the heads that share the key; sums in fp32 in a fixed
- *   order, p and ds rounded to bf16 for MOE_BF16
+ *   order, p and ds rounded to bf16 for MOE_BF16.  A NaN or an infinity in a row reaches what the formulas say and, through products with the
+ *   zeros of a mask, may reach gradients of rows of its own sequence that causality hides from it, up to 287 positions away.
  *   in : dO[q_rows,heads,d], Q, K, V, O, lse as the forward call had and left them; offsets, k_begin, k_end: k_begin rises, and no key belongs to two sequences
  *   out: dQ[q_rows,heads,d], dK[k_rows,kv_heads,d], dV[k_rows,kv_heads,d]: rows of sequences only, those of keys that no query sees zero
  * No output may lie on an input.  Uses the workspace. */

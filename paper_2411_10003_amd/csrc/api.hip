@@ -474,7 +474,8 @@ static int check_attn(const moe_attn_t* c)
     if (c->q_rows < 0 || c->q_rows >= (1 << 30) || c->k_rows < 0 || c->k_rows >= (1 << 30) || c->seqs < 0 || c->seqs > 65535) return MOE_ERR_SHAPE;
     if (c->kv_heads < 1 || c->heads < 1 || c->heads > 1024 || c->heads % c->kv_heads || c->d < 8 || c->d > ATTN_MAX_D || c->d % 8) return MOE_ERR_SHAPE;
     if ((c->causal != 0 && c->causal != 1) || !(c->scale > 0.0f) || !std::isfinite(c->scale)) return MOE_ERR_SHAPE;
-    if (((long long)c->q_rows / 32 + c->seqs) * c->heads >= (1 << 30) || ((long long)c->k_rows / 32 + c->seqs) * c->kv_heads >= (1 << 30)) return MOE_ERR_SHAPE;
+    // blocks of 512 threads, or 3/2 as many of 256: a launch counts its threads in 32 bits
+    if (((long long)c->q_rows / 256 + c->seqs) * c->heads >= (1 << 22) || ((long long)c->k_rows / 256 + c->seqs) * c->kv_heads >= (1 << 22)) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
 

@@ -87,7 +87,7 @@ def test_attention(lib):
         assert call(_attn(), begin=P) == -1 and call(_attn(), end=P) == -1
         for bad in (dict(q=-1), dict(q=1 << 30), dict(k=-1), dict(k=1 << 30), dict(seqs=-1), dict(seqs=65536), dict(heads=0), dict(kv=0), dict(heads=3), dict(heads=1026), dict(d=0),
                     dict(d=12), dict(d=136), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(q=(1 << 30) - 1, heads=64),
-                    dict(k=(1 << 30) - 1, heads=64, kv=64)):
+                    dict(k=(1 << 30) - 1, heads=64, kv=64), dict(q=0, seqs=65535, heads=66), dict(q=0, k=(1 << 26), heads=16, kv=16)):
             assert call(_attn(**bad)) == -2, bad
         assert call(_attn(dtype=7)) == -5
         for which in tensors:
