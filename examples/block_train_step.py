@@ -1,7 +1,8 @@
 """A pre-norm MoE block trained on one GPU: the norm ahead of the gate, the layer, the norm after it, all gradients, the update of the experts
-by Muon and the transfer of the updated ones into the slots the layer reads.
+by Muon and the transfer of the updated ones into the slots the layer reads.  With --heads the half before it too: norm, projection, rotation of queries and
+keys with a norm of their heads, attention over packed sequences of random lengths, projection.
 
-    python examples/block_train_step.py [--steps 20] [--tokens 2048] [--width 256] [--hidden 512] [--experts 8]
+    python examples/block_train_step.py [--steps 20] [--tokens 2048] [--width 256] [--hidden 512] [--experts 8] [--heads 4 --kv-heads 2]
 
 The block learns to give a fixed map of its input (synthetic).  All experts are this GPU's own (one destination), so nothing has to arrive from
 elsewhere.  fp32 master weights live in pools of all experts beside the bf16 copies that moe_trans takes them from.
@@ -78,6 +79,84 @@ class Block:
             p.sub_(lr_vectors * g)
 
 
+class AttentionHalf:
+    """S -> the attention's output over packed sequences; d / heads columns a head.  The projections are library products."""
+
+    def __init__(self, *, T, d, heads, kv_heads, seqs, seed=0):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        randn = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+        bf16 = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=DEV)  # noqa: E731
+        w, n = d // heads, heads + 2 * kv_heads
+        self.parts = (heads, kv_heads, kv_heads)
+        self.norm = binding.Norm(d=d, dtype="bf16", device=DEV)
+        self.rotary = binding.Rotary(heads=heads, kv_heads=kv_heads, d=w, dtype="bf16", norm=True, device=DEV)
+        self.attention = binding.Attention(heads=heads, kv_heads=kv_heads, d=w, dtype="bf16", rows=T, seqs=seqs, device=DEV)
+        self.frequencies = binding.rotary_frequencies(w, device=DEV)
+        self.gamma, self.beta = torch.ones(d, device=DEV), torch.zeros(d, device=DEV)
+        self.gamma_q, self.gamma_k = torch.ones(w, device=DEV), torch.ones(w, device=DEV)
+        self.Wqkv, self.Wo = (randn(d, n * w) / math.sqrt(d)).to(torch.bfloat16), (randn(heads * w, d) / math.sqrt(heads * w)).to(torch.bfloat16)
+        self.Y, self.mean, self.rstd = bf16(T, d), torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+        self.QKV, self.Q, self.K = bf16(T, n, w), bf16(T, heads, w), bf16(T, kv_heads, w)
+        self.O, self.lse = torch.zeros(T, heads, w, dtype=torch.bfloat16, device=DEV), torch.empty(heads * T, device=DEV)
+        self.dQKV, self.dS = torch.zeros_like(self.QKV), bf16(T, d)
+        self.dgamma, self.dbeta = torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+        self.dgamma_q, self.dgamma_k = torch.empty(w, device=DEV), torch.empty(w, device=DEV)
+
+    def forward(self, S, offsets, positions):
+        """offsets: where each sequence begins and the last one ends (all rows); positions: of each row in its sequence."""
+        T = S.shape[0]
+        self.S, self.offsets, self.positions = S, offsets, positions
+        self.norm.fwd(S, self.gamma, self.beta, self.Y, mean=self.mean, rstd=self.rstd)
+        torch.mm(self.Y, self.Wqkv, out=self.QKV.view(T, -1))
+        q, k, v = self.QKV.split(self.parts, 1)
+        self.rotary.fwd(q, k, positions, self.frequencies, self.Q, self.K, gamma_q=self.gamma_q, gamma_k=self.gamma_k)
+        self.attention.fwd(self.Q, self.K, v, self.O, offsets, lse=self.lse)
+        return self.O.view(T, -1) @ self.Wo
+
+    def backward(self, dX, dS):
+        """dX: gradient of what forward() returned; dS: of S by the other ways it goes.  Returns the gradient of S."""
+        T = dX.shape[0]
+        q, k, v = self.QKV.split(self.parts, 1)
+        dq, dk, dv = self.dQKV.split(self.parts, 1)
+        self.dWo = self.O.view(T, -1).T.contiguous() @ dX
+        dO = (dX @ self.Wo.T).view_as(self.O)
+        self.attention.bwd(dO, self.Q, self.K, v, self.O, self.lse, self.offsets, dq, dk, dv)
+        self.rotary.bwd(dq, dk, self.positions, self.frequencies, dq, dk, Q=q, K=k, gamma_q=self.gamma_q, gamma_k=self.gamma_k, dgamma_q=self.dgamma_q,
+                        dgamma_k=self.dgamma_k)
+        self.dWqkv = self.Y.T.contiguous() @ self.dQKV.view(T, -1)
+        self.norm.bwd(self.dQKV.view(T, -1) @ self.Wqkv.T, self.S, self.gamma, self.mean, self.rstd, self.dS, self.dgamma, self.dbeta, residual_grad=dS)
+        return self.dS
+
+    def update(self, lr):
+        for p, g in ((self.Wqkv, self.dWqkv), (self.Wo, self.dWo), (self.gamma, self.dgamma), (self.beta, self.dbeta), (self.gamma_q, self.dgamma_q),
+                     (self.gamma_k, self.dgamma_k)):
+            p.sub_((lr * g).to(p.dtype))
+
+
+def packed(T, seqs, g):
+    """T rows as `seqs` sequences of random lengths: offsets, and each row's position in its own."""
+    cuts = torch.randint(0, T + 1, (seqs - 1,), generator=g, device=DEV).sort().values
+    offsets = torch.cat((cuts.new_zeros(1), cuts, cuts.new_full((1,), T)))
+    rows = torch.arange(T, device=DEV)
+    return offsets.int(), (rows - offsets[torch.searchsorted(offsets, rows, right=True) - 1]).int()
+
+
+def train_both_halves(steps, T, d, h, E, heads, kv_heads, seqs=4, seed=0, lr=0.02, lr_vectors=0.05):
+    g = torch.Generator(device=DEV).manual_seed(seed + 1)
+    block, half = Block(T=T, d=d, h=h, E=E, seed=seed), AttentionHalf(T=T, d=d, heads=heads, kv_heads=kv_heads, seqs=seqs, seed=seed)
+    target_map = torch.randn(d, d, generator=g, device=DEV) / math.sqrt(d)
+    losses = []
+    for _ in range(steps):
+        R = torch.randn(T, d, generator=g, device=DEV).to(torch.bfloat16)
+        diff = block.forward(half.forward(R, *packed(T, seqs, g)), R).float() - torch.tanh(R.float() @ target_map)
+        losses.append(float(diff.square().mean()))
+        dX = block.backward((diff * (2.0 / T)).to(torch.bfloat16))
+        half.backward(dX, dX)
+        block.update(lr, lr_vectors)
+        half.update(lr_vectors)
+    return losses, block, half
+
+
 def train(steps, T, d, h, E, seed=0, lr=0.02, lr_vectors=0.05):
     g = torch.Generator(device=DEV).manual_seed(seed + 1)
     block = Block(T=T, d=d, h=h, E=E, seed=seed)
@@ -101,6 +180,10 @@ if __name__ == "__main__":
     ap.add_argument("--width", type=int, default=256)
     ap.add_argument("--hidden", type=int, default=512)
     ap.add_argument("--experts", type=int, default=8)
+    ap.add_argument("--heads", type=int, default=0)
+    ap.add_argument("--kv-heads", type=int, default=0)
     a = ap.parse_args()
-    for i, loss in enumerate(train(a.steps, a.tokens, a.width, a.hidden, a.experts)[0]):
+    sizes = (a.steps, a.tokens, a.width, a.hidden, a.experts)
+    losses = train_both_halves(*sizes, a.heads, a.kv_heads or a.heads)[0] if a.heads else train(*sizes)[0]
+    for i, loss in enumerate(losses):
         print(f"step {i}: loss {loss:.4f}", flush=True)
