@@ -300,9 +300,15 @@ __device__ __forceinline__ int few_keys(const attn_args& a, const Sequence& s)
     const int last = min(s.n - 1, (int)(((long long)s.tile * 32 + 31) / a.group));
     return a.causal ? min(s.m, max(0, last + 1 + s.m - s.n)) : s.m;
 }
-// Blocks of 32 rows, and whether a call of so many larger blocks is one for them: up to one for each CU, the longest of which all the others would wait for.
+// Blocks of 32 rows, and whether a call of so many larger blocks is one for them: where those leave CUs without one, all wait for the longest.  us, small | large blocks, causal:
+//   forward   bf16, 128 columns: 64 blocks (4096, 4 heads) 59 | 77, 80 (4 x 1024) 29 | 29, 128 (16 x 256) 18 | 17, 136 (4096) 99 | 78;  64 columns: 80 13 | 22, 160 23 | 23, 240 32 | 24
+//   gradient  bf16, 128 columns: 68 125 | 301, 136 (4096) 229 | 304, 128 (16 x 256) 42 | 50, 160 (4 x 1024) 112 | 98, 204 338 | 307;  64 columns: 160 54 | 67, 240 72 | 69
+//   fp32, 64 columns (4096): 68 123 | 495, 544 760 | 546, gradient 327 | 1500 and 2248 | 2026
 inline long long few_units(const attn_args& a) { return ((long long)a.q_rows * a.group / 32 + a.seqs) * a.kv_heads; }
-inline bool is_small(long long blocks) { return blocks <= 256; }
+template <typename ET, int DP> bool is_small(long long blocks, bool gradient)
+{
+    return blocks <= (sizeof(ET) == 4 ? 256 : gradient ? (DP == 64 ? 208 : 144) : DP == 64 ? 160 : 96);
+}
 // How the tiles of 32 along a block's other axis are cut into parts, blocks of their own: `chunk` tiles a part as the launch has it, more where that does not reach the
 // end.  Parts past the end have nothing to do; a part that is alone writes its rows itself, others are joined by a later launch.
 struct Parts {

@@ -3,6 +3,9 @@
 // One pass over the keys with a running maximum and sum.  A wave has 32 queries and all of their results: with S^T = K Q^T a lane holds 16 scores of ONE
 // query per 32 keys, so maximum and sum stay in the lane (its other half is 32 lanes on), and the exponentials are the second operand of O^T = V^T P^T
 // as they lie.  The maximum in use is let go stale: rescaling the results is rare after the first tiles and exact either way.
+//
+// Bound by the matrix cores, 4 d operations a pair of query and key, next to the vector units: a wave's 64 keys of 128 columns take 1220 to 1540 clocks of the ones and 930 to
+// 1110 of the others, so one has to run under the other.  Over a cache bound by keys and values, read once for the heads that share them.
 #include "attn.h"
 
 #include <type_traits>
@@ -109,6 +112,10 @@ constexpr int AHEAD = 6;                                   // fragments under wa
 
 // A block has 256 queries of one head, 32 a wave; keys and values go through a ring of five tiles in LDS.  In its matrix phase j a wave forms the scores of
 // tile j + 1 and adds tile j's values; in its vector phase the scores become exponentials, and the first fragments of the next matrix phase arrive.
+// The two waves of a SIMD are in opposite phases, held there by a barrier at each phase's end.  Why 256 rows: a ring of 160 KB serves eight waves, two a SIMD, and a
+// tile's way from the L2 all 256 rows.  One sequence of 16384, 32 and 8 heads of 128, bf16, causal: 1.71 to 1.80 ms by the
+// card, 2.2 TFLOP at 1.2 to 1.3 PFLOP/s, matrix pipes 74 % busy at the 1.4 GHz that the power cap leaves (a large library product reaches 1.15 to 1.36 PFLOP/s); with waves
+// that run freely 2.23 ms.  16384 rows in eleven sequences, 16 and 4 heads of 128: 204 to 218 us, 304 without phases.
 template <typename ET, int DP>
 __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
 {
@@ -393,10 +400,12 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
     static PerDeviceOnce once;
     hipError_t e = allow_lds(attend_few_kernel<ET, DP, FEW_WAVES>, bytes, once);
     if (e != hipSuccess) return e;
-    // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do
+    // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do.  Where there are
+    // blocks for all CUs without them they only cost: 1024 rows, 8 heads of 128, 264 blocks, causal: 42 us with, 15 without.  A token of each of 16 sequences over 1 to 16384
+    // keys, 32 and 8 heads of 128, 144 blocks, us: 2048 parts 120, 1024 111, 512 105, none 197
     const long long units = few_units(a);
     const long long tiles = ((long long)a.k_rows / a.seqs + FEW_KEYS - 1) / FEW_KEYS;
-    const long long want = ATTN_PARTS / units, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);
+    const long long want = units <= 256 ? ATTN_PARTS / units : 1, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);
     a.splits = (int)(want < most ? want : most);
     if (a.splits < 1) a.splits = 1;
     a.chunk = (int)((tiles / a.splits + FEW_WAVES) / FEW_WAVES * FEW_WAVES);
@@ -409,8 +418,9 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
 
 template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t st)
 {
-    // few rows: what a kv head has of an average sequence fits one block's 32 twice over
-    if ((long long)a.q_rows * a.group <= 64ll * a.seqs || is_small(((long long)a.q_rows / SIDE + a.seqs) * a.heads)) return launch_few<ET, DP>(a, st);
+    // or few rows a sequence, whatever their number: up to 16, or 32 of heads that share nothing, over 4096 keys, 32 and 8 heads of 128, us, small | large blocks:
+    // 8 rows 88 | 119, 16 86 | 120, 32 136 | 121; over 1024, 32 and 32 heads of 64: 32 rows 117 | 126, 64 158 | 132
+    if ((long long)a.q_rows <= (a.group == 1 ? 32ll : 16ll) * a.seqs || is_small<ET, DP>(((long long)a.q_rows / SIDE + a.seqs) * a.heads, false)) return launch_few<ET, DP>(a, st);
     return launch_rows<ET, DP>(a, st);
 }
 

@@ -131,7 +131,7 @@ hipError_t launch_muon_step(const moe_muon_t& c, const float* const* grads, floa
                             int32_t* version, void* ws, hipStream_t st);
 
 constexpr int ATTN_MAX_D = 128, ROTARY_MAX_D = 256;
-constexpr int ATTN_PARTS = 2048;       // parts of keys that a forward call of few rows may cut its sequences into, all together
+constexpr int ATTN_PARTS = 512;        // parts of keys that a forward call of few rows may cut its sequences into, all together
 constexpr int ATTN_BWD_PARTS = 1024;   // parts that each kernel of a small backward call may cut its blocks' work into, all together,
 constexpr int ATTN_PART_TILES = 16;    // of so many tiles of 32 at least
 inline size_t attn_stats_bytes(int heads, int q_rows) { return ((size_t)heads * q_rows * 2 * sizeof(float) + 255) / 256 * 256; }
