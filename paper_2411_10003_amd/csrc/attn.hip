@@ -366,14 +366,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(attn_args a)
         if (!f.there) return;                              // nor are the rows after it
         const float* from = a.partial + (size_t)unit * a.splits * partial_floats<DP>();
         float most = LOWEST, total = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p = 0; p < parts.used; ++p) most = fmaxf(most, from[(size_t)p * partial_floats<DP>() + 32 * DP + q]);
-        for (int p = 0; p < parts.used; ++p) {
-            const float* one = from + (size_t)p * partial_floats<DP>();
-            const float down = exp2_fast(one[32 * DP + q] - most);
-            const f32x4 x = *(const f32x4*)&one[q * DP + c];
-            total = fmaf(one[32 * DP + 32 + q], down, total);
+        for (int p = 0; p < parts.used; p += 4) {          // four parts' loads are under way together
+            float high[4], sums[4];
+            f32x4 x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], down, v[e]);
+            for (int k = 0; k < 4; ++k) {
+                const float* one = from + (size_t)min(p + k, parts.used - 1) * partial_floats<DP>();
+                high[k] = one[32 * DP + q], sums[k] = one[32 * DP + 32 + q], x[k] = *(const f32x4*)&one[q * DP + c];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (p + k >= parts.used) break;
+                const float next = fmaxf(most, high[k]), old = exp2_fast(most - next), down = exp2_fast(high[k] - next);
+                most = next;
+                total = fmaf(sums[k], down, total * old);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(x[k][e], down, v[e] * old);
+            }
         }
         const float by = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
         if (c < a.d) few_store<ET, DP>(a, s, f, c, v[0] * by, v[1] * by, v[2] * by, v[3] * by);
@@ -402,7 +411,7 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
     if (e != hipSuccess) return e;
     // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do.  Where there are
     // blocks for all CUs without them they only cost: 1024 rows, 8 heads of 128, 264 blocks, causal: 42 us with, 15 without.  A token of each of 16 sequences over 1 to 16384
-    // keys, 32 and 8 heads of 128, 144 blocks, us: 2048 parts 120, 1024 111, 512 105, none 197
+    // keys, 32 and 8 heads of 128, 144 blocks, us: 2048 parts 120, 1024 111, 512 104 (517 MB, 5.0 TB/s), none 197
     const long long units = few_units(a);
     const long long tiles = ((long long)a.k_rows / a.seqs + FEW_KEYS - 1) / FEW_KEYS;
     const long long want = units <= 256 ? ATTN_PARTS / units : 1, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);

@@ -125,6 +125,23 @@ def test_tokens_over_a_cache(lens, keys, cache, heads, kv, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,d", [(2, 1, 64), (3, 3, 128)])
+@pytest.mark.parametrize("seqs", [1, 3, 5, 63, 64, 65, 80])
+def test_cut_by_the_sum_of_the_lengths(seqs, heads, kv, d, dtype):
+    """Ragged caches whose sequences are cut into none to many parts each, empty places between them, up to three tokens a sequence; the workspace is as long as it has to be."""
+    g = torch.Generator().manual_seed(seqs)
+    keys = torch.randint(0, 700, (seqs,), generator=g).tolist()
+    lens = torch.randint(0, 4, (seqs,), generator=g).tolist()
+    keys[seqs // 2], lens[seqs // 2], keys[-1], lens[-1] = 9000, 2, 2500, 1
+    cache = 9000
+    Q, = A.tensors(sum(lens), (heads,), d, A.TYPES[dtype], "apart", seqs)
+    K, V = A.tensors(cache * seqs if seqs < 10 else 1000 * seqs + 9000, (kv, kv), d, A.TYPES[dtype], "fused", seqs + 1)
+    begin = [s * cache for s in range(seqs)] if seqs < 10 else [1000 * s + (8000 if s > seqs // 2 else 0) for s in range(seqs)]
+    begin[-1] = min(begin[-1], K.shape[0] - 2500)
+    _check(Q, K, V, lens, dtype, keys=keys, begin=begin)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["fused", "apart", "heads"])
 def test_layouts_and_rows_of_no_sequence(layout, dtype):
     """Rows in front of the first sequence and behind the last one are left as they were; outputs in the middle of something wider."""
@@ -200,6 +217,21 @@ def test_offsets_that_are_wrong(heads):
         wO, bO, _, _ = A.forward(Q, K, V, right, d ** -0.5, True)
         assert A.near(O, wO, bO)
         assert (guard[:20] == 7.0).all() and (guard[20 + rows:] == 7.0).all()
+
+
+@pytest.mark.parametrize("offsets,begin,end", [([0, 8, 0, 8, 0, 8], [0] * 5, [6000] * 5), ([0, 1, 2, 3, 4, 8], [0, 5000, 4000, -7, 2 ** 30], [6000, 100, 9000, 6000, 2 ** 31 - 1]),
+                                               ([8, 6, 4, 2, 0, 0], [0] * 5, [6000] * 5)])
+def test_wrong_offsets_of_cut_sequences(offsets, begin, end):
+    """Sequences that overlap or fall: what they leave in O is theirs to say, nothing behind the workspace or outside the tensors changes, and no row of no sequence."""
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=G.DEV)  # noqa: E731
+    Q, = A.tensors(8, (4,), 128, torch.bfloat16, "apart", 1)
+    K, V = A.tensors(6000, (2, 2), 128, torch.bfloat16, "apart", 2)
+    at = binding.Attention(heads=4, kv_heads=2, d=128, dtype="bf16", rows=8, k_rows=6000, seqs=5, device=G.DEV, alloc_workspace=False)
+    room = torch.full((at.workspace_bytes + 65536,), 0x5a, dtype=torch.uint8, device=G.DEV)
+    at.ws = room[:at.workspace_bytes]
+    O = torch.full((24, 4, 128), 7.0, dtype=torch.bfloat16, device=G.DEV)
+    at.fwd(Q, K, V, O[8:16], i32(offsets), k_begin=i32(begin), k_end=i32(end))
+    assert bool((room[at.workspace_bytes:] == 0x5a).all()) and bool((O[:8] == 7.0).all()) and bool((O[16:] == 7.0).all())
 
 
 @pytest.mark.parametrize("lens,heads", [([700, 33, 0, 600], 8), ([700, 33, 0, 600], 32), ([1] * 8, 8)])
