@@ -223,3 +223,35 @@ def test_nothing_to_do():
     at.ws = None
     with pytest.raises(ValueError):
         at.bwd(none, none, K, K, none, stats, i32(0, 0), none, dK, dV, k_begin=i32(3), k_end=i32(9))
+
+
+@pytest.mark.parametrize("dtype,heads,d", [("bf16", 36, 128), ("bf16", 48, 64), ("bf16", 2, 128), ("f32", 60, 64), ("f32", 2, 128)])
+def test_rows_past_32_bits(dtype, heads, d):
+    """Rows as far apart as they may lie, 4 MB of bf16 or 8 MB of fp32: the last of them more than 2^32 bytes in; blocks of every kernel."""
+    n, row = 1200, 2 ** 21 - 8
+    whole = torch.empty(n * row, dtype=A.TYPES[dtype], device=G.DEV)
+    Q, K, V = (whole.as_strided((n, heads, d), (row, d, 1), i * heads * d) for i in range(3))
+    for x, y in zip((Q, K, V), A.tensors(n, (heads,) * 3, d, A.TYPES[dtype], "apart", 3)):
+        x.copy_(y)
+    _check(Q, K, V, [700, 500], dtype)
+
+
+@pytest.mark.parametrize("lens,heads", [([300, 0, 77], 4), ([900, 1500], 24)])
+def test_two_streams(lens, heads):
+    """Two objects beside each other, each on a stream of its own, several times: the bits of the calls alone."""
+    calls = []
+    for seed in (1, 2):
+        Q, K, V = A.tensors(sum(lens), (heads, heads, heads), 128, torch.bfloat16, "fused", seed)
+        dO, O, lse = _given(Q, K, V, _parts(lens), True, seed)
+        at = binding.Attention(heads=heads, kv_heads=heads, d=128, dtype="bf16", rows=sum(lens), seqs=len(lens), device=G.DEV)
+        args = (at, dO, Q, K, V, O, lse, A.offsets(lens), None)
+        calls.append((args, _grads(*args), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for args, _, stream in calls:
+            with torch.cuda.stream(stream):
+                got.append(_grads(*args))
+        torch.cuda.synchronize()
+        for (_, want, _), new in zip(calls, got):
+            assert all(torch.equal(a, b) for a, b in zip(want, new))
