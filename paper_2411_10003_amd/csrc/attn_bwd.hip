@@ -359,8 +359,8 @@ __global__ __launch_bounds__(256, 1) void attend_dkv_f32_kernel(attn_args a)
 // bf16: a block has 256 keys, 32 a wave, and goes over 32 queries at a time.  In its matrix phase u a wave adds the products of tile u - 1 to both gradients and forms
 // the scores and <dO, v> of tile u; in its vector phase these become p and ds.  Registers: 32 rows of two gradients, of keys and of scores; the values, which
 // would be 32 more, lie in LDS (128 columns).  Tiles that causality hides from a wave's keys are worked on with zeros: no wave leaves the common step.
-// Four sequences of 8192, 32 and 8 heads of 128, causal: 4.05 ms, 1.09 PFLOP/s of its four products, matrix pipes 55 % busy at 1.8 GHz.  LDS gives 41 % of its reads: a
-// tile's queries and their gradients are each wanted by rows and by keys, and the values too.
+// Four sequences of 8192, 32 and 8 heads of 128, causal: 3.94 ms, 1.12 PFLOP/s of its four products, matrix pipes 58 % busy at 1.7 GHz, LDS 43 %: a tile's queries and their
+// gradients are each wanted by rows and by keys, and the values too.
 struct DkvReads {
     static constexpr int of(int i, int by_keys, bool v_in_lds) { return i < by_keys ? 2 : v_in_lds && ((i - by_keys) & 1) ? 2 : 1; }
 };
@@ -439,6 +439,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
         clear(dV[b]);
     }
     if (walk.steps > 0) {
+        // Requests are made in the shorter phase: 128 columns' is that of the vector units (the whole gradient of the case above 6.76 -> 6.69 ms), 64 columns' that of the matrix cores (855 us, 947 the other way).
+        constexpr bool LATE = DP == 128;
         constexpr int BY_KEYS = 4 * tile::DB, N = BY_KEYS + 2 * tile::T, PRE = AHEAD < BY_KEYS ? AHEAD : BY_KEYS;
         f32x16 x, y;
         frag p[2], ds[2], pre[PRE];
@@ -493,11 +495,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
         wait(std::integral_constant<int, 2>{});            // the values and tile 0
         PHASE_END();
         if (second) PHASE_END();                           // the second half is a phase behind
-        ask();
+        if constexpr (!LATE) ask();
         scores(0);
-        wait(std::integral_constant<int, 2>{});            // tile 1
+        wait(std::integral_constant<int, LATE ? 1 : 2>{});             // tile 1
         PHASE_END();
         request_first();
+        if constexpr (LATE) ask();
         soften();
         for (int u = 1; u < walk.steps; ++u) {             // closes as the one above
             PHASE_END();
@@ -510,10 +513,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_dkv_kernel(attn_args a)
             pace<DkvOrder<BY_KEYS, D::V_IN_LDS>, N, PRE>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
-            ask();                                         // in the place of tile u - 2, which the second half was done with a phase ago
-            wait(std::integral_constant<int, 2>{});        // tile u + 1 has arrived
+            if constexpr (!LATE) ask();                    // in the place of tile u - 2, which the second half was done with a phase ago
+            wait(std::integral_constant<int, LATE ? 1 : 2>{});         // tile u + 1 has arrived
             PHASE_END();
             request_first();
+            if constexpr (LATE) ask();
             soften();
         }
         PHASE_END();
