@@ -209,6 +209,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attend_kernel(attn_args a)
             step(next);
             vector_phase(j + 1);
         }
+        WAIT_VMCNT(2 * request::P);                        // as in the loop, for waves that never went through it: others read tile 2 from the next phase on
         PHASE_END();
         for (; j < tiles; ++j) {                           // this wave's last one, and those that only others see
             ask();

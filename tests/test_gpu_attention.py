@@ -69,6 +69,18 @@ MANY = [300, 1, 0, 257, 64, 513, 31, 700, 256]
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,keys", [([44, 100], [300, 700]), ([1, 128], [500, 1000]), ([300, 96], [300, 161])])
+def test_blocks_whose_later_waves_have_no_rows(lens, keys, d, causal, dtype):
+    """At most half of a large block's rows are there, over enough keys for every place of the ring."""
+    heads = 264 // len(lens)
+    Q, = A.tensors(sum(lens), (heads,), d, A.TYPES[dtype], "apart", 21)
+    K, V = A.tensors(sum(keys), (heads, heads), d, A.TYPES[dtype], "fused", 22)
+    _check(Q, K, V, lens, dtype, causal=causal, keys=keys)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("heads,kv,d,layout", [(18, 18, 128, "fused"), (36, 18, 64, "heads"), (20, 20, 72, "apart"), (40, 20, 32, "fused"), (24, 24, 8, "heads")])
 def test_many_blocks(heads, kv, d, layout, causal, dtype):
     Q, K, V = A.tensors(sum(MANY), (heads, kv, kv), d, A.TYPES[dtype], layout, heads + d)
