@@ -2,7 +2,8 @@
 //
 // One pass over the keys with a running maximum and sum.  A wave has 32 queries and all of their results: with S^T = K Q^T a lane holds 16 scores of ONE
 // query per 32 keys, so maximum and sum stay in the lane (its other half is 32 lanes on), and the exponentials are the second operand of O^T = V^T P^T
-// as they lie.  The maximum in use is let go stale: rescaling the results is rare after the first tiles and exact either way.
+// as they lie.  The maximum in use is let go stale: rescaling the results, a rounding of each, is rare after the first tiles, and
+// each row decides on it for itself: its bits do not depend on the rows beside it.
 //
 // Bound by the matrix cores, 4 d operations a pair of query and key, next to the vector units: a wave's 64 keys of 128 columns take 1220 to 1540 clocks of the ones and 930 to
 // 1110 of the others, so one has to run under the other.  Over a cache bound by keys and values, read once for the heads that share them.
@@ -55,7 +56,7 @@ template <typename ET, int DP> struct Rows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = first + 32 * b + 8 * (i >> 2) + 4 * hi + (i & 3) > limit ? -INFINITY : s[b][i];
     }
-    // Exponentials of the scores over the maximum in use, as they go into the products, and their sum.  Only where a lane's sum of them passes STALE (one of them
+    // Exponentials of the scores over the maximum in use, as they go into the products, and their sum.  Only where a row's sum of them passes STALE in a lane (one of them
     // does, or none of the row's keys came before) is the highest score looked for, the results so far scaled down to it and the exponentials formed again: a
     // maximum of every tile takes a tenth of the vector instructions.  Scores past fp32's range as exponents end there too.
     static constexpr float STALE = 1024.0f;
@@ -68,7 +69,10 @@ template <typename ET, int DP> struct Rows {
 #pragma unroll
             for (int i = 1; i < 16 * NB; i += 2) top = highest_of(top, s[i / 16][i % 16], s[(i + 1 < 16 * NB ? i + 1 : i) / 16][(i + 1 < 16 * NB ? i + 1 : i) % 16]);
             const Halves h = halves_of(top);
-            const float next = highest_of(most, h.low * scale2, h.high * scale2), down = exp2_fast(most - next);
+            // the wave takes the branch, each row decides for itself: the others keep their maximum, and so their exponentials, and are multiplied by one
+            const Halves of_row = halves_of(now);
+            const bool stale = of_row.low > STALE || of_row.high > STALE;
+            const float next = stale ? highest_of(most, h.low * scale2, h.high * scale2) : most, down = stale ? exp2_fast(most - next) : 1.0f;
             most = next;
             sum *= down;
 #pragma unroll

@@ -199,6 +199,27 @@ def test_values_out_of_the_ordinary(n, heads, dtype):
     assert torch.isnan(O2[2 * n]).all() and torch.equal(O2[2 * n + 1:], O[2 * n + 1:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,heads,d", [(1, 32, 64), (3, 6, 128), (400, 2, 64), (400, 2, 128), (400, 134, 64), (400, 134, 128)])
+def test_bits_of_a_row_are_its_own(n, heads, d, causal, dtype):
+    """What lies in one query, scores that outgrow the maximum in use or infinities, changes no bit of the others, its neighbours in a wave among them."""
+    t, m = A.TYPES[dtype], 700
+    Q, = A.tensors(n, (heads,), d, t, "apart", 31)
+    K, V = A.tensors(m, (1, 1), d, t, "apart", 32)
+    K *= torch.linspace(0.2, 3.0, m, device=G.DEV)[:, None, None].to(t)    # later keys have the higher scores
+    at = binding.Attention(heads=heads, kv_heads=1, d=d, dtype=dtype, rows=n, k_rows=m, seqs=1, causal=causal, device=G.DEV)
+    off, where = A.offsets([n]), _where([m])
+    O, lse = _run(at, Q, K, V, off, where)
+    for factor in (30.0, -30.0, 0.0, math.inf, -math.inf):
+        for row, head in ((0, 0), (n // 2, heads - 1), (n - 1, heads // 2)):
+            Q2 = Q.clone()
+            Q2[row, head] = Q2[row, head] * factor
+            O2, lse2 = _run(at, Q2, K, V, off, where)
+            O2[row, head], lse2[head, row] = O[row, head], lse[head, row]
+            assert torch.equal(O, O2) and torch.equal(lse, lse2), (factor, row, head)
+
+
 def _where(keys):
     ends = A.offsets(keys)
     return ends[:-1].contiguous(), ends[1:].contiguous()
