@@ -367,7 +367,7 @@ int moe_rotary_bwd(const moe_rotary_t* cfg, const moe_heads_t* dQo, const moe_he
  * A query that sees nothing has O = 0 and lse = -inf.  Rows that no sequence has are left as they were.  Offsets are held inside 0 .. q_rows and 0 .. k_rows on the
  * device, whatever they are (offsets that fall, or lie on each other: some of the rows are not right).
  * A NaN or an infinity in a row of Q stays in that row, one in K in the rows that see the key; one in V reaches the rows that see it and, through
- * products with the zeros of a mask, may reach queries of its own sequence that causality hides it from by up to 63 keys.  Memory past a sequence's end is
+ * products with the zeros of a mask, may reach queries of its own sequence that causality hides it from by up to 94 keys.  Memory past a sequence's end is
  * not read into any result.
  * Limits: 0 <= q_rows, k_rows < 2^30, 0 <= seqs <= 65535, heads a multiple of kv_heads, heads <= 1024, d a multiple of 8 up to 128, scale > 0 and finite,
  * (q_rows / 256 + seqs) * heads < 2^22, (k_rows / 256 + seqs) * kv_heads < 2^22. */
@@ -392,7 +392,7 @@ int moe_attn_fwd(const moe_attn_t* cfg, const moe_heads_t* Q, const moe_heads_t*
 /* Gradient of moe_attn_fwd.  With p_ij = exp(a_ij - lse_i), D_i = <dO_i, O_i>, ds_ij = p_ij (<dO_i, v_j> - D_i):
  *   dQ_i = scale sum_j ds_ij k_j;  dK_j = scale sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i, the last two over the heads that share the key; sums in fp32 in a fixed
  *   order, p and ds rounded to bf16 for MOE_BF16.  A NaN or an infinity in a row reaches what the formulas say and, through products with the
- *   zeros of a mask, may reach gradients of rows of its own sequence that causality hides from it, up to 287 positions away.
+ *   zeros of a mask, may reach gradients of rows of its own sequence that causality hides from it by up to 286 positions.
  *   in : dO[q_rows,heads,d], Q, K, V, O, lse as the forward call had and left them; offsets, k_begin, k_end: k_begin rises, and no key belongs to two sequences
  *   out: dQ[q_rows,heads,d], dK[k_rows,kv_heads,d], dV[k_rows,kv_heads,d]: rows of sequences only, those of keys that no query sees zero
  * No output may lie on an input.  Uses the workspace. */

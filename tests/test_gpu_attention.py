@@ -1,6 +1,8 @@
 """Attention of packed sequences, forward, against the formulas in 64 bits (attn_util: values and bounds): widths, groups of heads, lengths from none to more
 than a block's rows, keys more and fewer than queries, layouts, keys in a cache, rows that see nothing, values that no row may see."""
 import math
+import os
+import re
 
 import pytest
 import torch
@@ -218,6 +220,36 @@ def test_bits_of_a_row_are_its_own(n, heads, d, causal, dtype):
             O2, lse2 = _run(at, Q2, K, V, off, where)
             O2[row, head], lse2[head, row] = O[row, head], lse[head, row]
             assert torch.equal(O, O2) and torch.equal(lse, lse2), (factor, row, head)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,d", [(2, 64), (2, 128), (134, 64), (134, 128)])
+def test_reach_of_a_value_that_is_no_number(heads, d, dtype):
+    """A NaN in V: in all rows that see it, in no row that is further from it than the header says, where the bits are those without it."""
+    reach, n, m, t = _said(r"hides it from by up to (\d+) keys"), 400, 401, A.TYPES[dtype]
+    Q, = A.tensors(n, (heads,), d, t, "apart", 41)
+    K, V = A.tensors(m, (1, 1), d, t, "apart", 42)
+    at = binding.Attention(heads=heads, kv_heads=1, d=d, dtype=dtype, rows=n, k_rows=m, seqs=1, device=G.DEV)
+    O, lse = _run(at, Q, K, V, A.offsets([n]), _where([m]))
+    furthest = 0
+    for key in (0, 63, 64, 95, 127, 191, 255, 256, 300, 383, 400):
+        for bad in (math.nan, math.inf):
+            V2 = V.clone()
+            V2[key] = bad
+            O2, lse2 = _run(at, Q, K, V2, A.offsets([n]), _where([m]))
+            hidden_by = key - (torch.arange(n, device=G.DEV) + m - n)          # keys between the last one that a row sees and this one
+            assert not torch.isfinite(O2[hidden_by <= 0]).any() and torch.equal(lse, lse2)
+            changed = ~(O2 == O).flatten(1).all(1)
+            furthest = max(furthest, int(hidden_by[changed].max()))
+    assert furthest <= reach
+    if heads > 100 and dtype == "bf16":
+        assert furthest == reach                           # tiles of 64 keys: the header says no more than there is
+
+
+def _said(pattern):
+    """A number that the header says."""
+    header = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "moehot.h")
+    return int(re.search(pattern, " ".join(line.strip(" *") for line in open(header).read().splitlines())).group(1))
 
 
 def _where(keys):

@@ -8,7 +8,7 @@ import torch
 import attn_util as A
 import gpu_util as G
 from paper_2411_10003_amd import binding
-from test_gpu_attention import MANY, _parts, _where
+from test_gpu_attention import MANY, _parts, _said, _where
 
 pytestmark = pytest.mark.gpu
 
@@ -180,6 +180,39 @@ def test_values_out_of_the_ordinary(heads, kv):
     got = _grads(at, dO, Q, K, V, O, lse, off, None)
     for a, b in zip(got, want):
         assert torch.equal(a[:200], b[:200]) and torch.equal(a[350:], b[350:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,d", [(2, 64), (2, 128), (112, 64), (112, 128)])
+def test_reach_of_a_value_that_is_no_number(heads, d, dtype):
+    """A NaN in a row of one input: where the formulas have it, and in rows that causality hides from it no further away than the header says; the others keep their bits."""
+    reach, n, m, t = _said(r"hides from it by up to (\d+) positions"), 600, 601, A.TYPES[dtype]
+    Q, = A.tensors(n, (heads,), d, t, "apart", 51)
+    K, V = A.tensors(m, (heads, heads), d, t, "apart", 52)
+    parts, where = _parts([n], [m]), _where([m])
+    dO, O, lse = _given(Q, K, V, parts, True, 53)
+    at = binding.Attention(heads=heads, kv_heads=heads, d=d, dtype=dtype, rows=n, k_rows=m, seqs=1, device=G.DEV)
+    clean = _grads(at, dO, Q, K, V, O, lse, A.offsets([n]), where)
+    queries, keys = torch.arange(n, device=G.DEV) + m - n, torch.arange(m, device=G.DEV)           # a query stands where the last key that it sees does
+    furthest = 0
+    for which in range(5):
+        for row in (0, 31, 32, 127, 224, 255, 256, 480, 511, 599):
+            given = [dO, Q, K, V, O]
+            given[which] = given[which].clone()
+            given[which][row] = math.nan
+            got = _grads(at, *given, lse, A.offsets([n]), where)
+            changed = [~(a == b).flatten(1).all(1) for a, b in zip(got, clean)]
+            if which in (2, 3):                            # a key: queries before it do not see it; other keys do not know of it
+                away = row - queries[changed[0]]
+                assert all(c.sum() <= 1 for c in changed[1:])
+            else:                                          # a query: keys behind it are hidden from it; other queries do not know of it
+                away = torch.cat([keys[c] - queries[row] for c in changed[1:]])
+                assert changed[0].sum() <= 1
+            if away.numel():
+                furthest = max(furthest, int(away.max()))
+    assert furthest <= reach
+    if heads > 100 and dtype == "bf16":
+        assert furthest == reach                           # blocks of 256 keys, tiles of 32 queries
 
 
 @pytest.mark.parametrize("heads,kv", [(4, 2), (96, 48)])
