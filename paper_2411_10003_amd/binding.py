@@ -407,6 +407,7 @@ def _argument(given, *said) -> Optional[int]:
 
 
 def _device_index(device) -> int:
+    """The number of a device; without one it is the first, whichever is the current one."""
     device = torch.device(device)
     if device.type != "cuda":
         raise ValueError(f"device {device}: a GPU is needed")
@@ -422,6 +423,24 @@ def _on_device(index: int) -> int:
     if current != index:
         raise ValueError(f"the current device is {current}, this object's is {index}")
     return _stream()
+
+
+class _WithWorkspace:
+    """An object whose calls belong on one device, with a workspace there."""
+
+    def _place(self, device, workspace_bytes: int, alloc_workspace: bool):
+        self._index, self.workspace_bytes = _device_index(device), workspace_bytes
+        self.ws = torch.empty(workspace_bytes, dtype=torch.uint8, device=torch.device("cuda", self._index)) if alloc_workspace else None
+
+    @property
+    def ws(self) -> Optional[torch.Tensor]:
+        return self._ws
+
+    @ws.setter
+    def ws(self, tensor: Optional[torch.Tensor]):
+        if tensor is not None:
+            _ptr(tensor, tensor.dtype, -(-self.workspace_bytes // tensor.element_size()), "workspace", self._index)
+        self._ws = tensor
 
 
 class _PerShape:
@@ -461,7 +480,7 @@ def rotary_frequencies(rot: int, base: float = 10000.0, *, factor: float = 1.0, 
     return f.to(device)
 
 
-class Rotary:
+class Rotary(_WithWorkspace):
     """Norm (with norm=True) and rotation of the heads of queries and keys (moe_rotary_fwd, moe_rotary_bwd), with the workspace of the backward pass.  Tensors are
     [rows, heads, d] of any strides whose heads are contiguous and lie at multiples of 16 bytes, say views of a projection's output.
 
@@ -477,9 +496,7 @@ class Rotary:
         self._rest = (self.heads, self.kv_heads, self.d, self.rot, int(bool(interleaved)), int(self.norm), DTYPES[dtype], eps, amplitude)
         n = ctypes.c_size_t()
         _checked(self.lib.moe_rotary_workspace_bytes(ctypes.byref(_Rotary(0, *self._rest, 0)), ctypes.byref(n)), "moe_rotary_workspace_bytes")
-        self.workspace_bytes = n.value
-        self._index = _device_index(device)
-        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+        self._place(device, n.value, alloc_workspace)
         self._calls = _PerShape()
 
     def _parts(self, rows: int):
@@ -508,16 +525,16 @@ class Rotary:
             _checked(rc, "moe_rotary_fwd")
 
     def bwd(self, dQo, dKo, positions, frequencies, dQ, dK, *, Q=None, K=None, gamma_q=None, gamma_k=None, dgamma_q=None, dgamma_k=None):
-        if self.ws is None:
+        if self._ws is None:
             raise ValueError("no workspace attached")
         rows = dQo.shape[0]
         call = self._calls.get((rows, 0, 1), "moe_rotary_bwd", lambda: self._bwd(_int32(rows, "rows")))
-        rc = call(dQo, dKo, Q, K, gamma_q, gamma_k, positions, frequencies, dQ, dK, dgamma_q, dgamma_k, self.ws.data_ptr(), _on_device(self._index))
+        rc = call(dQo, dKo, Q, K, gamma_q, gamma_k, positions, frequencies, dQ, dK, dgamma_q, dgamma_k, self._ws.data_ptr(), _on_device(self._index))
         if rc != 0:
             _checked(rc, "moe_rotary_bwd")
 
 
-class Attention:
+class Attention(_WithWorkspace):
     """Attention of packed sequences (moe_attn_fwd, moe_attn_bwd), with a workspace for calls of up to `rows` query rows, `k_rows` rows of keys and `seqs` sequences.
     Tensors are [rows, heads, d] of any strides whose heads are contiguous and lie at multiples of 16 bytes.
 
@@ -535,9 +552,7 @@ class Attention:
         self._rest = (self.heads, self.kv_heads, self.d, DTYPES[dtype], int(bool(causal)), scale)
         n = ctypes.c_size_t()
         _checked(self.lib.moe_attn_workspace_bytes(ctypes.byref(_Attn(self.rows, self.k_rows, self.seqs, *self._rest)), ctypes.byref(n)), "moe_attn_workspace_bytes")
-        self.workspace_bytes = n.value
-        self._index = _device_index(device)
-        self.ws = torch.empty(n.value, dtype=torch.uint8, device=device) if alloc_workspace else None
+        self._place(device, n.value, alloc_workspace)
         self._calls = _PerShape()
 
     def _spec(self, rows: int, k_rows: int, seqs: int, back: bool):
@@ -555,7 +570,7 @@ class Attention:
         return (cfg, q("Q"), k("K"), k("V"), q("O"), lse, *where, "int", "int")
 
     def _call(self, entry: str, Q, K, offsets, k_begin, k_end):
-        if self.ws is None:
+        if self._ws is None:
             raise ValueError("no workspace attached")
         if (k_begin is None) != (k_end is None):
             raise ValueError("k_begin and k_end: both or neither")
@@ -568,13 +583,13 @@ class Attention:
     def fwd(self, Q, K, V, O, offsets, *, k_begin=None, k_end=None, lse=None):
         """offsets[seqs + 1]: where each sequence's queries begin and the last one's end; its keys lie there too, or at k_begin .. k_end."""
         call = self._call("moe_attn_fwd", Q, K, offsets, k_begin, k_end)
-        rc = call(Q, K, V, O, lse, offsets, k_begin, k_end, self.ws.data_ptr(), _on_device(self._index))
+        rc = call(Q, K, V, O, lse, offsets, k_begin, k_end, self._ws.data_ptr(), _on_device(self._index))
         if rc != 0:
             _checked(rc, "moe_attn_fwd")
 
     def bwd(self, dO, Q, K, V, O, lse, offsets, dQ, dK, dV, *, k_begin=None, k_end=None):
         call = self._call("moe_attn_bwd", Q, K, offsets, k_begin, k_end)
-        rc = call(dO, Q, K, V, O, lse, offsets, k_begin, k_end, dQ, dK, dV, self.ws.data_ptr(), _on_device(self._index))
+        rc = call(dO, Q, K, V, O, lse, offsets, k_begin, k_end, dQ, dK, dV, self._ws.data_ptr(), _on_device(self._index))
         if rc != 0:
             _checked(rc, "moe_attn_bwd")
 

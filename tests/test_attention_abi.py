@@ -179,6 +179,51 @@ def test_the_current_device(monkeypatch):
     assert binding._device_index("cuda") == 0 and binding._device_index("cuda:3") == 3
 
 
+@pytest.mark.parametrize("device,index", [("cuda", 0), ("cuda:0", 0), ("cuda:1", 1), (torch.device("cuda"), 0)])
+def test_the_workspace_is_on_the_objects_device(monkeypatch, device, index):
+    """Also where another device is the current one, which is what torch takes a device without a number for."""
+    made, empty = [], torch.empty
+
+    def on_the_cpu(*size, device=None, **rest):
+        made.append(torch.device(device))
+        return Elsewhere.of(empty(*size, **rest), torch.device(device).index)
+
+    class Elsewhere(torch.Tensor):
+        is_cuda = True
+
+        @classmethod
+        def of(cls, t, index):
+            t = t.as_subclass(cls)
+            t.index = 1 if index is None else index        # 1 is the current device
+            return t
+
+        def get_device(self):
+            return self.index
+
+        def is_contiguous(self):
+            return True
+
+    monkeypatch.setattr(torch, "empty", on_the_cpu)
+    a = binding.Attention(heads=4, kv_heads=2, d=64, dtype="bf16", rows=8, seqs=2, device=device)
+    r = binding.Rotary(heads=4, kv_heads=2, d=64, dtype="bf16", norm=True, device=device)
+    assert made == [torch.device("cuda", index)] * 2
+    for o in (a, r):
+        assert o._index == index and o.ws.get_device() == index and o.ws.numel() >= o.workspace_bytes
+        with pytest.raises(ValueError, match=f"workspace: on device {1 - index}"):
+            o.ws = Elsewhere.of(empty(o.workspace_bytes, dtype=torch.uint8), 1 - index)
+        with pytest.raises(ValueError, match="workspace: .* elements, need"):
+            o.ws = Elsewhere.of(empty(o.workspace_bytes - 1, dtype=torch.uint8), index)
+        with pytest.raises(ValueError, match="workspace: .* elements, need"):
+            o.ws = Elsewhere.of(empty(o.workspace_bytes // 4 - 1, dtype=torch.float32), index)
+        with pytest.raises(ValueError, match="workspace: need a contiguous device tensor"):
+            o.ws = empty(o.workspace_bytes, dtype=torch.uint8)
+        for mine in (empty(o.workspace_bytes + 256, dtype=torch.uint8), empty(o.workspace_bytes // 4, dtype=torch.float32)):
+            mine = o.ws = Elsewhere.of(mine, index)
+            assert o.ws is mine
+        o.ws = None
+        assert o.ws is None
+
+
 def test_sizes_that_are_refused():
     for bad in (dict(heads=2 ** 32 + 4), dict(d=2 ** 32 + 64), dict(rot=2 ** 32)):
         with pytest.raises(ValueError):
