@@ -46,7 +46,7 @@ template <typename ET> struct Frag;
 template <> struct Frag<bf16_t> {
     typedef bf16x8 type;
     static __device__ __forceinline__ f32x16 mma(const type& a, const type& b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-    // Eight results of a product as a fragment: rounded to bf16, 2^-9 each, as every operand of the matrix cores is; sums stay in fp32.
+    // Eight results of a product as a fragment: rounded to bf16, by 2^-8 of itself at most, as every operand of the matrix cores is; sums stay in fp32.
     static __device__ __forceinline__ type pack(const f32x16& s, int h)
     {
         const u32x4 v = {pack_bf16x2(s[8 * h], s[8 * h + 1]), pack_bf16x2(s[8 * h + 2], s[8 * h + 3]), pack_bf16x2(s[8 * h + 4], s[8 * h + 5]), pack_bf16x2(s[8 * h + 6], s[8 * h + 7])};

@@ -416,7 +416,8 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
     if (e != hipSuccess) return e;
     // parts of the same number of tiles, whatever a sequence's length, so that blocks take equally long; those past a sequence's end have nothing to do.  Where there are
     // blocks for all CUs without them they only cost: 1024 rows, 8 heads of 128, 264 blocks, causal: 42 us with, 15 without.  A token of each of 16 sequences over 1 to 16384
-    // keys, 32 and 8 heads of 128, 144 blocks, us: 2048 parts 120, 1024 111, 512 104 (517 MB, 5.0 TB/s), none 197
+    // keys, 32 and 8 heads of 128, 144 blocks, us: 2048 parts 120, 1024 111, 512 104 (517 MB, 5.0 TB/s), none 197.  Lengths are known to the device alone, so parts are as
+    // long as the cache has room for: one token over 4096 keys 15 us in a cache of 4096 rows, 18 of 16384, 30 of 131072; sixteen of them 53, 49, 49
     const long long units = few_units(a);
     const long long tiles = ((long long)a.k_rows / a.seqs + FEW_KEYS - 1) / FEW_KEYS;
     const long long want = units <= 256 ? ATTN_PARTS / units : 1, most = (tiles + 2 * FEW_WAVES - 1) / (2 * FEW_WAVES);
@@ -433,7 +434,8 @@ template <typename ET, int DP> hipError_t launch_few(attn_args a, hipStream_t st
 template <typename ET, int DP> hipError_t attend(const attn_args& a, hipStream_t st)
 {
     // or few rows a sequence, whatever their number: up to 16, or 32 of heads that share nothing, over 4096 keys, 32 and 8 heads of 128, us, small | large blocks:
-    // 8 rows 88 | 119, 16 86 | 120, 32 136 | 121; over 1024, 32 and 32 heads of 64: 32 rows 117 | 126, 64 158 | 132
+    // 8 rows 88 | 119, 16 86 | 120, 32 136 | 121; over 1024, 32 and 32 heads of 64: 32 rows 117 | 126, 64 158 | 132.  It is the average that counts: a sequence of
+    // 16384 and 1023 empty ones, 32 and 8 heads of 128, take 4620 us so, 1710 where the call has one sequence
     if ((long long)a.q_rows <= (a.group == 1 ? 32ll : 16ll) * a.seqs || is_small<ET, DP>(((long long)a.q_rows / SIDE + a.seqs) * a.heads, false)) return launch_few<ET, DP>(a, st);
     return launch_rows<ET, DP>(a, st);
 }

@@ -9,7 +9,7 @@
 // the halves of a head are pairs and whole pieces, a thread has both pieces of its pairs and no word goes between lanes.  Angles are 64-bit products reduced
 // to a turn before they are rounded (a position of 10^6 leaves fp32 two digits of its angle), once per row for all heads, kept in LDS.
 //
-// 32768 rows of 32 and 8 heads of 128, bf16, norms: forward 671 MB in 137 us (4.9 TB/s), gradient 1006 MB in 206 us (4.9 TB/s); a large copy reaches 5.2 TB/s.
+// 32768 rows of 32 and 8 heads of 128, bf16, norms: forward 671 MB in 131 us (5.1 TB/s), gradient 1006 MB in 205 us (4.9 TB/s); a large copy reaches 5.2 TB/s.
 // 16 tokens into a cache 4.7 us, one launch; 512 rows of 2 and 2 heads of 32, fp32, gradient with norms 9.1 us, two launches.
 #include "internal.h"
 
